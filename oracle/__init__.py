@@ -27,9 +27,13 @@ and the token lifetimes [t, e_t) that the running mask reduces to, are in
 The target epilogue of App. D.4 step 5 (aggregation over the G query heads and
 count normalisation, App. B.1-B.2) is in ``oracle.target``.
 
+The compact cache of a served model (8-bit pages, append, attention over page lists,
+retention one token at a time) is in ``oracle.compact_cache``.
+
 Every function here is pinned by tests against closed forms, hand enumeration and
-brute force (tests/test_oracle_pins.py); no function is "parity unpinned".
+brute force (tests/test_oracle_pins.py, tests/test_oracle_*.py); no function is "parity unpinned".
 """
+from . import compact_cache  # noqa: F401
 from .future_mass import (  # noqa: F401
     bf16_bits_to_f64,
     causal_logits,

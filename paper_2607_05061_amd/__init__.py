@@ -23,7 +23,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from typing import Optional, Tuple
+from typing import Any, NamedTuple, Optional, Tuple
 
 __all__ = [
     "KVPOP_OK", "KVPOP_EINVAL", "KVPOP_EUNSUPPORTED", "KVPOP_EHIP", "KvpopDims", "KvpopError",
@@ -31,6 +31,9 @@ __all__ = [
     "kvpop_future_attn_scores", "kvpop_strerror", "kvpop_abi_version", "KVPOP_AGG_MAX", "KVPOP_AGG_MEAN",
     "KvpopTopkDims", "kvpop_running_topk", "kvpop_running_topk_workspace_size", "kvpop_sparse_attn_fwd",
     "kvpop_running_topk_noalloc", "KVPOP_ETOOBIG", "KVPOP_NOALLOC_SCRATCH_BYTES", "kvpop_future_attn_bands",
+    "KVPOP_CACHE_INT8", "KVPOP_CACHE_E4M3", "KvpopCache", "KvpopCacheC", "KvpopRowsC", "KvpopAppendC", "KvpopRetainC",
+    "kvpop_cache_empty", "kvpop_cache_append", "kvpop_cache_attn", "kvpop_cache_attn_workspace_size",
+    "kvpop_retain_prompt", "kvpop_retain_step",
 ]
 
 KVPOP_OK = 0
@@ -41,6 +44,8 @@ KVPOP_ETOOBIG = 4
 KVPOP_NOALLOC_SCRATCH_BYTES = 32 << 20
 KVPOP_AGG_MAX = 0
 KVPOP_AGG_MEAN = 1
+KVPOP_CACHE_INT8 = 0
+KVPOP_CACHE_E4M3 = 1
 ABI_VERSION = 3
 
 _PKG_DIR = os.path.dirname(os.path.abspath(__file__))
@@ -62,6 +67,35 @@ class KvpopDims(ctypes.Structure):
 class KvpopTopkDims(ctypes.Structure):
     """Mirror of ``kvpop_topk_dims`` in include/kvpop.h."""
     _fields_ = [("batch", ctypes.c_int32), ("n_heads", ctypes.c_int32), ("seq_len", ctypes.c_int32)]
+
+
+class KvpopCacheC(ctypes.Structure):
+    """Mirror of ``kvpop_cache`` in include/kvpop_cache.h."""
+    _fields_ = [(n, ctypes.c_int32) for n in ("batch", "n_kv_heads", "head_dim", "format", "page_size", "n_pages",
+                                              "max_pages")]
+    _fields_ += [(n, ctypes.c_void_p) for n in ("k_pages", "v_pages", "k_exp", "v_exp", "page_table")]
+
+
+class KvpopRowsC(ctypes.Structure):
+    """Mirror of ``kvpop_rows`` in include/kvpop_cache.h."""
+    _fields_ = [("ptr", ctypes.c_void_p), ("stride_b", ctypes.c_int64), ("stride_h", ctypes.c_int64),
+                ("stride_t", ctypes.c_int64)]
+
+
+class KvpopAppendC(ctypes.Structure):
+    """Mirror of ``kvpop_append`` in include/kvpop_cache.h."""
+    _fields_ = [("n_tokens", ctypes.c_int32), ("n_entries", ctypes.c_int32), ("k", KvpopRowsC), ("v", KvpopRowsC),
+                ("held", ctypes.c_void_p), ("count", ctypes.c_void_p), ("start", ctypes.c_void_p),
+                ("src", ctypes.c_void_p), ("pos0", ctypes.c_void_p), ("cos", ctypes.c_void_p),
+                ("sin", ctypes.c_void_p), ("n_positions", ctypes.c_int32), ("rot_dim", ctypes.c_int32),
+                ("adjacent", ctypes.c_int32), ("n_q_heads", ctypes.c_int32), ("q", KvpopRowsC),
+                ("q_out", ctypes.c_void_p)]
+
+
+class KvpopRetainC(ctypes.Structure):
+    """Mirror of ``kvpop_retain`` in include/kvpop_cache.h."""
+    _fields_ = [("batch", ctypes.c_int32), ("n_heads", ctypes.c_int32), ("slots", ctypes.c_int32),
+                ("pos", ctypes.c_void_p), ("prio", ctypes.c_void_p), ("held", ctypes.c_void_p)]
 
 
 class KvpopError(RuntimeError):
@@ -108,6 +142,17 @@ def lib() -> ctypes.CDLL:
         L.kvpop_running_topk_noalloc.restype = ctypes.c_int
         L.kvpop_sparse_attn_fwd.argtypes = [ctypes.POINTER(KvpopDims), P, P, P, P, P, P, P, P]
         L.kvpop_sparse_attn_fwd.restype = ctypes.c_int
+        C, R, S = ctypes.POINTER(KvpopCacheC), ctypes.POINTER(KvpopRowsC), ctypes.POINTER(KvpopRetainC)
+        L.kvpop_cache_append.argtypes = [C, ctypes.POINTER(KvpopAppendC), P]
+        L.kvpop_cache_append.restype = ctypes.c_int
+        L.kvpop_cache_attn_workspace_size.argtypes = [C, I32, I32]
+        L.kvpop_cache_attn_workspace_size.restype = ctypes.c_size_t
+        L.kvpop_cache_attn.argtypes = [C, I32, I32, F, R, P, P, P, P, P, ctypes.c_size_t, P]
+        L.kvpop_cache_attn.restype = ctypes.c_int
+        L.kvpop_retain_prompt.argtypes = [S, I32, P, P, P, P, P]
+        L.kvpop_retain_prompt.restype = ctypes.c_int
+        L.kvpop_retain_step.argtypes = [S, P, P, P, I32, I32, I32, P, P]
+        L.kvpop_retain_step.restype = ctypes.c_int
         L.kvpop_strerror.argtypes = [ctypes.c_int]
         L.kvpop_strerror.restype = ctypes.c_char_p
         L.kvpop_abi_version.argtypes = []
@@ -419,3 +464,235 @@ def kvpop_sparse_attn_fwd(q, k, v, evict, scale: float, key_bias=None, o=None, l
     if st != KVPOP_OK:
         raise KvpopError(st, "kvpop_sparse_attn_fwd")
     return o, lse
+
+
+# ---------------------------------------------------------------------------
+# The compact cache (include/kvpop_cache.h)
+# ---------------------------------------------------------------------------
+
+class KvpopCache(NamedTuple):
+    """A pool of 8-bit pages and the page lists of B sequences of H KV heads.
+
+    k_pages, v_pages: int8 or float8_e4m3fn [n_pages, P, D], P 16, 32, 64 or 128, D 64 or
+    128; k_exp, v_exp: int8 [n_pages], a page's values are code * 2 ** exp; page_table:
+    int32 [B, H, max_pages], slot j of a list is row j % P of entry j // P."""
+    k_pages: Any
+    v_pages: Any
+    k_exp: Any
+    v_exp: Any
+    page_table: Any
+
+
+def kvpop_cache_empty(batch: int, n_kv_heads: int, tokens: int, head_dim: int, page_size: int = 64,
+                      dtype=None, device="cuda") -> KvpopCache:
+    """A cache with room for ``tokens`` tokens in each list, its pages dealt to the lists in
+    order. dtype: torch.int8 (the default) or torch.float8_e4m3fn."""
+    torch = _torch()
+    per = -(-tokens // page_size)
+    n = batch * n_kv_heads * per
+    dtype = torch.int8 if dtype is None else dtype
+    pages = [torch.zeros((n, page_size, head_dim), dtype=torch.int8, device=device).view(dtype) for _ in range(2)]
+    exps = [torch.zeros(n, dtype=torch.int8, device=device) for _ in range(2)]
+    table = torch.arange(n, dtype=torch.int32, device=device).view(batch, n_kv_heads, per)
+    return KvpopCache(pages[0], pages[1], exps[0], exps[1], table)
+
+
+def _need(ok: bool, text: str):
+    if not ok:
+        raise ValueError(text)
+
+
+def _small(x, name: str, dtype, shape, device):
+    """A pointer to a contiguous tensor of this type and shape, or None."""
+    if x is None:
+        return None
+    _check_tensor(x, name, dtype, device)
+    if x.shape != shape:
+        raise ValueError("%s must be %s" % (name, list(shape)))
+    return x.data_ptr()
+
+
+def _cache_c(cache) -> KvpopCacheC:
+    torch = _torch()
+    k, v, ke, ve, table = cache
+    device = getattr(k, "device", None)
+    dtype = getattr(k, "dtype", None)
+    if dtype not in (torch.int8, torch.float8_e4m3fn):
+        raise TypeError("k_pages must be int8 or float8_e4m3fn")
+    _check_tensor(k, "k_pages", dtype, None)
+    _check_tensor(v, "v_pages", dtype, device)
+    _check_tensor(ke, "k_exp", torch.int8, device)
+    _check_tensor(ve, "v_exp", torch.int8, device)
+    _check_tensor(table, "page_table", torch.int32, device)
+    _need(k.dim() == 3 and v.shape == k.shape, "k_pages and v_pages must be [n_pages, P, D]")
+    n, P, D = k.shape
+    _need(ke.shape == (n,) and ve.shape == (n,), "k_exp and v_exp must be [n_pages]")
+    _need(table.dim() == 3, "page_table must be [B, H, max_pages]")
+    B, H, per = table.shape
+    return KvpopCacheC(B, H, D, KVPOP_CACHE_INT8 if dtype == torch.int8 else KVPOP_CACHE_E4M3, P, n, per,
+                       k.data_ptr(), v.data_ptr(), ke.data_ptr(), ve.data_ptr(), table.data_ptr())
+
+
+def _rows_c(x, name: str, lead, device) -> KvpopRowsC:
+    """A bf16 tensor [B, heads, N, D], strided but for its last dimension. lead: the sizes
+    that are given (None: any)."""
+    torch = _torch()
+    if not isinstance(x, torch.Tensor):
+        raise TypeError("%s must be a torch.Tensor" % name)
+    if x.device != device:
+        raise ValueError("%s must be on the GPU device of the cache" % name)
+    if x.dtype != torch.bfloat16:
+        raise TypeError("%s must be %s, got %s" % (name, torch.bfloat16, x.dtype))
+    shape = x.shape
+    if len(shape) != 4 or any(w is not None and w != g for w, g in zip(lead, shape)):
+        raise ValueError("%s must be [B, heads, N, D] = %s" % (name, list(lead)))
+    sb, sh, st, sd = x.stride()
+    if sd != 1:
+        raise ValueError("%s must be contiguous in its last dimension" % name)
+    # The stride of a dimension of one element means nothing.
+    return KvpopRowsC(x.data_ptr(), sb if shape[0] > 1 else 0, sh if shape[1] > 1 else 0, st if shape[2] > 1 else 0)
+
+
+def _call(name: str, device, *args):
+    """Calls an entry point with the device of its tensors as the current one: the default
+    stream's handle is that of whichever device is current."""
+    torch = _torch()
+    f = getattr(lib(), name)
+    if device.index == torch.cuda.current_device():
+        st = f(*args)
+    else:
+        with torch.cuda.device(device):
+            st = f(*args)
+    if st != KVPOP_OK:
+        raise KvpopError(st, name)
+
+
+def kvpop_cache_append(cache: KvpopCache, k, v, held, count=None, start=None, src=None, q=None, rotary=None,
+                       pos0=None, adjacent: bool = False, q_out=None, stream=None):
+    """New keys and values into the lists' pages, the keys (and queries) turned by their
+    positions. k, v: bf16 [B, H, N, D] (any strides that are multiples of 8); held: int32
+    [B, H], the lists' lengths after the call; count: int32 [B, H], how many tokens each list takes
+    (None: all); start: int32 [B, H], the first slot written, negative for none (None: held -
+    count); src: int32 [B, H, M], which tokens (None: 0, 1, ...); rotary: (cos, sin), fp32
+    [positions, R / 2] each; pos0: int32 [B], the position of token 0 (None: 0); adjacent: pairs
+    (2 j, 2 j + 1) instead of (j, j + R / 2). With q (bf16 [B, Hq, N, D]) returns it rotated,
+    bf16 [B, Hq, N, D] contiguous; else None. include/kvpop_cache.h has the exponents' rule."""
+    torch = _torch()
+    c = _cache_c(cache)
+    device = cache.k_pages.device
+    B, H, D = c.batch, c.n_kv_heads, c.head_dim
+    kr = _rows_c(k, "k", (B, H, None, D), device)
+    N = k.shape[2]
+    vr = _rows_c(v, "v", (B, H, N, D), device)
+    M = N
+    if src is not None:
+        M = src.shape[-1] if src.dim() == 3 else 0
+    a = KvpopAppendC(N, M, kr, vr)
+    a.held = _small(held, "held", torch.int32, (B, H), device)
+    a.count = _small(count, "count", torch.int32, (B, H), device)
+    a.start = _small(start, "start", torch.int32, (B, H), device)
+    a.src = _small(src, "src", torch.int32, (B, H, M), device)
+    a.pos0 = _small(pos0, "pos0", torch.int32, (B,), device)
+    if rotary is not None:
+        cos, sin = rotary
+        _check_tensor(cos, "cos", torch.float32, device)
+        _need(cos.dim() == 2, "cos and sin must be [positions, R / 2]")
+        a.n_positions, a.rot_dim, a.adjacent = cos.shape[0], 2 * cos.shape[1], int(bool(adjacent))
+        a.cos, a.sin = cos.data_ptr(), _small(sin, "sin", torch.float32, cos.shape, device)
+    if q is not None:
+        a.q = _rows_c(q, "q", (B, None, N, D), device)
+        a.n_q_heads = q.shape[1]
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=torch.bfloat16, device=device)
+        a.q_out = _small(q_out, "q_out", torch.bfloat16, q.shape, device)
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    _call("kvpop_cache_append", device, ctypes.byref(c), ctypes.byref(a), _stream_ptr(stream, device))
+    return q_out
+
+
+def kvpop_cache_attn_workspace_size(cache: KvpopCache, n_q_heads: int, n_tokens: int) -> int:
+    """Bytes of workspace of a kvpop_cache_attn call with q [B, n_q_heads, n_tokens, D]."""
+    return int(lib().kvpop_cache_attn_workspace_size(ctypes.byref(_cache_c(cache)), n_q_heads, n_tokens))
+
+
+def kvpop_cache_attn(q, cache: KvpopCache, held, scale: float, q_lens=None, o=None, lse=None, workspace=None,
+                     stream=None):
+    """Attention of the newest queries q (bf16 [B, Hq, N, D]) over the lists: query i of the n =
+    q_lens[b] (None: N) of a sequence sees the slots below held[b, h] - (n - 1 - i). Returns
+    (o bf16 [B, Hq, N, D], lse fp32 [B, Hq, N]); rows from n on, and queries that see
+    nothing, get 0 and -inf."""
+    torch = _torch()
+    c = _cache_c(cache)
+    device = cache.k_pages.device
+    qr = _rows_c(q, "q", (c.batch, None, None, c.head_dim), device)
+    Hq, N = q.shape[1], q.shape[2]
+    hp = _small(held, "held", torch.int32, (c.batch, c.n_kv_heads), device)
+    np_ = _small(q_lens, "q_lens", torch.int32, (c.batch,), device)
+    if o is None:
+        o = torch.empty(q.shape, dtype=torch.bfloat16, device=device)
+    op = _small(o, "o", torch.bfloat16, q.shape, device)
+    lse = _prep_out(lse, "lse", (c.batch, Hq, N), device)
+    cp = ctypes.byref(c)
+    need = lib().kvpop_cache_attn_workspace_size(cp, Hq, N)
+    if workspace is None:
+        if need:
+            if stream is None:
+                workspace = torch.empty(need, dtype=torch.uint8, device=device)
+            else:
+                with _on_launch_stream(stream, device):
+                    workspace = torch.empty(need, dtype=torch.uint8, device=device)
+    elif workspace.numel() * workspace.element_size() < need or workspace.device != device:
+        raise ValueError("workspace must hold %d bytes on the device of the cache" % need)
+    _call("kvpop_cache_attn", device, cp, Hq, N, float(scale), ctypes.byref(qr), hp, np_, op, lse.data_ptr(),
+          workspace.data_ptr() if workspace is not None else None, need, _stream_ptr(stream, device))
+    return o, lse
+
+
+def kvpop_retain_prompt(evict, scores, budget: int, log_gamma=None, lens=None, pos=None, prio=None, held=None,
+                        stream=None):
+    """The tokens that a prompt's end keeps, from kvpop_running_topk's evict and its scores
+    (both [B, H, T]): (pos int32 [B, H, budget], prio fp32 [B, H, budget], held int32 [B, H]),
+    ascending positions, then -1 and -inf. lens: int32 [B], the prompts' lengths (None: T)."""
+    torch = _torch()
+    _check_tensor(scores, "scores", torch.float32, None)
+    _need(scores.dim() == 3, "scores must be [B, H, T]")
+    device = scores.device
+    B, H, T = scores.shape
+    ep = _small(evict, "evict", torch.int32, scores.shape, device)
+    lg = _small(log_gamma, "log_gamma", torch.float32, (H,), device)
+    lp = _small(lens, "lens", torch.int32, (B,), device)
+    S = int(budget)
+    _need(S >= 1, "budget must be positive")
+    if pos is None:
+        pos = torch.empty((B, H, S), dtype=torch.int32, device=device)
+    if held is None:
+        held = torch.empty((B, H), dtype=torch.int32, device=device)
+    prio = _prep_out(prio, "prio", (B, H, S), device)
+    s = KvpopRetainC(B, H, S, _small(pos, "pos", torch.int32, (B, H, S), device), prio.data_ptr(),
+                     _small(held, "held", torch.int32, (B, H), device))
+    _call("kvpop_retain_prompt", device, ctypes.byref(s), T, ep, scores.data_ptr(), lg, lp, _stream_ptr(stream, device))
+    return pos, prio, held
+
+
+def kvpop_retain_step(scores, q_pos, pos, prio, held, sinks: int, window: int, topk: int, log_gamma=None,
+                      slot=None, stream=None):
+    """The running top-k for single tokens: which slot (int32 [B, H], -1 for none) the
+    token at q_pos (int32 [B], negative for an idle sequence) takes in each list of at most sinks
+    + window + topk tokens. scores: fp32 [B, H], of the token at q_pos - window, which leaves
+    the protected window. Updates pos, prio ([B, H, S]) and held ([B, H]) in place."""
+    torch = _torch()
+    _check_tensor(pos, "pos", torch.int32, None)
+    _need(pos.dim() == 3, "pos must be [B, H, S]")
+    device = pos.device
+    B, H, S = pos.shape
+    s = KvpopRetainC(B, H, S, pos.data_ptr(), _small(prio, "prio", torch.float32, pos.shape, device),
+                     _small(held, "held", torch.int32, (B, H), device))
+    rp = _small(scores, "scores", torch.float32, (B, H), device)
+    qp = _small(q_pos, "q_pos", torch.int32, (B,), device)
+    lg = _small(log_gamma, "log_gamma", torch.float32, (H,), device)
+    if slot is None:
+        slot = torch.empty((B, H), dtype=torch.int32, device=device)
+    _call("kvpop_retain_step", device, ctypes.byref(s), rp, lg, qp, int(sinks), int(window), int(topk),
+          _small(slot, "slot", torch.int32, (B, H), device), _stream_ptr(stream, device))
+    return slot

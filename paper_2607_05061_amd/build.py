@@ -1,7 +1,7 @@
 """Build the in-tree shared library ``libkvpop.so`` for gfx950 with hipcc.
 
 Run as ``python -m paper_2607_05061_amd.build``. The library has no PyTorch
-dependency: its C ABI (include/kvpop.h) takes plain device pointers. Each source
+dependency: its C ABI (include/kvpop.h, include/kvpop_cache.h) takes plain device pointers. Each source
 is compiled to its own object (in parallel), then the objects are linked.
 """
 from __future__ import annotations
@@ -18,7 +18,8 @@ CSRC = os.path.join(PKG_DIR, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB_NAME = "libkvpop.so"
 LIB_PATH = os.path.join(PKG_DIR, LIB_NAME)
-SOURCES = ["kvpop_api.cpp", "kvpop_kernels.hip", "kvpop_topk.hip", "kvpop_sparse_attn.hip"]
+SOURCES = ["kvpop_api.cpp", "kvpop_kernels.hip", "kvpop_topk.hip", "kvpop_sparse_attn.hip",
+           "kvpop_cache.hip", "kvpop_cache_attn.hip"]
 
 # Packed fp32 VALU forms are disabled for all device code.
 HIP_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

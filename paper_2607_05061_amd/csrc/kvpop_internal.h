@@ -65,6 +65,66 @@ struct SparseLaunch {
 };
 void sparse_attn_plan(SparseLaunch& L);
 
+// The compact cache (kvpop_cache.hip, kvpop_cache_attn.hip). All sizes already validated.
+struct Rows {
+  const uint16_t* ptr;      // bf16, last dimension contiguous
+  int64_t sb, sh, st;       // strides in elements
+};
+
+struct CacheView {
+  uint8_t *k, *v;           // [n_pages, P, D] codes
+  int8_t *ke, *ve;          // [n_pages] exponents
+  const int32_t* table;     // [B, H, max_pages]
+  int32_t B, H, D, P, n_pages, max_pages, format;
+};
+
+struct AppendLaunch {
+  CacheView c;
+  Rows q, k, v;             // q.ptr nullptr without queries
+  uint16_t* q_out;
+  const int32_t *held, *count, *start, *src, *pos0;
+  const float *cos, *sin;
+  int32_t Hq, N, M, n_positions, rot, adjacent;
+  void* stream;
+};
+
+struct CacheAttnLaunch {
+  CacheView c;
+  Rows q;
+  const int32_t *held, *q_lens;
+  uint16_t* o;              // bf16 [B, Hq, N, D]
+  float* lse;               // fp32 [B, Hq, N]
+  float* workspace;
+  int32_t Hq, N;
+  float scale;
+  void* stream;
+};
+
+struct RetainLaunch {
+  int32_t B, H, S;
+  int32_t* pos;             // [B, H, S]
+  float* prio;              // [B, H, S]
+  int32_t* held;            // [B, H]
+  const float* scores;      // prompt: [B, H, T]; step: [B, H]
+  const float* log_gamma;   // [H] or nullptr
+  const int32_t* evict;     // prompt: [B, H, T]
+  const int32_t* lens;      // prompt: [B] or nullptr
+  const int32_t* q_pos;     // step: [B]
+  int32_t* slot;            // step: [B, H] out
+  int32_t T, sinks, window, topk;
+  void* stream;
+};
+
+int launch_cache_append(const AppendLaunch& L);
+int launch_cache_attn(const CacheAttnLaunch& L);
+int launch_retain_prompt(const RetainLaunch& L);
+int launch_retain_step(const RetainLaunch& L);
+// Workgroups of the launches above (checked against the grid limit), and floats of
+// workspace of the attention.
+int64_t cache_append_blocks(const AppendLaunch& L);
+int64_t cache_attn_blocks(const CacheAttnLaunch& L);
+int64_t cache_attn_workspace_floats(const CacheAttnLaunch& L);
+
 // Each returns 0 on success or the hipError_t of a failed launch.
 int launch_row_lse(const Launch& L);
 int launch_future_mass(const Launch& L);
