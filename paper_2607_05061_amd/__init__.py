@@ -23,6 +23,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Any, NamedTuple, Optional, Tuple
 
 __all__ = [
@@ -142,8 +143,9 @@ def lib() -> ctypes.CDLL:
         L.kvpop_running_topk_noalloc.restype = ctypes.c_int
         L.kvpop_sparse_attn_fwd.argtypes = [ctypes.POINTER(KvpopDims), P, P, P, P, P, P, P, P]
         L.kvpop_sparse_attn_fwd.restype = ctypes.c_int
-        C, R, S = ctypes.POINTER(KvpopCacheC), ctypes.POINTER(KvpopRowsC), ctypes.POINTER(KvpopRetainC)
-        L.kvpop_cache_append.argtypes = [C, ctypes.POINTER(KvpopAppendC), P]
+        # Structures go by address: a ctypes mirror by reference, or its packed bytes.
+        C = R = S = P
+        L.kvpop_cache_append.argtypes = [C, P, P]
         L.kvpop_cache_append.restype = ctypes.c_int
         L.kvpop_cache_attn_workspace_size.argtypes = [C, I32, I32]
         L.kvpop_cache_attn_workspace_size.restype = ctypes.c_size_t
@@ -497,72 +499,86 @@ def kvpop_cache_empty(batch: int, n_kv_heads: int, tokens: int, head_dim: int, p
     return KvpopCache(pages[0], pages[1], exps[0], exps[1], table)
 
 
+# The mirrors' fields in order, for calls that pack them at once.
+_CACHE_PACK = struct.Struct("7i4x5P")
+_ROWS_PACK = struct.Struct("P3q")
+_APPEND_PACK = struct.Struct("2i P3q P3q 7P 4i P3q P")
+_RETAIN_PACK = struct.Struct("3i4x3P")
+
+
 def _need(ok: bool, text: str):
     if not ok:
         raise ValueError(text)
 
 
-def _small(x, name: str, dtype, shape, device):
-    """A pointer to a contiguous tensor of this type and shape, or None."""
+def _ptr(x, name: str, dtype, shape, dev: int) -> int:
+    """The address of a contiguous tensor of this type and shape on GPU ``dev``; 0 for None."""
     if x is None:
-        return None
-    _check_tensor(x, name, dtype, device)
-    if x.shape != shape:
-        raise ValueError("%s must be %s" % (name, list(shape)))
-    return x.data_ptr()
+        return 0
+    try:
+        if x.dtype is dtype and x.get_device() == dev and x.shape == shape and x.is_contiguous():
+            return x.data_ptr()
+    except AttributeError:
+        pass
+    _check_tensor(x, name, dtype, _torch().device("cuda", dev))
+    raise ValueError("%s must be %s" % (name, list(shape)))
 
 
-def _cache_c(cache) -> KvpopCacheC:
+def _cache_parts(cache):
+    """A cache checked: (packed kvpop_cache, B, H, D, GPU index)."""
     torch = _torch()
     k, v, ke, ve, table = cache
-    device = getattr(k, "device", None)
+    i8 = torch.int8
     dtype = getattr(k, "dtype", None)
-    if dtype not in (torch.int8, torch.float8_e4m3fn):
+    if dtype is not i8 and dtype is not torch.float8_e4m3fn:
         raise TypeError("k_pages must be int8 or float8_e4m3fn")
-    _check_tensor(k, "k_pages", dtype, None)
-    _check_tensor(v, "v_pages", dtype, device)
-    _check_tensor(ke, "k_exp", torch.int8, device)
-    _check_tensor(ve, "v_exp", torch.int8, device)
-    _check_tensor(table, "page_table", torch.int32, device)
-    _need(k.dim() == 3 and v.shape == k.shape, "k_pages and v_pages must be [n_pages, P, D]")
-    n, P, D = k.shape
-    _need(ke.shape == (n,) and ve.shape == (n,), "k_exp and v_exp must be [n_pages]")
-    _need(table.dim() == 3, "page_table must be [B, H, max_pages]")
+    if not k.is_cuda:
+        _check_tensor(k, "k_pages", dtype, None)
+    _need(k.dim() == 3, "k_pages must be [n_pages, P, D]")
+    dev = k.get_device()
+    shape = k.shape
+    n, P, D = shape
+    _need(getattr(table, "shape", None) is not None and len(table.shape) == 3, "page_table must be [B, H, max_pages]")
     B, H, per = table.shape
-    return KvpopCacheC(B, H, D, KVPOP_CACHE_INT8 if dtype == torch.int8 else KVPOP_CACHE_E4M3, P, n, per,
-                       k.data_ptr(), v.data_ptr(), ke.data_ptr(), ve.data_ptr(), table.data_ptr())
+    packed = _CACHE_PACK.pack(B, H, D, KVPOP_CACHE_INT8 if dtype is i8 else KVPOP_CACHE_E4M3, P, n, per,
+                              _ptr(k, "k_pages", dtype, shape, dev), _ptr(v, "v_pages", dtype, shape, dev),
+                              _ptr(ke, "k_exp", i8, (n,), dev), _ptr(ve, "v_exp", i8, (n,), dev),
+                              _ptr(table, "page_table", torch.int32, (B, H, per), dev))
+    return packed, B, H, D, dev
 
 
-def _rows_c(x, name: str, lead, device) -> KvpopRowsC:
-    """A bf16 tensor [B, heads, N, D], strided but for its last dimension. lead: the sizes
-    that are given (None: any)."""
+def _rows(x, name: str, B: int, heads, N, D: int, dev: int):
+    """A bf16 tensor [B, heads, N, D] (heads, N None: any), strided but for its last dimension:
+    (address, strides of its first three), its heads and its tokens."""
     torch = _torch()
     if not isinstance(x, torch.Tensor):
         raise TypeError("%s must be a torch.Tensor" % name)
-    if x.device != device:
+    if x.get_device() != dev:
         raise ValueError("%s must be on the GPU device of the cache" % name)
-    if x.dtype != torch.bfloat16:
+    if x.dtype is not torch.bfloat16:
         raise TypeError("%s must be %s, got %s" % (name, torch.bfloat16, x.dtype))
     shape = x.shape
-    if len(shape) != 4 or any(w is not None and w != g for w, g in zip(lead, shape)):
-        raise ValueError("%s must be [B, heads, N, D] = %s" % (name, list(lead)))
+    if len(shape) != 4 or shape[0] != B or shape[3] != D or (heads or shape[1]) != shape[1] or (N or shape[2]) != shape[2]:
+        raise ValueError("%s must be [B, heads, N, D] = %s, got %s" % (name, [B, heads, N, D], list(shape)))
     sb, sh, st, sd = x.stride()
     if sd != 1:
         raise ValueError("%s must be contiguous in its last dimension" % name)
     # The stride of a dimension of one element means nothing.
-    return KvpopRowsC(x.data_ptr(), sb if shape[0] > 1 else 0, sh if shape[1] > 1 else 0, st if shape[2] > 1 else 0)
+    _, h, n, _ = shape
+    return (x.data_ptr(), sb if B > 1 else 0, sh if h > 1 else 0, st if n > 1 else 0), h, n
 
 
-def _call(name: str, device, *args):
-    """Calls an entry point with the device of its tensors as the current one: the default
-    stream's handle is that of whichever device is current."""
+def _call(name: str, dev: int, stream, *args):
+    """Calls an entry point on ``stream`` or the current one of GPU ``dev``, which is made the current
+    device: the default stream's handle is that of whichever device is current."""
     torch = _torch()
     f = getattr(lib(), name)
-    if device.index == torch.cuda.current_device():
-        st = f(*args)
+    handle = torch._C._cuda_getCurrentRawStream(dev) if stream is None else int(stream.cuda_stream)
+    if dev == torch._C._cuda_getDevice():
+        st = f(*args, handle)
     else:
-        with torch.cuda.device(device):
-            st = f(*args)
+        with torch.cuda.device(dev):
+            st = f(*args, handle)
     if st != KVPOP_OK:
         raise KvpopError(st, name)
 
@@ -578,42 +594,40 @@ def kvpop_cache_append(cache: KvpopCache, k, v, held, count=None, start=None, sr
     (2 j, 2 j + 1) instead of (j, j + R / 2). With q (bf16 [B, Hq, N, D]) returns it rotated,
     bf16 [B, Hq, N, D] contiguous; else None. include/kvpop_cache.h has the exponents' rule."""
     torch = _torch()
-    c = _cache_c(cache)
-    device = cache.k_pages.device
-    B, H, D = c.batch, c.n_kv_heads, c.head_dim
-    kr = _rows_c(k, "k", (B, H, None, D), device)
-    N = k.shape[2]
-    vr = _rows_c(v, "v", (B, H, N, D), device)
+    i32, bf16 = torch.int32, torch.bfloat16
+    c, B, H, D, dev = _cache_parts(cache)
+    kr, _, N = _rows(k, "k", B, H, None, D, dev)
+    vr, _, _ = _rows(v, "v", B, H, N, D, dev)
     M = N
     if src is not None:
         M = src.shape[-1] if src.dim() == 3 else 0
-    a = KvpopAppendC(N, M, kr, vr)
-    a.held = _small(held, "held", torch.int32, (B, H), device)
-    a.count = _small(count, "count", torch.int32, (B, H), device)
-    a.start = _small(start, "start", torch.int32, (B, H), device)
-    a.src = _small(src, "src", torch.int32, (B, H, M), device)
-    a.pos0 = _small(pos0, "pos0", torch.int32, (B,), device)
+    lists = (B, H)
+    cos = sin = n_positions = rot = 0
     if rotary is not None:
-        cos, sin = rotary
-        _check_tensor(cos, "cos", torch.float32, device)
-        _need(cos.dim() == 2, "cos and sin must be [positions, R / 2]")
-        a.n_positions, a.rot_dim, a.adjacent = cos.shape[0], 2 * cos.shape[1], int(bool(adjacent))
-        a.cos, a.sin = cos.data_ptr(), _small(sin, "sin", torch.float32, cos.shape, device)
+        t_cos, t_sin = rotary
+        _need(len(getattr(t_cos, "shape", ())) == 2, "cos and sin must be [positions, R / 2]")
+        n_positions, rot = t_cos.shape
+        cos = _ptr(t_cos, "cos", torch.float32, (n_positions, rot), dev)
+        sin = _ptr(t_sin, "sin", torch.float32, (n_positions, rot), dev)
+    qr, Hq, qo = (0, 0, 0, 0), 0, 0
     if q is not None:
-        a.q = _rows_c(q, "q", (B, None, N, D), device)
-        a.n_q_heads = q.shape[1]
+        qr, Hq, _ = _rows(q, "q", B, None, N, D, dev)
         if q_out is None:
-            q_out = torch.empty(q.shape, dtype=torch.bfloat16, device=device)
-        a.q_out = _small(q_out, "q_out", torch.bfloat16, q.shape, device)
+            q_out = torch.empty((B, Hq, N, D), dtype=bf16, device=q.device)
+        qo = _ptr(q_out, "q_out", bf16, (B, Hq, N, D), dev)
     elif q_out is not None:
         raise ValueError("q_out without q")
-    _call("kvpop_cache_append", device, ctypes.byref(c), ctypes.byref(a), _stream_ptr(stream, device))
+    a = _APPEND_PACK.pack(N, M, *kr, *vr, _ptr(held, "held", i32, lists, dev), _ptr(count, "count", i32, lists, dev),
+                          _ptr(start, "start", i32, lists, dev), _ptr(src, "src", i32, (B, H, M), dev),
+                          _ptr(pos0, "pos0", i32, (B,), dev), cos, sin, n_positions, 2 * rot, 1 if adjacent else 0, Hq,
+                          *qr, qo)
+    _call("kvpop_cache_append", dev, stream, c, a)
     return q_out
 
 
 def kvpop_cache_attn_workspace_size(cache: KvpopCache, n_q_heads: int, n_tokens: int) -> int:
     """Bytes of workspace of a kvpop_cache_attn call with q [B, n_q_heads, n_tokens, D]."""
-    return int(lib().kvpop_cache_attn_workspace_size(ctypes.byref(_cache_c(cache)), n_q_heads, n_tokens))
+    return int(lib().kvpop_cache_attn_workspace_size(_cache_parts(cache)[0], n_q_heads, n_tokens))
 
 
 def kvpop_cache_attn(q, cache: KvpopCache, held, scale: float, q_lens=None, o=None, lse=None, workspace=None,
@@ -623,29 +637,27 @@ def kvpop_cache_attn(q, cache: KvpopCache, held, scale: float, q_lens=None, o=No
     (o bf16 [B, Hq, N, D], lse fp32 [B, Hq, N]); rows from n on, and queries that see
     nothing, get 0 and -inf."""
     torch = _torch()
-    c = _cache_c(cache)
-    device = cache.k_pages.device
-    qr = _rows_c(q, "q", (c.batch, None, None, c.head_dim), device)
-    Hq, N = q.shape[1], q.shape[2]
-    hp = _small(held, "held", torch.int32, (c.batch, c.n_kv_heads), device)
-    np_ = _small(q_lens, "q_lens", torch.int32, (c.batch,), device)
+    i32 = torch.int32
+    c, B, H, D, dev = _cache_parts(cache)
+    qr, Hq, N = _rows(q, "q", B, None, None, D, dev)
     if o is None:
-        o = torch.empty(q.shape, dtype=torch.bfloat16, device=device)
-    op = _small(o, "o", torch.bfloat16, q.shape, device)
-    lse = _prep_out(lse, "lse", (c.batch, Hq, N), device)
-    cp = ctypes.byref(c)
-    need = lib().kvpop_cache_attn_workspace_size(cp, Hq, N)
+        o = torch.empty((B, Hq, N, D), dtype=torch.bfloat16, device=q.device)
+    if lse is None:
+        lse = torch.empty((B, Hq, N), dtype=torch.float32, device=q.device)
+    need = lib().kvpop_cache_attn_workspace_size(c, Hq, N)
     if workspace is None:
         if need:
             if stream is None:
-                workspace = torch.empty(need, dtype=torch.uint8, device=device)
+                workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
             else:
-                with _on_launch_stream(stream, device):
-                    workspace = torch.empty(need, dtype=torch.uint8, device=device)
-    elif workspace.numel() * workspace.element_size() < need or workspace.device != device:
+                with _on_launch_stream(stream, q.device):
+                    workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    elif workspace.numel() * workspace.element_size() < need or workspace.device != q.device:
         raise ValueError("workspace must hold %d bytes on the device of the cache" % need)
-    _call("kvpop_cache_attn", device, cp, Hq, N, float(scale), ctypes.byref(qr), hp, np_, op, lse.data_ptr(),
-          workspace.data_ptr() if workspace is not None else None, need, _stream_ptr(stream, device))
+    _call("kvpop_cache_attn", dev, stream, c, Hq, N, float(scale), _ROWS_PACK.pack(*qr),
+          _ptr(held, "held", i32, (B, H), dev), _ptr(q_lens, "q_lens", i32, (B,), dev),
+          _ptr(o, "o", torch.bfloat16, (B, Hq, N, D), dev), _ptr(lse, "lse", torch.float32, (B, Hq, N), dev),
+          workspace.data_ptr() if workspace is not None else 0, need)
     return o, lse
 
 
@@ -655,23 +667,23 @@ def kvpop_retain_prompt(evict, scores, budget: int, log_gamma=None, lens=None, p
     (both [B, H, T]): (pos int32 [B, H, budget], prio fp32 [B, H, budget], held int32 [B, H]),
     ascending positions, then -1 and -inf. lens: int32 [B], the prompts' lengths (None: T)."""
     torch = _torch()
-    _check_tensor(scores, "scores", torch.float32, None)
+    i32, f32 = torch.int32, torch.float32
+    _check_tensor(scores, "scores", f32, None)
     _need(scores.dim() == 3, "scores must be [B, H, T]")
-    device = scores.device
+    device, dev = scores.device, scores.get_device()
     B, H, T = scores.shape
-    ep = _small(evict, "evict", torch.int32, scores.shape, device)
-    lg = _small(log_gamma, "log_gamma", torch.float32, (H,), device)
-    lp = _small(lens, "lens", torch.int32, (B,), device)
     S = int(budget)
     _need(S >= 1, "budget must be positive")
     if pos is None:
-        pos = torch.empty((B, H, S), dtype=torch.int32, device=device)
+        pos = torch.empty((B, H, S), dtype=i32, device=device)
+    if prio is None:
+        prio = torch.empty((B, H, S), dtype=f32, device=device)
     if held is None:
-        held = torch.empty((B, H), dtype=torch.int32, device=device)
-    prio = _prep_out(prio, "prio", (B, H, S), device)
-    s = KvpopRetainC(B, H, S, _small(pos, "pos", torch.int32, (B, H, S), device), prio.data_ptr(),
-                     _small(held, "held", torch.int32, (B, H), device))
-    _call("kvpop_retain_prompt", device, ctypes.byref(s), T, ep, scores.data_ptr(), lg, lp, _stream_ptr(stream, device))
+        held = torch.empty((B, H), dtype=i32, device=device)
+    st = _RETAIN_PACK.pack(B, H, S, _ptr(pos, "pos", i32, (B, H, S), dev), _ptr(prio, "prio", f32, (B, H, S), dev),
+                           _ptr(held, "held", i32, (B, H), dev))
+    _call("kvpop_retain_prompt", dev, stream, st, T, _ptr(evict, "evict", i32, (B, H, T), dev), scores.data_ptr(),
+          _ptr(log_gamma, "log_gamma", f32, (H,), dev), _ptr(lens, "lens", i32, (B,), dev))
     return pos, prio, held
 
 
@@ -682,17 +694,17 @@ def kvpop_retain_step(scores, q_pos, pos, prio, held, sinks: int, window: int, t
     + window + topk tokens. scores: fp32 [B, H], of the token at q_pos - window, which leaves
     the protected window. Updates pos, prio ([B, H, S]) and held ([B, H]) in place."""
     torch = _torch()
-    _check_tensor(pos, "pos", torch.int32, None)
-    _need(pos.dim() == 3, "pos must be [B, H, S]")
-    device = pos.device
-    B, H, S = pos.shape
-    s = KvpopRetainC(B, H, S, pos.data_ptr(), _small(prio, "prio", torch.float32, pos.shape, device),
-                     _small(held, "held", torch.int32, (B, H), device))
-    rp = _small(scores, "scores", torch.float32, (B, H), device)
-    qp = _small(q_pos, "q_pos", torch.int32, (B,), device)
-    lg = _small(log_gamma, "log_gamma", torch.float32, (H,), device)
+    i32, f32 = torch.int32, torch.float32
+    _check_tensor(pos, "pos", i32, None)
+    shape = pos.shape
+    _need(len(shape) == 3, "pos must be [B, H, S]")
+    dev = pos.get_device()
+    B, H, S = shape
+    lists = (B, H)
     if slot is None:
-        slot = torch.empty((B, H), dtype=torch.int32, device=device)
-    _call("kvpop_retain_step", device, ctypes.byref(s), rp, lg, qp, int(sinks), int(window), int(topk),
-          _small(slot, "slot", torch.int32, (B, H), device), _stream_ptr(stream, device))
+        slot = torch.empty(lists, dtype=i32, device=pos.device)
+    st = _RETAIN_PACK.pack(B, H, S, pos.data_ptr(), _ptr(prio, "prio", f32, shape, dev), _ptr(held, "held", i32, lists, dev))
+    _call("kvpop_retain_step", dev, stream, st, _ptr(scores, "scores", f32, lists, dev),
+          _ptr(log_gamma, "log_gamma", f32, (H,), dev), _ptr(q_pos, "q_pos", i32, (B,), dev), int(sinks), int(window),
+          int(topk), _ptr(slot, "slot", i32, lists, dev))
     return slot

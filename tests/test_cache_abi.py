@@ -162,3 +162,17 @@ def test_binding_refuses_what_the_library_cannot_see():
                              torch.zeros(1, 1, 4), torch.zeros(1, 1, dtype=torch.int32), 1, 1, 1)
     with pytest.raises(ValueError, match="GPU"):
         kv.kvpop_retain_prompt(torch.zeros(1, 1, 4, dtype=torch.int32), torch.zeros(1, 1, 4), 4)
+
+
+def test_packed_structures_are_the_mirrors():
+    """The binding packs the structures' fields at once: sizes and offsets are ctypes' own."""
+    for pack, mirror in ((kv._CACHE_PACK, kv.KvpopCacheC), (kv._ROWS_PACK, kv.KvpopRowsC),
+                         (kv._APPEND_PACK, kv.KvpopAppendC), (kv._RETAIN_PACK, kv.KvpopRetainC)):
+        assert pack.size == ctypes.sizeof(mirror), mirror
+        n = len(pack.unpack(bytes(pack.size)))
+        x = mirror.from_buffer_copy(pack.pack(*range(1, n + 1)))
+        flat = []
+        for name, t in mirror._fields_:
+            v = getattr(x, name)
+            flat += [getattr(v, f) for f, _ in t._fields_] if t is kv.KvpopRowsC else [v]
+        assert flat == list(range(1, n + 1)), mirror
