@@ -94,8 +94,9 @@ def attention_check(q64, host, held, scale, o, lse, q_lens=None, where=None):
                 bound = (2.0 ** -8 * np.abs(ro) + (2.0 ** -11 + 2 * eps)[:, None] * (p @ np.abs(v)) + tiny) * 1.01 + 1e-30
                 err = np.abs(o[b, g, :n] - ro)
                 bad = ~(err <= bound)[some]
-                assert not bad.any(), "b%d qh%d: %d of %d out of bound, worst ratio %.3g" % (
-                    b, g, bad.sum(), bad.size, np.nanmax((err / bound)[some]))
+                assert not bad.any(), "b%d qh%d: %d of %d out of bound, worst ratio %.3g, (query, dim) %s: %s for %s" % (
+                    b, g, bad.sum(), bad.size, np.nanmax((err / bound)[some]), np.argwhere(bad)[:4].tolist(),
+                    o[b, g, :n][some][bad][:4], ro[some][bad][:4])
                 lerr = np.abs(lse[b, g, :n][some] - rl[some])
                 lb = (eps + 2.0 ** -22 * (np.abs(rl) + 1))[some]
                 assert (lerr <= lb).all(), "b%d qh%d lse: %.3g of bound" % (b, g, np.max(lerr / lb))
