@@ -630,6 +630,7 @@ int kvpop_retain_prompt(const kvpop_retain* s, int32_t seq_len, const int32_t* e
   L.evict = evict;
   L.lens = lens;
   L.T = seq_len;
+  if (lists * ((seq_len + 1023) / 1024) > INT32_MAX) return KVPOP_EUNSUPPORTED;  // more workgroups than a grid holds
   return launch([&] { return kvpop::launch_retain_prompt(L); });
 }
 

@@ -13,6 +13,9 @@ namespace {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kExpMin = -32, kExpMax = 32;
 
@@ -21,27 +24,25 @@ __device__ __forceinline__ int clampi(int x, int lo, int hi) { return min(max(x,
 __device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
 
-__device__ __forceinline__ void unpack8(const uint4& w, float (&x)[8]) {
-  const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    x[2 * i] = bf16_lo(u[i]);
-    x[2 * i + 1] = bf16_hi(u[i]);
-  }
-}
-
 // ---------------------------------------------------------------------------
 // Codes
 // ---------------------------------------------------------------------------
 
 // The least e with a <= qmax 2^e, into [kExpMin, kExpMax]; a >= 0 and finite. With a =
 // m 2^x, m in [1/2, 1): 127 2^e = (127/128) 2^(e+7) and 448 2^e = (7/8) 2^(e+9).
-template <int FMT>
-__device__ __forceinline__ int needed_exponent(double a) {
-  if (a == 0.0) return kExpMin;
-  const double m = __builtin_amdgcn_frexp_mant(a);
-  const int x = __builtin_amdgcn_frexp_exp(a);
-  const int e = FMT == KVPOP_CACHE_INT8 ? x - (m <= 127.0 / 128.0 ? 7 : 6) : x - (m <= 0.875 ? 9 : 8);
+template <int FMT, class F>
+__device__ __forceinline__ int needed_exponent(F a) {
+  if (a == 0) return kExpMin;
+  int x;
+  bool low;
+  if constexpr (sizeof(F) == 8) {
+    x = __builtin_amdgcn_frexp_exp(a);
+    low = __builtin_amdgcn_frexp_mant(a) <= (FMT == KVPOP_CACHE_INT8 ? 127.0 / 128.0 : 0.875);
+  } else {
+    x = __builtin_amdgcn_frexp_expf(a);
+    low = __builtin_amdgcn_frexp_mantf(a) <= (FMT == KVPOP_CACHE_INT8 ? 127.f / 128.f : 0.875f);
+  }
+  const int e = FMT == KVPOP_CACHE_INT8 ? x - (low ? 7 : 6) : x - (low ? 9 : 8);
   return clampi(e, kExpMin, kExpMax);
 }
 
@@ -55,24 +56,33 @@ __device__ __forceinline__ float to_odd(double y) {
   return __uint_as_float(b);
 }
 
-// Four codes of y[0..3] (already divided by the scale); NaN gives 0.
-template <int FMT>
-__device__ __forceinline__ uint32_t codes4(const double* y) {
+__device__ __forceinline__ float to_odd(float y) { return y; }
+
+__device__ __forceinline__ double scaled(double y, int e) { return __builtin_ldexp(y, e); }
+__device__ __forceinline__ float scaled(float y, int e) { return __builtin_ldexpf(y, e); }
+__device__ __forceinline__ int nearest(double y) { return (int)__builtin_rint(y); }
+__device__ __forceinline__ int nearest(float y) { return (int)__builtin_rintf(y); }
+__device__ __forceinline__ double larger(double m, double y) { return __builtin_fmax(m, __builtin_fabs(y)); }
+__device__ __forceinline__ float larger(float m, float y) { return __builtin_fmaxf(m, __builtin_fabsf(y)); }
+
+// y saturated; NaN gives 0.
+__device__ __forceinline__ double saturated(double y, double q) {
+  return y == y ? __builtin_fmin(__builtin_fmax(y, -q), q) : 0.0;
+}
+__device__ __forceinline__ float saturated(float y, float q) {
+  return y == y ? __builtin_fminf(__builtin_fmaxf(y, -q), q) : 0.f;
+}
+
+// Four codes of y[0..3] (already divided by the scale, and within the codes' range).
+template <int FMT, class F>
+__device__ __forceinline__ uint32_t codes4(const F* y) {
   if constexpr (FMT == KVPOP_CACHE_INT8) {
-    uint32_t r = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const double c = y[i] == y[i] ? __builtin_fmin(__builtin_fmax(y[i], -127.0), 127.0) : 0.0;
-      r |= ((uint32_t)(int)__builtin_rint(c) & 0xFFu) << (8 * i);
-    }
-    return r;
+    const uint32_t lo = __builtin_amdgcn_perm((uint32_t)nearest(y[1]), (uint32_t)nearest(y[0]), 0x0C0C0400u);
+    const uint32_t hi = __builtin_amdgcn_perm((uint32_t)nearest(y[3]), (uint32_t)nearest(y[2]), 0x04000C0Cu);
+    return lo | hi;
   } else {
-    float f[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      f[i] = to_odd(y[i] == y[i] ? __builtin_fmin(__builtin_fmax(y[i], -448.0), 448.0) : 0.0);
-    int r = __builtin_amdgcn_cvt_pk_fp8_f32(f[0], f[1], 0, false);
-    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(f[2], f[3], r, true);
+    const int r = __builtin_amdgcn_cvt_pk_fp8_f32(to_odd(y[0]), to_odd(y[1]), 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(to_odd(y[2]), to_odd(y[3]), r, true);
   }
 }
 
@@ -101,170 +111,282 @@ __device__ __forceinline__ uint32_t moved4(uint32_t w, int shift) {
 // Append
 // ---------------------------------------------------------------------------
 
-// Elements 8 c .. 8 c + 7 of R(p) applied to a row, F = float or double. row: the row's
-// first element; cs, sn: the position's table rows.
+// A thread holds two pieces of 8 elements of a row. Pieces that turn into each other (halves)
+// go together, so that a row and its angles are read once: piece j with j + R / 16 below
+// the R / 16 pairs, neighbours (2 j, 2 j + 1) otherwise.
+struct Pieces {
+  int a, b;     // element offsets of the two pieces
+  bool turn;    // by the 8 angles from t on
+  int t;
+};
+__device__ __forceinline__ Pieces pieces(int j, int rot, int adjacent) {
+  const bool halves = !adjacent && 16 * j < rot;
+  const int half = rot / 2;
+  if (halves) return {8 * j, 8 * j + half, true, 8 * j};
+  return {16 * j, 16 * j + 8, 16 * j < rot, 8 * j};
+}
+
+struct Words8 {
+  u32x4 a, b;
+};
+__device__ __forceinline__ Words8 load_pieces(const uint16_t* row, const Pieces& pc) {
+  return {*reinterpret_cast<const u32x4*>(row + pc.a), *reinterpret_cast<const u32x4*>(row + pc.b)};
+}
+
+struct Angles {
+  f32x4 c[2], s[2];
+};
+__device__ __forceinline__ Angles load_angles(const float* cs, const float* sn, const Pieces& pc) {
+  return {{*reinterpret_cast<const f32x4*>(cs + pc.t), *reinterpret_cast<const f32x4*>(cs + pc.t + 4)},
+          {*reinterpret_cast<const f32x4*>(sn + pc.t), *reinterpret_cast<const f32x4*>(sn + pc.t + 4)}};
+}
+
+// The first and second elements of the 8 pairs.
+__device__ __forceinline__ void paired(const Words8& w, int adjacent, float (&a)[8], float (&b)[8]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t u0 = i < 2 ? w.a[2 * i] : w.b[2 * i - 4], u1 = i < 2 ? w.a[2 * i + 1] : w.b[2 * i - 3];
+    const uint32_t p = adjacent ? __builtin_amdgcn_perm(u1, u0, 0x05040100u) : w.a[i];
+    const uint32_t q = adjacent ? __builtin_amdgcn_perm(u1, u0, 0x07060302u) : w.b[i];
+    a[2 * i] = bf16_lo(p), a[2 * i + 1] = bf16_hi(p);
+    b[2 * i] = bf16_lo(q), b[2 * i + 1] = bf16_hi(q);
+  }
+}
+
+// The pairs turned, F = float or double (where products of bf16 and fp32 are exact).
 template <class F>
-__device__ __forceinline__ void rotated8(const uint16_t* row, int c, int rot, int adjacent, const float* cs,
-                                         const float* sn, F (&y)[8]) {
-  float x[8];
-  unpack8(*reinterpret_cast<const uint4*>(row + 8 * c), x);
-  if (8 * c >= rot) {
+__device__ __forceinline__ void turned(const float (&a)[8], const float (&b)[8], bool turn, const Angles& g, F (&x)[8],
+                                       F (&y)[8]) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = (F)x[i];
-  } else if (adjacent) {
-    const float4 co = *reinterpret_cast<const float4*>(cs + 4 * c), si = *reinterpret_cast<const float4*>(sn + 4 * c);
-    const float cc[4] = {co.x, co.y, co.z, co.w}, ss[4] = {si.x, si.y, si.z, si.w};
+  for (int i = 0; i < 8; ++i) {
+    const F c = g.c[i / 4][i % 4], s = g.s[i / 4][i % 4], p = a[i], q = b[i];
+    x[i] = turn ? p * c - q * s : p;
+    y[i] = turn ? q * c + p * s : q;
+  }
+}
+
+// 0, or NaN if a turned value may be NaN or infinite: what goes into it, times 0 (products of
+// bf16 and fp32 do not pass the range of 64 bits).
+__device__ __forceinline__ float not_finite(const float (&a)[8], const float (&b)[8], const Angles& g) {
+  float r = 0.f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const F a = x[2 * i], b = x[2 * i + 1];
-      y[2 * i] = a * (F)cc[i] - b * (F)ss[i];
-      y[2 * i + 1] = b * (F)cc[i] + a * (F)ss[i];
-    }
-  } else {
-    const int half = rot / 16;  // chunks per half
-    const bool second = c >= half;
-    const int j = 8 * (second ? c - half : c);
-    float z[8];
-    unpack8(*reinterpret_cast<const uint4*>(row + 8 * (second ? c - half : c + half)), z);
+  for (int i = 0; i < 8; ++i) {
+    r = __builtin_fmaf(a[i], 0.f, r);
+    r = __builtin_fmaf(b[i], 0.f, r);
+    r = __builtin_fmaf(g.c[i / 4][i % 4], 0.f, r);
+    r = __builtin_fmaf(g.s[i / 4][i % 4], 0.f, r);
+  }
+  return r;
+}
+
+constexpr int kQHeads = 4;  // query heads a thread turns by the same angles
+
+// The queries' part: D / 16 threads per token and kQHeads heads.
+template <int D>
+__device__ __forceinline__ void turn_queries(const AppendLaunch& a, int64_t blk) {
+  constexpr int C = D / 16;
+  const int groups = (a.Hq + kQHeads - 1) / kQHeads;
+  const int64_t item = blk * (blockDim.x / C) + threadIdx.x / C;  // (b, token, heads)
+  if (item >= (int64_t)a.c.B * a.N * groups) return;
+  const int hg = (int)(item % groups), n = (int)(item / groups % a.N), b = (int)(item / groups / a.N);
+  const Pieces pc = pieces(threadIdx.x % C, a.rot, a.adjacent);
+  const int64_t p = (a.pos0 ? a.pos0[b] : 0) + (int64_t)n;
+  const bool ok = a.rot == 0 || (p >= 0 && p < a.n_positions);
+  const uint16_t* x = a.q.ptr + b * a.q.sb + n * a.q.st;
+  Words8 w[kQHeads] = {};
+  Angles g = {};
+  if (ok) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const F s = second ? (F)sn[j + i] : -(F)sn[j + i];
-      y[i] = (F)x[i] * (F)cs[j + i] + (F)z[i] * s;
+    for (int i = 0; i < kQHeads; ++i)
+      w[i] = load_pieces(x + min(hg * kQHeads + i, a.Hq - 1) * a.q.sh, pc);
+    if (pc.turn) g = load_angles(a.cos + p * (a.rot / 2), a.sin + p * (a.rot / 2), pc);
+  }
+#pragma unroll
+  for (int i = 0; i < kQHeads; ++i) {
+    const int h = hg * kQHeads + i;
+    if (h < a.Hq) {
+      float p[8], q[8], x[8], y[8];
+      paired(w[i], a.adjacent, p, q);
+      turned(p, q, pc.turn, g, x, y);
+      union {
+        bf16x8 h;
+        u32x4 u;
+      } u, v;
+      f32x8 f0, f1;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) f0[k] = x[k], f1[k] = y[k];
+      u.h = __builtin_convertvector(f0, bf16x8);
+      v.h = __builtin_convertvector(f1, bf16x8);
+      u32x4 lo = u.u, hi = v.u;
+      if (a.adjacent) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          lo[2 * k] = __builtin_amdgcn_perm(v.u[k], u.u[k], 0x05040100u);
+          lo[2 * k + 1] = __builtin_amdgcn_perm(v.u[k], u.u[k], 0x07060302u);
+          hi[2 * k] = __builtin_amdgcn_perm(v.u[k + 2], u.u[k + 2], 0x05040100u);
+          hi[2 * k + 1] = __builtin_amdgcn_perm(v.u[k + 2], u.u[k + 2], 0x07060302u);
+        }
+      }
+      uint16_t* out = a.q_out + (((int64_t)b * a.Hq + h) * a.N + n) * D;
+      *reinterpret_cast<u32x4*>(out + pc.a) = lo;
+      *reinterpret_cast<u32x4*>(out + pc.b) = hi;
     }
   }
 }
 
-// One workgroup per (list, page that may get tokens, side): the rows of a page stay in
-// registers between the maximum, which needs all of them, and the codes. D / 8 threads
-// hold one row, 8 elements each. The workgroups after those turn the queries.
-template <int D, int FMT, int ITER>
-__global__ __launch_bounds__(512) void cache_append_kernel(AppendLaunch a, int pages, int64_t kv_blocks) {
-  constexpr int C = D / 8;
-  const int tid = threadIdx.x, c = tid % C, r0 = tid / C, rows = blockDim.x / C;
-  if ((int64_t)blockIdx.x >= kv_blocks) {
-    const int64_t row = ((int64_t)blockIdx.x - kv_blocks) * rows + r0;  // (b, head, token)
-    if (row >= (int64_t)a.c.B * a.Hq * a.N) return;
-    const int n = (int)(row % a.N);
-    const int64_t bh = row / a.N;
-    const int h = (int)(bh % a.Hq), b = (int)(bh / a.Hq);
-    const int64_t p = (a.pos0 ? a.pos0[b] : 0) + (int64_t)n;
-    float y[8];
-    if (a.rot == 0 || (p >= 0 && p < a.n_positions)) {
-      const int64_t t = a.rot ? p * (a.rot / 2) : 0;
-      rotated8(a.q.ptr + b * a.q.sb + h * a.q.sh + n * a.q.st, c, a.rot, a.adjacent, a.cos + t, a.sin + t, y);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) y[i] = 0.f;
-    }
-    f32x8 v;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = y[i];
-    *reinterpret_cast<bf16x8*>(a.q_out + row * D + 8 * c) = __builtin_convertvector(v, bf16x8);
-    return;
-  }
-  __shared__ int need_sh[8];
-  const int P = a.c.P;
-  const int side = (int)(blockIdx.x & 1);
-  const int list = (int)((blockIdx.x >> 1) / (unsigned)pages), nth = (int)((blockIdx.x >> 1) % (unsigned)pages);
-  const int b = list / a.c.H, h = list % a.c.H;
-  const int64_t held = a.held[list];
-  const int cnt = a.count ? clampi(a.count[list], 0, a.M) : a.M;
-  const int64_t start = a.start ? (int64_t)a.start[list] : held - cnt;
-  if (start < 0) return;
-  const int64_t page0 = start / P + nth;
-  if (page0 >= a.c.max_pages) return;
-  const int64_t first = page0 * P;
-  const int64_t lo = max(start, first), hi = min(start + cnt, first + P);
-  if (lo >= hi) return;
-  const int page = a.c.table[(int64_t)list * a.c.max_pages + page0];
-  if ((unsigned)page >= (unsigned)a.c.n_pages) return;
-  uint8_t* codes = (side ? a.c.v : a.c.k) + (int64_t)page * P * D;
-  int8_t* exps = side ? a.c.ve : a.c.ke;
-  // Rows of the page that other tokens use: below lo and from hi on, of the list's held.
-  const int before = (int)(min(lo, held) - first), after = (int)(min(held, first + P) - hi);
-  const bool others = before > 0 || after > 0;
-  const int was = others ? clampi(exps[page], kExpMin, kExpMax) : kExpMin;
+// What one workgroup writes: rows lo - first .. hi - first - 1 of a page, from the list's
+// entries lo - start on.
+struct PageJob {
+  int list, b, h, page, n_rows, first_row, entry;
+  int before, after;  // rows other tokens use: the first ones, and those behind the written ones
+  int was;            // the exponent these have
+};
 
-  const Rows x = side ? a.v : a.k;
-  const uint16_t* base = x.ptr + b * x.sb + h * x.sh;
-  const int rot = side ? 0 : a.rot;
-  const int n_rows = (int)(hi - lo);
-  double y[ITER][8];
-  double big = 0.0;
+template <int D, int FMT, int ITER, class F>
+__device__ __forceinline__ void write_page(const AppendLaunch& a, const PageJob& job, const Rows& x, int rot,
+                                           uint8_t* codes, int8_t* exps, int* need_sh) {
+  constexpr int C = D / 16;
+  const int tid = threadIdx.x, r0 = tid / C, rows = blockDim.x / C;
+  const Pieces pc = pieces(tid % C, rot, a.adjacent);
+  const uint16_t* base = x.ptr + job.b * x.sb + job.h * x.sh;
+  const int pos0 = a.pos0 ? a.pos0[job.b] : 0;
+  Words8 w[ITER];
+  Angles g[ITER];
 #pragma unroll
   for (int it = 0; it < ITER; ++it) {
     const int r = it * rows + r0;
-    bool ok = r < n_rows;
-    int64_t n = 0, t = 0;
-    if (ok) {
-      const int64_t i = lo - start + r;
-      n = a.src ? (int64_t)a.src[(int64_t)list * a.M + i] : i;
-      ok = n >= 0 && n < a.N;
-      if (rot) {
-        const int64_t p = (a.pos0 ? a.pos0[b] : 0) + n;
-        ok = ok && p >= 0 && p < a.n_positions;
-        t = p * (rot / 2);
+    w[it] = Words8{};  // a row that is not there is zeros
+    g[it] = Angles{};
+    if (r < job.n_rows) {
+      const int i = job.entry + r;
+      const int64_t n = a.src ? (int64_t)a.src[(int64_t)job.list * a.M + i] : i, p = pos0 + n;
+      if (n >= 0 && n < a.N && (rot == 0 || (p >= 0 && p < a.n_positions))) {
+        w[it] = load_pieces(base + n * x.st, pc);
+        if (pc.turn) g[it] = load_angles(a.cos + p * (rot / 2), a.sin + p * (rot / 2), pc);
       }
     }
-    if (ok) {
-      rotated8(base + n * x.st, c, rot, a.adjacent, a.cos + t, a.sin + t, y[it]);
-    } else {
+  }
+  F y[ITER][2][8], big = 0;
+  float odd = 0.f;  // NaN if a value may be NaN or infinite
 #pragma unroll
-      for (int i = 0; i < 8; ++i) y[it][i] = 0.0;
-    }
+  for (int it = 0; it < ITER; ++it) {
+    float p[8], q[8];
+    paired(w[it], a.adjacent, p, q);
+    turned(p, q, pc.turn && rot, g[it], y[it][0], y[it][1]);
+    odd += not_finite(p, q, g[it]);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const double v = __builtin_fabs(y[it][i]);
-      big = v < __builtin_inf() ? __builtin_fmax(big, v) : big;
-    }
+    for (int i = 0; i < 16; ++i) big = larger(big, y[it][i / 8][i % 8]);  // passes over NaN
+  }
+  if (odd != odd) {
+    big = 0;
+#pragma unroll
+    for (int it = 0; it < ITER; ++it)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const F v = larger(0, y[it][i / 8][i % 8]);
+        big = v < (F)__builtin_inff() ? larger(big, v) : big;
+      }
   }
   int need = needed_exponent<FMT>(big);
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) need = max(need, __shfl_xor(need, o));
   if ((tid & 63) == 0) need_sh[tid >> 6] = need;
   __syncthreads();
-  for (int w = 0; w < (int)(blockDim.x >> 6); ++w) need = max(need, need_sh[w]);
-  const int e = max(need, was);
+  for (int i = 0; i < (int)(blockDim.x >> 6); ++i) need = max(need, need_sh[i]);
+  const int e = max(need, job.was);
+#pragma unroll
+  for (int it = 0; it < ITER; ++it)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) y[it][i / 8][i % 8] = scaled(y[it][i / 8][i % 8], -e);
+  // Within the codes' range, unless a value is not finite or the largest scale does not hold it.
+  if (odd != odd || e == kExpMax) {
+#pragma unroll
+    for (int it = 0; it < ITER; ++it)
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        y[it][i / 8][i % 8] = saturated(y[it][i / 8][i % 8], (F)(FMT == KVPOP_CACHE_INT8 ? 127 : 448));
+  }
 #pragma unroll
   for (int it = 0; it < ITER; ++it) {
     const int r = it * rows + r0;
-    if (r < n_rows) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) y[it][i] = __builtin_ldexp(y[it][i], -e);
-      uint2 w;
-      w.x = codes4<FMT>(y[it]);
-      w.y = codes4<FMT>(y[it] + 4);
-      *reinterpret_cast<uint2*>(codes + (lo - first + r) * D + 8 * c) = w;
+    u32x2 lo = {codes4<FMT>(y[it][0]), codes4<FMT>(y[it][0] + 4)}, hi = {codes4<FMT>(y[it][1]), codes4<FMT>(y[it][1] + 4)};
+    if (a.adjacent) {
+      const u32x2 u = lo, v = hi;
+      lo = u32x2{__builtin_amdgcn_perm(v.x, u.x, 0x05010400u), __builtin_amdgcn_perm(v.x, u.x, 0x07030602u)};
+      hi = u32x2{__builtin_amdgcn_perm(v.y, u.y, 0x05010400u), __builtin_amdgcn_perm(v.y, u.y, 0x07030602u)};
+    }
+    if (r < job.n_rows) {
+      uint8_t* at = codes + (job.first_row + r) * D;
+      *reinterpret_cast<u32x2*>(at + pc.a) = lo;
+      *reinterpret_cast<u32x2*>(at + pc.b) = hi;
     }
   }
-  if (tid == 0) exps[page] = (int8_t)e;
-  if (others && e > was) {
-    const int n_old = max(before, 0) + max(after, 0);
+  if (tid == 0) exps[job.page] = (int8_t)e;
+  const int n_before = max(job.before, 0), n_old = n_before + max(job.after, 0);
+  if (n_old > 0 && e > job.was) {
     for (int i = r0; i < n_old; i += rows) {
-      const int64_t r = i < before ? i : hi - first + (i - max(before, 0));
-      uint2* at = reinterpret_cast<uint2*>(codes + r * D + 8 * c);
-      uint2 w = *at;
-      w.x = moved4<FMT>(w.x, was - e);
-      w.y = moved4<FMT>(w.y, was - e);
-      *at = w;
+      const int r = i < n_before ? i : job.first_row + job.n_rows + (i - n_before);
+      u32x4* at = reinterpret_cast<u32x4*>(codes + r * D + 16 * (tid % C));
+      u32x4 v = *at;
+      v.x = moved4<FMT>(v.x, job.was - e);
+      v.y = moved4<FMT>(v.y, job.was - e);
+      v.z = moved4<FMT>(v.z, job.was - e);
+      v.w = moved4<FMT>(v.w, job.was - e);
+      *at = v;
     }
   }
+}
+
+// One workgroup per (list, page that may get tokens, side): the rows of a page stay in
+// registers between the maximum, which needs all of them, and the codes. Keys that turn are held in
+// 64 bits, others in 32, where bf16 is exact. The workgroups after those turn the queries.
+template <int D, int FMT, int ITER>
+__global__ __launch_bounds__(512) void cache_append_kernel(AppendLaunch a, int pages, int64_t kv_blocks) {
+  __shared__ int need_sh[8];
+  if ((int64_t)blockIdx.x >= kv_blocks) {
+    turn_queries<D>(a, (int64_t)blockIdx.x - kv_blocks);
+    return;
+  }
+  const int P = a.c.P;
+  const int side = (int)(blockIdx.x & 1);
+  PageJob job;
+  job.list = (int)((blockIdx.x >> 1) / (unsigned)pages);
+  job.b = job.list / a.c.H, job.h = job.list % a.c.H;
+  const int64_t held = a.held[job.list];
+  const int cnt = a.count ? clampi(a.count[job.list], 0, a.M) : a.M;
+  const int64_t start = a.start ? (int64_t)a.start[job.list] : held - cnt;
+  if (start < 0) return;
+  const int64_t nth = start / P + (blockIdx.x >> 1) % (unsigned)pages;
+  if (nth >= a.c.max_pages) return;
+  const int64_t first = nth * P, lo = max(start, first), hi = min(start + cnt, first + P);
+  if (lo >= hi) return;
+  job.page = a.c.table[(int64_t)job.list * a.c.max_pages + nth];
+  if ((unsigned)job.page >= (unsigned)a.c.n_pages) return;
+  job.n_rows = (int)(hi - lo), job.first_row = (int)(lo - first), job.entry = (int)(lo - start);
+  job.before = (int)(min(lo, held) - first), job.after = (int)(min(held, first + P) - hi);
+  uint8_t* codes = (side ? a.c.v : a.c.k) + (int64_t)job.page * P * D;
+  int8_t* exps = side ? a.c.ve : a.c.ke;
+  job.was = job.before > 0 || job.after > 0 ? clampi(exps[job.page], kExpMin, kExpMax) : kExpMin;
+  if (side == 0 && a.rot)
+    write_page<D, FMT, ITER, double>(a, job, a.k, a.rot, codes, exps, need_sh);
+  else
+    write_page<D, FMT, ITER, float>(a, job, side ? a.v : a.k, 0, codes, exps, need_sh);
 }
 
 // Pages of a list that M consecutive slots can touch.
 int append_pages(const AppendLaunch& L) { return (L.M + L.c.P - 2) / L.c.P + 1; }
 
-// Threads per workgroup: four rows' worth of 8 elements per thread at most (up to 512
+// Threads per workgroup: two rows' worth of 16 elements per thread at most (up to 512
 // threads for the largest page), or one wave for a few tokens.
 struct AppendShape {
   int threads, iter;
 };
 AppendShape append_shape(const AppendLaunch& L) {
-  const int chunks = (L.M < L.c.P ? L.M : L.c.P) * (L.c.D / 8);
-  if (chunks <= 64) return {64, 1};
+  const int items = (L.M < L.c.P ? L.M : L.c.P) * (L.c.D / 16);
+  if (items <= 64) return {64, 1};
   int threads = 64;
-  while (4 * threads < chunks) threads *= 2;
-  return {threads, 4};
+  while (2 * threads < items) threads *= 2;
+  return {threads, 2};
 }
 
 template <int D, int FMT>
@@ -277,7 +399,7 @@ int launch_append(const AppendLaunch& L) {
   if (s.iter == 1)
     hipLaunchKernelGGL((cache_append_kernel<D, FMT, 1>), grid, block, 0, st, L, pages, kv);
   else
-    hipLaunchKernelGGL((cache_append_kernel<D, FMT, 4>), grid, block, 0, st, L, pages, kv);
+    hipLaunchKernelGGL((cache_append_kernel<D, FMT, 2>), grid, block, 0, st, L, pages, kv);
   return (int)hipGetLastError();
 }
 
@@ -357,37 +479,58 @@ __global__ __launch_bounds__(kStepThreads) void retain_step_kernel(RetainLaunch 
   a.slot[list] = slot;
 }
 
-constexpr int kPromptThreads = 1024;
+constexpr int kPromptThreads = 1024, kPromptEach = 4, kPromptPart = kPromptThreads * kPromptEach;
 
-// One workgroup per list: a stable compaction in steps of 1024 positions.
-__global__ __launch_bounds__(kPromptThreads) void retain_prompt_kernel(RetainLaunch a) {
+// A stable compaction: one workgroup per list and 4096 positions. It counts the kept tokens
+// before its part (a list's lifetimes are read from L2 by its later workgroups: at most T / 4096
+// times) and writes its own; the last one also clears the slots that are left.
+__global__ __launch_bounds__(kPromptThreads) void retain_prompt_kernel(RetainLaunch a, int parts) {
   constexpr int W = kPromptThreads / 64;
-  __shared__ int n_sh[2][W];
-  const int list = blockIdx.x, b = list / a.H, h = list % a.H, tid = threadIdx.x;
+  __shared__ int n_sh[W], own_sh[W];
+  const int list = blockIdx.x / parts, part = blockIdx.x % parts, b = list / a.H, h = list % a.H;
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const int n = a.lens ? clampi(a.lens[b], 0, a.T) : a.T;
+  const int begin = part * kPromptPart;
+  if (begin >= n && part > 0) return;
+  const bool last = begin + kPromptPart >= n;
   const int32_t* evict = a.evict + (int64_t)list * a.T;
   const float* r = a.scores + (int64_t)list * a.T;
   int32_t* pos = a.pos + (int64_t)list * a.S;
   float* prio = a.prio + (int64_t)list * a.S;
   const float lg = a.log_gamma ? a.log_gamma[h] : 0.f;
-  int held = 0, turn = 0;
-  for (int t0 = 0; t0 < n; t0 += kPromptThreads) {
-    const int t = t0 + tid;
-    const bool keep = t < n && evict[t] >= n;
-    const uint64_t m = __builtin_amdgcn_ballot_w64(keep);
-    if ((tid & 63) == 0) n_sh[turn][tid >> 6] = __builtin_popcountll(m);
-    __syncthreads();
-    int at = held + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0u));
-    for (int w = 0; w < W; ++w) {
-      if (w < (tid >> 6)) at += n_sh[turn][w];
-      held += n_sh[turn][w];
-    }
-    turn ^= 1;
-    if (keep && at < a.S) {
-      pos[at] = t;
-      prio[at] = static_priority(r[t], (float)t, lg);
-    }
+  // A wave's own positions are 4 runs of 64 after each other.
+  uint64_t m[kPromptEach];
+  int own = 0;
+#pragma unroll
+  for (int i = 0; i < kPromptEach; ++i) {
+    const int t = begin + (wave * kPromptEach + i) * 64 + lane;
+    m[i] = __builtin_amdgcn_ballot_w64(t < n && evict[min(t, a.T - 1)] >= n);
+    own += __builtin_popcountll(m[i]);
   }
+  int before = 0;
+#pragma unroll 8
+  for (int t = tid; t < begin; t += kPromptThreads) before += evict[t] >= n;
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) before += __shfl_xor(before, o);
+  if (lane == 0) n_sh[wave] = before, own_sh[wave] = own;
+  __syncthreads();
+  int at = 0, held = 0;
+#pragma unroll
+  for (int w = 0; w < W; ++w) {
+    at += n_sh[w] + (w < wave ? own_sh[w] : 0);
+    held += n_sh[w] + own_sh[w];
+  }
+#pragma unroll
+  for (int i = 0; i < kPromptEach; ++i) {
+    const int t = begin + (wave * kPromptEach + i) * 64 + lane;
+    const int slot = at + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(m[i] >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m[i], 0u));
+    if ((m[i] >> lane & 1) && slot < a.S) {
+      pos[slot] = t;
+      prio[slot] = static_priority(r[t], (float)t, lg);
+    }
+    at += __builtin_popcountll(m[i]);
+  }
+  if (!last) return;
   held = min(held, a.S);
   for (int i = held + tid; i < a.S; i += kPromptThreads) {
     pos[i] = -1;
@@ -401,8 +544,9 @@ __global__ __launch_bounds__(kPromptThreads) void retain_prompt_kernel(RetainLau
 int64_t cache_append_blocks(const AppendLaunch& L) {
   const AppendShape s = append_shape(L);
   const int64_t kv = 2LL * L.c.B * L.c.H * append_pages(L);
-  const int64_t q_rows = L.q.ptr ? (int64_t)L.c.B * L.Hq * L.N : 0, per = s.threads / (L.c.D / 8);
-  return kv + (q_rows + per - 1) / per;
+  const int64_t items = L.q.ptr ? (int64_t)L.c.B * L.N * ((L.Hq + kQHeads - 1) / kQHeads) : 0;
+  const int64_t per = s.threads / (L.c.D / 16);
+  return kv + (items + per - 1) / per;
 }
 
 int launch_cache_append(const AppendLaunch& L) {
@@ -413,8 +557,9 @@ int launch_cache_append(const AppendLaunch& L) {
 }
 
 int launch_retain_prompt(const RetainLaunch& L) {
-  hipLaunchKernelGGL(retain_prompt_kernel, dim3((unsigned)(L.B * L.H)), dim3(kPromptThreads), 0, (hipStream_t)L.stream,
-                     L);
+  const int parts = (L.T + kPromptPart - 1) / kPromptPart;
+  hipLaunchKernelGGL(retain_prompt_kernel, dim3((unsigned)(L.B * L.H * parts)), dim3(kPromptThreads), 0,
+                     (hipStream_t)L.stream, L, parts);
   return (int)hipGetLastError();
 }
 

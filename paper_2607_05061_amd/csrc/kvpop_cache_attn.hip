@@ -12,7 +12,6 @@
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
-#include <stdlib.h>
 
 #include "kvpop_cache.h"
 #include "kvpop_internal.h"
@@ -387,7 +386,7 @@ __device__ __forceinline__ float max_pair(float x) {
 constexpr int chunk_tile(int D) { return 8192 / D; }  // keys: 16 KB a widened side
 
 template <int D, int FMT>
-__global__ __launch_bounds__(kChunkThreads, 2) void cache_attn_chunk_kernel(CacheAttnLaunch a, int row_blocks,
+__global__ __attribute__((amdgpu_flat_work_group_size(kChunkThreads, kChunkThreads), amdgpu_waves_per_eu(2, 2))) void cache_attn_chunk_kernel(CacheAttnLaunch a, int row_blocks,
                                                                             int splits) {
   constexpr int KS = D / 16, DB = D / 32;                        // k-steps, blocks of 32 dims
   constexpr int TILE = chunk_tile(D), NB = TILE / 32, NE = TILE / 16;  // blocks of 32 keys; of 16, with exponents
@@ -760,13 +759,12 @@ Plan plan(const CacheAttnLaunch& L) {
   Plan p;
   const int64_t lists = (int64_t)L.c.B * L.c.H, R = (int64_t)(L.Hq / L.c.H) * L.N;
   const int64_t room = (int64_t)L.c.max_pages * L.c.P;
-  p.chunk = R >= (getenv("KC") ? atoi(getenv("KC")) : kChunkLeast);
+  p.chunk = R >= (kChunkLeast);
   p.waves = kChunkWaves;
   if (p.chunk) {
     p.row_blocks = (int)((R + kChunkRows - 1) / kChunkRows);
     const int64_t blocks = lists * p.row_blocks, tiles = (room + chunk_tile(L.c.D) - 1) / chunk_tile(L.c.D);
     int64_t s = blocks < kCus ? kCus / blocks : 1;
-    if (getenv("KS")) s = atoi(getenv("KS"));
     s = s < tiles / 4 ? s : tiles / 4;
     p.splits = (int)(s < 1 ? 1 : s > kMaxSplits ? kMaxSplits : s);
     return p;
