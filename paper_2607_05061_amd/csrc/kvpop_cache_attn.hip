@@ -795,11 +795,11 @@ int launch_attn(const CacheAttnLaunch& L) {
   else
     hipLaunchKernelGGL((cache_attn_kernel<D, FMT, 4>), grid, block, 0, st, L, p.row_blocks, p.splits);
   if (const hipError_t e = hipGetLastError(); e != hipSuccess || p.splits == 1) return (int)e;
-  // Many parts are read by 8 groups of threads each, a few by one.
+  // Several parts are read by 8 groups of threads each row, two or three by one.
   const int64_t rows = (int64_t)L.c.B * L.Hq * L.N;
   const int tile = p.chunk ? chunk_tile(D) : kTile, least = p.chunk ? 1 : kMinTiles * p.waves;
   constexpr int kMost = 2048 / D;  // rows a workgroup with one group a row
-  if (p.splits > 8)
+  if (p.splits >= 4)
     hipLaunchKernelGGL((cache_attn_join_kernel<D, 8>), dim3((unsigned)((8 * rows + kMost - 1) / kMost)), dim3(256), 0, st,
                        L, p.splits, tile, least);
   else
