@@ -338,8 +338,14 @@ __device__ __forceinline__ void write_page(const AppendLaunch& a, const PageJob&
 }
 
 // One workgroup per (list, page that may get tokens, side): the rows of a page stay in
-// registers between the maximum, which needs all of them, and the codes. Keys that turn are held in
+// registers between the maximum, which needs all of them, and the codes; nothing is shared between
+// workgroups, so nothing depends on their order. Keys that turn are held in
 // 64 bits, others in 32, where bf16 is exact. The workgroups after those turn the queries.
+// HBM bounds large calls: 3 ragged chunks of 20001 tokens (28 query heads, 4 lists each, 1.05 GB)
+// 221 us, 4.7 TB/s; 8 x 4 lists of 8192 with as many query heads 79-93 us (0.31 GB). Small
+// ones are the latency of one page's loads: 5 us for one token of 8 lists, 6 us for one of 1024.
+// With the angles read per element and head instead: 455 us for the chunks, 52 instead of 15 us
+// for 16 lists that gather 2276 of 32768 tokens.
 template <int D, int FMT, int ITER>
 __global__ __launch_bounds__(512) void cache_append_kernel(AppendLaunch a, int pages, int64_t kv_blocks) {
   __shared__ int need_sh[8];
@@ -425,7 +431,8 @@ constexpr int kStepThreads = 256;
 
 // One workgroup per list: every slot's position and priority is read once, the token
 // that leaves the window gets its priority on the way, and the least eligible one is
-// the largest of (key, position) pairs, then the first slot that holds it.
+// the largest of (key, position) pairs, then the first slot that holds it. The time is that of
+// reading 8 bytes a slot: 2048 lists of 2276 slots (37 MB) 10 us, 8 lists 5.5 us (latency).
 __global__ __launch_bounds__(kStepThreads) void retain_step_kernel(RetainLaunch a) {
   __shared__ unsigned long long best_sh[kStepThreads / 64];
   __shared__ int slot_sh[kStepThreads / 64];
@@ -483,7 +490,8 @@ constexpr int kPromptThreads = 1024, kPromptEach = 4, kPromptPart = kPromptThrea
 
 // A stable compaction: one workgroup per list and 4096 positions. It counts the kept tokens
 // before its part (a list's lifetimes are read from L2 by its later workgroups: at most T / 4096
-// times) and writes its own; the last one also clears the slots that are left.
+// times) and writes its own; the last one also clears the slots that are left. 32 lists of 32768
+// positions 9 us, 8 of 131072 13 us (one workgroup per list: 23 and 83 us).
 __global__ __launch_bounds__(kPromptThreads) void retain_prompt_kernel(RetainLaunch a, int parts) {
   constexpr int W = kPromptThreads / 64;
   __shared__ int n_sh[W], own_sh[W];

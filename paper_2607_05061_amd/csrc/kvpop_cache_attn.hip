@@ -106,13 +106,17 @@ __device__ __forceinline__ int split_tiles(int n, int splits, int least) {
 }
 
 // One workgroup: 16 rows (query tokens times the G heads of a KV head, tokens slowest)
-// against a run of a list's tiles, which its four waves divide. S^T = K Q^T puts keys on
+// against a run of a list's tiles, which its waves divide. S^T = K Q^T puts keys on
 // the accumulator's rows and queries on its columns, so a lane holds 4 keys of each 16 for
 // the query lane % 16; with two such blocks the lane's 8 probabilities are the B operand of
 // O^T += V^T P^T as they stand, its contraction index running over the keys
 // {4 g .. 4 g + 3, 16 + 4 g ..} of lane group g. A lane loads the D / 16 bytes at D / 16 (lane %
 // 16) of each of these keys, so that byte t of its 8 loads is its A operand of the
 // product for the head dims t, t + D / 16, ...: no value passes through LDS.
+// HBM bounds it: 8 KB of a tile are on their way while one is multiplied. 32 x 8 lists of 16384
+// tokens of 128 dims (1.07 GB) take 185-195 us, 5.5-5.8 TB/s (part of the pool stays in
+// the 256 MB cache), 128 x 8 of 2276 115 us, 5.2 TB/s. Two tiles on their way (172 registers instead
+// of 142): 113 us, but 9.1 instead of 7.6 us for 64 x 8 lists of 100.
 template <int D, int FMT, int W>
 __global__ __launch_bounds__(64 * W) void cache_attn_kernel(CacheAttnLaunch a, int row_blocks, int splits) {
   constexpr int KS = D / 32;  // k-steps of the logits
@@ -139,7 +143,8 @@ __global__ __launch_bounds__(64 * W) void cache_attn_kernel(CacheAttnLaunch a, i
 
   const int end_wg = min(tiles, (split + 1) * per);
   const int share = (end_wg - split * per + W - 1) / W;
-  const int t0 = split * per + wave * share, t1 = min(end_wg, t0 + share);
+  // Nothing to read where no row of the workgroup has a query.
+  const int t0 = split * per + wave * share, t1 = rb * kRows / G < nq ? min(end_wg, t0 + share) : t0;
 
   struct Tile {
     Words<4> k[2][KW / 4];
@@ -368,6 +373,12 @@ __global__ __launch_bounds__(64 * W) void cache_attn_kernel(CacheAttnLaunch a, i
 //                  neighbouring threads write neighbouring places.
 // Three tile buffers: while one is multiplied, with the next one's first logits, the one after
 // is widened, and the bytes of the following one are on their way in registers.
+//
+// 1024 queries of 32 heads over 8 lists of 32768 tokens: 0.56-0.59 ms, 920-970 TFLOP/s (37-39%
+// of the dense peak), D = 64 0.37 ms. Matrix cores are busy on 44% of the cycles, the vector ALU
+// (exponential, its argument and sum per pair, the widening) on 57%, LDS on 32%. With the
+// numerators of 64 keys after all their logits, and two buffers: 0.70 ms; with the masks of the last
+// tiles as selects in every block, 0.63 ms; with a raised priority around the products, the same.
 constexpr int kChunkWaves = 8, kChunkThreads = 64 * kChunkWaves, kChunkRows = 32 * kChunkWaves;
 constexpr float kSlack = 8.f;  // how far x may pass the reference before the sums are rescaled, in powers of two
 
@@ -742,26 +753,36 @@ __global__ __launch_bounds__(256) void cache_attn_join_kernel(CacheAttnLaunch a,
   if (d0 == 0) a.lse[out] = z > 0.f || z != z ? (m + __builtin_amdgcn_logf(z)) * kLn2 : neg_inf();
 }
 
-// Which kernel, and how many workgroups share a list.
+// Which kernel, and how many workgroups share a list (us on one MI355X, D = 128, int8, 64
+// tokens a page, G = 4 unless said).
 //
-// Chunks (at least kChunkLeast rows a list): one workgroup of 8 waves per CU fills it.
+// The chunk kernel costs a wave's worth of matrix products per 32 rows but widens a tile once per
+// 256; the other one reads a list once per 16 rows. Lists of 4096 tokens, (lists, rows), chunk
+// and other: (8, 80) 19.8 and 17.1, (16, 80) 24.1 and 23.5; (32, 48) 24.8 and 25.8, (32, 32)
+// 23.1 and 20.8; (64, 48) 36.6 and 36.6, (128, 48) 57.5 and 69.3, (128, 32) 55.6 and 43.9; of
+// 8192, (8, 96) 26.0 and 28.1. It gets one workgroup per CU, parts of at least 4 tiles.
 //
-// Fewer rows: a list's bytes are the time, so the waves are spread over lists and their parts until
-// every CU has a workgroup of 8 (one list part each), or lists are so many that workgroups of
-// 4 fill the CUs by themselves. Parts cost a second launch.
+// The other kernel's time is the lists' bytes. With at most one workgroup per CU it takes 8 waves
+// (lists of 2276 tokens: 256 of them 27.7, 4 waves 32.0; 136 22.6 and 29.8); beyond, as
+// many workgroups of 4 waves as fit: at D = 128 a second one of 8 waves does not fit a CU's registers
+// (320 lists 40.5, 8 waves 45.7), at D = 64 it does (384 28.5, 8 waves 25.4; 640 35.7 and
+// 38.1). Fewer lists than CUs are split until each CU has a part, which costs a
+// second launch: not for lists of up to 512 tokens (8 of 384: 8.6, split 9.7-10.1; 512 9.7 and 9.7;
+// 640 10.8 and 9.8). Parts of less than 2 tiles a wave go to workgroups of 4 waves with at least
+// one each (8 lists of 2276: 18 parts 10.2, 9 of 8 waves 10.7; 32 of 4096, 8 parts: 8
+// waves 14.4, 4 waves 15.3).
 struct Plan {
   bool chunk;
   int row_blocks, waves, splits;
 };
 constexpr int kCus = 256;
-constexpr int kChunkLeast = 81;
 Plan plan(const CacheAttnLaunch& L) {
   Plan p;
   const int64_t lists = (int64_t)L.c.B * L.c.H, R = (int64_t)(L.Hq / L.c.H) * L.N;
   const int64_t room = (int64_t)L.c.max_pages * L.c.P;
-  p.chunk = R >= (kChunkLeast);
-  p.waves = kChunkWaves;
+  p.chunk = R > 80 || (R > 32 && lists >= 32);
   if (p.chunk) {
+    p.waves = kChunkWaves;
     p.row_blocks = (int)((R + kChunkRows - 1) / kChunkRows);
     const int64_t blocks = lists * p.row_blocks, tiles = (room + chunk_tile(L.c.D) - 1) / chunk_tile(L.c.D);
     int64_t s = blocks < kCus ? kCus / blocks : 1;
@@ -773,7 +794,7 @@ Plan plan(const CacheAttnLaunch& L) {
   const int64_t blocks = lists * p.row_blocks, tiles = (room + kTile - 1) / kTile;
   p.splits = 1;
   p.waves = 4;
-  if (tiles <= 16 || blocks >= kCus + kCus / 2) return p;
+  if (tiles <= 16 || blocks > (L.c.D == 64 ? 2 : 1) * kCus) return p;
   int64_t s = blocks < kCus ? kCus / blocks : 1;
   if (tiles >= 16 * s)
     p.waves = 8;

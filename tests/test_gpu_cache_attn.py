@@ -60,7 +60,7 @@ def test_long_list_in_many_parts():
     _run(rng, 1, 2, 1, 200, 64, 64, "int8", [[20000]])
 
 
-@pytest.mark.parametrize("N", [1, 40])
+@pytest.mark.parametrize("N", [1, 40, 120])
 def test_scales_of_every_size(N):
     """Exponents over their whole range: a few pages hold all the mass, or values of any size."""
     rng = np.random.default_rng(3)
@@ -74,7 +74,7 @@ def test_scales_of_every_size(N):
         attention_check(q64, host, held, 0.125, o, lse)
 
 
-@pytest.mark.parametrize("N", [1, 40])
+@pytest.mark.parametrize("N", [1, 40, 120])
 def test_sharp_and_flat_logits_and_queries_of_any_size(N):
     rng = np.random.default_rng(4)
     _run(rng, 1, 4, 2, N, 128, 64, "int8", [[900, 333]], scale=0.5)      # one key takes nearly all
@@ -83,7 +83,7 @@ def test_sharp_and_flat_logits_and_queries_of_any_size(N):
     _run(rng, 1, 4, 2, N, 64, 64, "e4m3", [[500, 64]], scale=1e3, q_gain=1e-9)
 
 
-@pytest.mark.parametrize("N", [1, 6, 40])
+@pytest.mark.parametrize("N", [1, 6, 40, 120])
 def test_growing_logits_move_the_maximum(N):
     """Each key's logit is above all before it: the running maximum moves in every step."""
     D, P, L = 64, 16, 640
@@ -101,7 +101,7 @@ def test_growing_logits_move_the_maximum(N):
         attention_check(q64, host, [[L]], float(np.float32(scale)), o, lse)
 
 
-@pytest.mark.parametrize("N", [1, 40])
+@pytest.mark.parametrize("N", [1, 40, 120])
 def test_bytes_that_are_not_seen_do_not_matter(N):
     """Slots past a list's end hold NaN codes; entries without a page are left out; spare pages too."""
     rng = np.random.default_rng(6)
@@ -134,7 +134,7 @@ def test_lists_share_pages():
     attention_check(q64, host, held, float(np.float32(0.01)), o, lse)
 
 
-@pytest.mark.parametrize("N", [1, 50])
+@pytest.mark.parametrize("N", [1, 50, 120])
 def test_a_query_that_is_not_finite_stays_by_itself(N):
     rng = np.random.default_rng(8)
     host = HostCache(rng, 1, 2, 10, 16, 64, "int8")
@@ -172,3 +172,17 @@ def test_results_do_not_depend_on_the_run(N):
     for _ in range(3):
         b = kv.kvpop_cache_attn(q, cache, held, 0.01)
         assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+@pytest.mark.parametrize("fmt,D", [("int8", 128), ("e4m3", 64)])
+@pytest.mark.parametrize("B,H,G,N", [(1, 8, 4, 20), (1, 8, 4, 21), (4, 8, 4, 8), (4, 8, 4, 9), (1, 31, 3, 11), (1, 32, 3, 11)])
+def test_both_sides_of_the_line_between_the_kernels(fmt, D, B, H, G, N):
+    rng = np.random.default_rng(B * H * G * N)
+    _run(rng, B, H * G, H, N, D, 32, fmt, rng.integers(0, 700, (B, H)))
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("B,H", [(32, 8), (33, 8), (64, 8), (65, 8), (1, 255)])
+def test_as_many_lists_as_workgroups_fit(B, H, D):
+    rng = np.random.default_rng(B * H + D)
+    _run(rng, B, H, H, 1, D, 64, "int8", rng.integers(0, 600, (B, H)), room=600)
