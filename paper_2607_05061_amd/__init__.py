@@ -524,9 +524,8 @@ def _ptr(x, name: str, dtype, shape, dev: int) -> int:
     raise ValueError("%s must be %s" % (name, list(shape)))
 
 
-def _cache_parts(cache):
+def _cache_parts(torch, cache):
     """A cache checked: (packed kvpop_cache, B, H, D, GPU index)."""
-    torch = _torch()
     k, v, ke, ve, table = cache
     i8 = torch.int8
     dtype = getattr(k, "dtype", None)
@@ -547,10 +546,9 @@ def _cache_parts(cache):
     return packed, B, H, D, dev
 
 
-def _rows(x, name: str, B: int, heads, N, D: int, dev: int):
+def _rows(torch, x, name: str, B: int, heads, N, D: int, dev: int):
     """A bf16 tensor [B, heads, N, D] (heads, N None: any), strided but for its last dimension:
     (address, strides of its first three), its heads and its tokens."""
-    torch = _torch()
     if not isinstance(x, torch.Tensor):
         raise TypeError("%s must be a torch.Tensor" % name)
     if x.get_device() != dev:
@@ -568,11 +566,9 @@ def _rows(x, name: str, B: int, heads, N, D: int, dev: int):
     return (x.data_ptr(), sb if B > 1 else 0, sh if h > 1 else 0, st if n > 1 else 0), h, n
 
 
-def _call(name: str, dev: int, stream, *args):
-    """Calls an entry point on ``stream`` or the current one of GPU ``dev``, which is made the current
+def _call(torch, f, dev: int, stream, *args):
+    """Calls entry point ``f`` on ``stream`` or the current one of GPU ``dev``, which is made the current
     device: the default stream's handle is that of whichever device is current."""
-    torch = _torch()
-    f = getattr(lib(), name)
     handle = torch._C._cuda_getCurrentRawStream(dev) if stream is None else int(stream.cuda_stream)
     if dev == torch._C._cuda_getDevice():
         st = f(*args, handle)
@@ -580,7 +576,7 @@ def _call(name: str, dev: int, stream, *args):
         with torch.cuda.device(dev):
             st = f(*args, handle)
     if st != KVPOP_OK:
-        raise KvpopError(st, name)
+        raise KvpopError(st, f.__name__)
 
 
 def kvpop_cache_append(cache: KvpopCache, k, v, held, count=None, start=None, src=None, q=None, rotary=None,
@@ -595,9 +591,9 @@ def kvpop_cache_append(cache: KvpopCache, k, v, held, count=None, start=None, sr
     bf16 [B, Hq, N, D] contiguous; else None. include/kvpop_cache.h has the exponents' rule."""
     torch = _torch()
     i32, bf16 = torch.int32, torch.bfloat16
-    c, B, H, D, dev = _cache_parts(cache)
-    kr, _, N = _rows(k, "k", B, H, None, D, dev)
-    vr, _, _ = _rows(v, "v", B, H, N, D, dev)
+    c, B, H, D, dev = _cache_parts(torch, cache)
+    kr, _, N = _rows(torch, k, "k", B, H, None, D, dev)
+    vr, _, _ = _rows(torch, v, "v", B, H, N, D, dev)
     M = N
     if src is not None:
         M = src.shape[-1] if src.dim() == 3 else 0
@@ -611,7 +607,7 @@ def kvpop_cache_append(cache: KvpopCache, k, v, held, count=None, start=None, sr
         sin = _ptr(t_sin, "sin", torch.float32, (n_positions, rot), dev)
     qr, Hq, qo = (0, 0, 0, 0), 0, 0
     if q is not None:
-        qr, Hq, _ = _rows(q, "q", B, None, N, D, dev)
+        qr, Hq, _ = _rows(torch, q, "q", B, None, N, D, dev)
         if q_out is None:
             q_out = torch.empty((B, Hq, N, D), dtype=bf16, device=q.device)
         qo = _ptr(q_out, "q_out", bf16, (B, Hq, N, D), dev)
@@ -621,13 +617,13 @@ def kvpop_cache_append(cache: KvpopCache, k, v, held, count=None, start=None, sr
                           _ptr(start, "start", i32, lists, dev), _ptr(src, "src", i32, (B, H, M), dev),
                           _ptr(pos0, "pos0", i32, (B,), dev), cos, sin, n_positions, 2 * rot, 1 if adjacent else 0, Hq,
                           *qr, qo)
-    _call("kvpop_cache_append", dev, stream, c, a)
+    _call(torch, lib().kvpop_cache_append, dev, stream, c, a)
     return q_out
 
 
 def kvpop_cache_attn_workspace_size(cache: KvpopCache, n_q_heads: int, n_tokens: int) -> int:
     """Bytes of workspace of a kvpop_cache_attn call with q [B, n_q_heads, n_tokens, D]."""
-    return int(lib().kvpop_cache_attn_workspace_size(_cache_parts(cache)[0], n_q_heads, n_tokens))
+    return int(lib().kvpop_cache_attn_workspace_size(_cache_parts(_torch(), cache)[0], n_q_heads, n_tokens))
 
 
 def kvpop_cache_attn(q, cache: KvpopCache, held, scale: float, q_lens=None, o=None, lse=None, workspace=None,
@@ -638,8 +634,8 @@ def kvpop_cache_attn(q, cache: KvpopCache, held, scale: float, q_lens=None, o=No
     nothing, get 0 and -inf."""
     torch = _torch()
     i32 = torch.int32
-    c, B, H, D, dev = _cache_parts(cache)
-    qr, Hq, N = _rows(q, "q", B, None, None, D, dev)
+    c, B, H, D, dev = _cache_parts(torch, cache)
+    qr, Hq, N = _rows(torch, q, "q", B, None, None, D, dev)
     if o is None:
         o = torch.empty((B, Hq, N, D), dtype=torch.bfloat16, device=q.device)
     if lse is None:
@@ -654,7 +650,7 @@ def kvpop_cache_attn(q, cache: KvpopCache, held, scale: float, q_lens=None, o=No
                     workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
     elif workspace.numel() * workspace.element_size() < need or workspace.device != q.device:
         raise ValueError("workspace must hold %d bytes on the device of the cache" % need)
-    _call("kvpop_cache_attn", dev, stream, c, Hq, N, float(scale), _ROWS_PACK.pack(*qr),
+    _call(torch, lib().kvpop_cache_attn, dev, stream, c, Hq, N, float(scale), _ROWS_PACK.pack(*qr),
           _ptr(held, "held", i32, (B, H), dev), _ptr(q_lens, "q_lens", i32, (B,), dev),
           _ptr(o, "o", torch.bfloat16, (B, Hq, N, D), dev), _ptr(lse, "lse", torch.float32, (B, Hq, N), dev),
           workspace.data_ptr() if workspace is not None else 0, need)
@@ -682,7 +678,7 @@ def kvpop_retain_prompt(evict, scores, budget: int, log_gamma=None, lens=None, p
         held = torch.empty((B, H), dtype=i32, device=device)
     st = _RETAIN_PACK.pack(B, H, S, _ptr(pos, "pos", i32, (B, H, S), dev), _ptr(prio, "prio", f32, (B, H, S), dev),
                            _ptr(held, "held", i32, (B, H), dev))
-    _call("kvpop_retain_prompt", dev, stream, st, T, _ptr(evict, "evict", i32, (B, H, T), dev), scores.data_ptr(),
+    _call(torch, lib().kvpop_retain_prompt, dev, stream, st, T, _ptr(evict, "evict", i32, (B, H, T), dev), scores.data_ptr(),
           _ptr(log_gamma, "log_gamma", f32, (H,), dev), _ptr(lens, "lens", i32, (B,), dev))
     return pos, prio, held
 
@@ -704,7 +700,7 @@ def kvpop_retain_step(scores, q_pos, pos, prio, held, sinks: int, window: int, t
     if slot is None:
         slot = torch.empty(lists, dtype=i32, device=pos.device)
     st = _RETAIN_PACK.pack(B, H, S, pos.data_ptr(), _ptr(prio, "prio", f32, shape, dev), _ptr(held, "held", i32, lists, dev))
-    _call("kvpop_retain_step", dev, stream, st, _ptr(scores, "scores", f32, lists, dev),
+    _call(torch, lib().kvpop_retain_step, dev, stream, st, _ptr(scores, "scores", f32, lists, dev),
           _ptr(log_gamma, "log_gamma", f32, (H,), dev), _ptr(q_pos, "q_pos", i32, (B,), dev), int(sinks), int(window),
           int(topk), _ptr(slot, "slot", i32, lists, dev))
     return slot
