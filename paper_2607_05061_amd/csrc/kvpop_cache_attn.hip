@@ -547,55 +547,52 @@ __global__ __attribute__((amdgpu_flat_work_group_size(kChunkThreads, kChunkThrea
     for (int s = 0; s < KS; ++s) x = mfma32(*reinterpret_cast<const f16x8*>(kt + s * 1024), qf[s], x);
     return x;
   };
-  // x - M of a block of 32 keys from its bare products, -inf where a key is not seen; moves
-  // M where one passes it by more than kSlack.
-  auto settle = [&](f32x16& x, int e0, int e1, int key0) __attribute__((always_inline)) {
+  // Numerators 2^(x - M) of a block of 32 keys from its bare products, summed and in 16 bits. The
+  // usual block is all seen, and none of its numerators passes 2^15 or is NaN: their sums
+  // show it. Any other is done over with its keys that are not seen left out, and M moved
+  // where one passes it by more than kSlack.
+  auto numerators = [&](const f32x16& x, int e0, int e1, int key0, f16x8 (&p)[2]) __attribute__((always_inline)) {
     const float kc0 = __builtin_ldexpf(cq, (int16_t)e0), kc1 = __builtin_ldexpf(cq, (int16_t)e1);
     const float v0 = (float)(e0 >> 16), v1 = (float)(e1 >> 16), m0 = v0 - M, m1 = v1 - M;
+    const float w0 = __builtin_ldexpf(1.f, -(e0 >> 16)), w1 = __builtin_ldexpf(1.f, -(e1 >> 16));
+    float s0 = 0.f, s1 = 0.f;
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+      const float y0 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r], kc0, m0));
+      const float y1 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r + 8], kc1, m1));
+      s0 += y0, s1 += y1;
+      p[0][r] = (_Float16)y0, p[1][r] = (_Float16)y1;
+    }
     const bool whole = key0 + 32 <= sure && e0 != kNoPage && e1 != kNoPage;
-    auto hide = [&](f32x16& y) __attribute__((always_inline)) {
+    if (!whole || __builtin_amdgcn_ballot_w64(!(s0 <= 0x1p15f && s1 <= 0x1p15f)) != 0) {
       int key = key0 + 4 * hi;
       asm volatile("" : "+v"(key));  // the comparisons stay in this branch
+      f32x16 y;
+      float mx = neg_inf();
 #pragma unroll
-      for (int r = 0; r < 16; ++r)
+      for (int r = 0; r < 16; ++r) {
+        y[r] = __builtin_fmaf(x[r], r < 8 ? kc0 : kc1, r < 8 ? v0 : v1);
         if ((r < 8 ? e0 : e1) == kNoPage || key + 8 * (r >> 2) + (r & 3) >= seen) y[r] = neg_inf();
-    };
-    f32x16 y;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) y[r] = __builtin_fmaf(x[r], r < 8 ? kc0 : kc1, r < 8 ? m0 : m1);
-    if (!whole) hide(y);
-    float mx = y[0];
-#pragma unroll
-    for (int r = 1; r < 16; ++r) mx = fmaxf(mx, y[r]);
-    mx = max_pair(mx);
-    if (__builtin_amdgcn_ballot_w64(mx > kSlack) != 0) {
-#pragma unroll
-      for (int r = 0; r < 16; ++r) y[r] = __builtin_fmaf(x[r], r < 8 ? kc0 : kc1, r < 8 ? v0 : v1);
-      if (!whole) hide(y);
-      mx = y[0];
-#pragma unroll
-      for (int r = 1; r < 16; ++r) mx = fmaxf(mx, y[r]);
+        mx = fmaxf(mx, y[r]);
+      }
       mx = max_pair(mx);
       const float m = mx > M + kSlack ? mx : M, mu = m == neg_inf() ? 0.f : m;
-      const float f = __builtin_amdgcn_exp2f(M - mu);
+      if (__builtin_amdgcn_ballot_w64(m != M) != 0) {
+        const float f = __builtin_amdgcn_exp2f(M - mu);
 #pragma unroll
-      for (int d = 0; d < DB; ++d) o[d] *= f;
-      S *= f;
-      M = m;
+        for (int d = 0; d < DB; ++d) o[d] *= f;
+        S *= f;
+        M = m;
+      }
+      s0 = s1 = 0.f;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) y[r] -= mu;
+      for (int r = 0; r < 8; ++r) {
+        const float y0 = __builtin_amdgcn_exp2f(y[r] - mu), y1 = __builtin_amdgcn_exp2f(y[r + 8] - mu);
+        s0 += y0, s1 += y1;
+        p[0][r] = (_Float16)y0, p[1][r] = (_Float16)y1;
+      }
     }
-    x = y;
-  };
-  // Numerators of a settled block, summed and in 16 bits.
-  auto numerators = [&](const f32x16& x, int e0, int e1, f16x8 (&p)[2]) __attribute__((always_inline)) {
-    const float w0 = __builtin_ldexpf(1.f, -(e0 >> 16)), w1 = __builtin_ldexpf(1.f, -(e1 >> 16));
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const float y = __builtin_amdgcn_exp2f(x[r]);
-      S = __builtin_fmaf(y, r < 8 ? w0 : w1, S);
-      p[r / 8][r & 7] = (_Float16)y;
-    }
+    S = __builtin_fmaf(s0, w0, __builtin_fmaf(s1, w1, S));
   };
   auto weigh = [&](const f16x8 (&p)[2], int n, int buf) __attribute__((always_inline)) {
     const uint8_t* vt_ = sm[buf][1] + n * 2 * DB * 1024 + lane * 16;
@@ -627,19 +624,17 @@ __global__ __attribute__((amdgpu_flat_work_group_size(kChunkThreads, kChunkThrea
     int buf = 0;
     for (int t = t0; t < t1; ++t) {
       const int b1 = buf == 2 ? 0 : buf + 1, b2 = buf == 0 ? 2 : buf - 1;
-      // Matrix products stand beside vector work that does not wait for them: a block's logits
-      // beside the numerators of the one before, its product with V beside the settling of
-      // the next, the last ones beside the widening. Past the last tile, what is
+      // Matrix products stand beside vector work that does not wait for them: a block's product
+      // with V and the logits of the block after the next beside the next one's
+      // numerators, the last ones beside the widening. Past the last tile, what is
       // widened and multiplied is not used.
       if (TILE * t < any) {
-        settle(l, e[0], e[1], TILE * t);
 #pragma unroll
         for (int n = 0; n < NB; ++n) {
           f16x8 p[2];
-          f32x16 ln = n + 1 < NB ? logits(n + 1, buf) : logits(0, b1);
-          numerators(l, e[2 * n], e[2 * n + 1], p);
-          weigh(p, n, buf);  // before M may move
-          if (n + 1 < NB) settle(ln, e[2 * n + 2], e[2 * n + 3], TILE * t + 32 * (n + 1));
+          const f32x16 ln = n + 1 < NB ? logits(n + 1, buf) : logits(0, b1);
+          numerators(l, e[2 * n], e[2 * n + 1], TILE * t + 32 * n, p);
+          weigh(p, n, buf);
           l = ln;
         }
         widen(x, b2);
