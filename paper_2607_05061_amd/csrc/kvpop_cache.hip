@@ -237,14 +237,13 @@ __device__ __forceinline__ void turn_queries(const AppendLaunch& a, int64_t blk)
 // What one workgroup writes: rows lo - first .. hi - first - 1 of a page, from the list's
 // entries lo - start on.
 struct PageJob {
-  int list, b, h, page, n_rows, first_row, entry;
+  int list, b, h, nth, n_rows, first_row, entry;  // nth: the page's place in the list
   int before, after;  // rows other tokens use: the first ones, and those behind the written ones
-  int was;            // the exponent these have
 };
 
 template <int D, int FMT, int ITER, class F>
 __device__ __forceinline__ void write_page(const AppendLaunch& a, const PageJob& job, const Rows& x, int rot,
-                                           uint8_t* codes, int8_t* exps, int* need_sh) {
+                                           uint8_t* pool, int8_t* exps, int* need_sh) {
   constexpr int C = D / 16;
   const int tid = threadIdx.x, r0 = tid / C, rows = blockDim.x / C;
   const Pieces pc = pieces(tid % C, rot, a.adjacent);
@@ -266,6 +265,11 @@ __device__ __forceinline__ void write_page(const AppendLaunch& a, const PageJob&
       }
     }
   }
+  // The page is looked up while the rows are on their way.
+  const int page = a.c.table[(int64_t)job.list * a.c.max_pages + job.nth];
+  if ((unsigned)page >= (unsigned)a.c.n_pages) return;
+  uint8_t* codes = pool + (int64_t)page * a.c.P * D;
+  const int was = job.before > 0 || job.after > 0 ? clampi(exps[page], kExpMin, kExpMax) : kExpMin;
   F y[ITER][2][8], big = 0;
   float odd = 0.f;  // NaN if a value may be NaN or infinite
 #pragma unroll
@@ -293,7 +297,7 @@ __device__ __forceinline__ void write_page(const AppendLaunch& a, const PageJob&
   if ((tid & 63) == 0) need_sh[tid >> 6] = need;
   __syncthreads();
   for (int i = 0; i < (int)(blockDim.x >> 6); ++i) need = max(need, need_sh[i]);
-  const int e = max(need, job.was);
+  const int e = max(need, was);
 #pragma unroll
   for (int it = 0; it < ITER; ++it)
 #pragma unroll
@@ -321,17 +325,17 @@ __device__ __forceinline__ void write_page(const AppendLaunch& a, const PageJob&
       *reinterpret_cast<u32x2*>(at + pc.b) = hi;
     }
   }
-  if (tid == 0) exps[job.page] = (int8_t)e;
+  if (tid == 0) exps[page] = (int8_t)e;
   const int n_before = max(job.before, 0), n_old = n_before + max(job.after, 0);
-  if (n_old > 0 && e > job.was) {
+  if (n_old > 0 && e > was) {
     for (int i = r0; i < n_old; i += rows) {
       const int r = i < n_before ? i : job.first_row + job.n_rows + (i - n_before);
       u32x4* at = reinterpret_cast<u32x4*>(codes + r * D + 16 * (tid % C));
       u32x4 v = *at;
-      v.x = moved4<FMT>(v.x, job.was - e);
-      v.y = moved4<FMT>(v.y, job.was - e);
-      v.z = moved4<FMT>(v.z, job.was - e);
-      v.w = moved4<FMT>(v.w, job.was - e);
+      v.x = moved4<FMT>(v.x, was - e);
+      v.y = moved4<FMT>(v.y, was - e);
+      v.z = moved4<FMT>(v.z, was - e);
+      v.w = moved4<FMT>(v.w, was - e);
       *at = v;
     }
   }
@@ -366,17 +370,13 @@ __global__ __launch_bounds__(512) void cache_append_kernel(AppendLaunch a, int p
   if (nth >= a.c.max_pages) return;
   const int64_t first = nth * P, lo = max(start, first), hi = min(start + cnt, first + P);
   if (lo >= hi) return;
-  job.page = a.c.table[(int64_t)job.list * a.c.max_pages + nth];
-  if ((unsigned)job.page >= (unsigned)a.c.n_pages) return;
   job.n_rows = (int)(hi - lo), job.first_row = (int)(lo - first), job.entry = (int)(lo - start);
   job.before = (int)(min(lo, held) - first), job.after = (int)(min(held, first + P) - hi);
-  uint8_t* codes = (side ? a.c.v : a.c.k) + (int64_t)job.page * P * D;
-  int8_t* exps = side ? a.c.ve : a.c.ke;
-  job.was = job.before > 0 || job.after > 0 ? clampi(exps[job.page], kExpMin, kExpMax) : kExpMin;
+  job.nth = (int)nth;
   if (side == 0 && a.rot)
-    write_page<D, FMT, ITER, double>(a, job, a.k, a.rot, codes, exps, need_sh);
+    write_page<D, FMT, ITER, double>(a, job, a.k, a.rot, a.c.k, a.c.ke, need_sh);
   else
-    write_page<D, FMT, ITER, float>(a, job, side ? a.v : a.k, 0, codes, exps, need_sh);
+    write_page<D, FMT, ITER, float>(a, job, side ? a.v : a.k, 0, side ? a.c.v : a.c.k, side ? a.c.ve : a.c.ke, need_sh);
 }
 
 // Pages of a list that M consecutive slots can touch.

@@ -24,6 +24,7 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
@@ -33,6 +34,7 @@ constexpr int kRows = 16;        // (token, head) rows per workgroup
 constexpr int kTile = 32;        // keys per step of a wave
 constexpr int kMinTiles = 1;     // least tiles per wave of a split list
 constexpr int kMaxSplits = 64;
+constexpr int kFewParts = 4;     // fewer parts are joined by one group of threads a row
 
 __device__ __forceinline__ int clampi(int x, int lo, int hi) { return min(max(x, lo), hi); }
 __device__ __forceinline__ float neg_inf() { return -__builtin_inff(); }
@@ -703,23 +705,39 @@ __global__ __launch_bounds__(256) void cache_attn_join_kernel(CacheAttnLaunch a,
   const int64_t row = (int64_t)blockIdx.x * ROWS + rr;
   const bool there = row < (int64_t)a.c.B * a.c.H * R;
   const int list = there ? (int)(row / R) : 0, r = (int)(row % R);
+  // Every part's sums are asked for before it is known which of them the list has: the time is
+  // the latency of these loads. Parts that are not there are left out below.
+  constexpr int K = J > 1 ? kMaxSplits / J : kFewParts - 1;
+  const float* ms = a.workspace + (int64_t)a.c.B * a.c.H * R * splits * D + 2 * row * splits;
+  const float* po = a.workspace + row * splits * D + d0;
+  f32x2 mz[K];
+  f32x8 part[K];
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    const int s = j + J * k;
+    if (there && s < splits) {
+      mz[k] = *reinterpret_cast<const f32x2*>(ms + 2 * s);
+      part[k] = *reinterpret_cast<const f32x8*>(po + (int64_t)s * D);
+    }
+  }
   const int L = clampi(a.held[list], 0, a.c.max_pages * a.c.P);
   const int tiles = (L + tile - 1) / tile, per = split_tiles(tiles, splits, least), active = (tiles + per - 1) / per;
   const bool work = there && active > 1;  // else the workgroup of the only part wrote the row
-  const float* ms = a.workspace + (int64_t)a.c.B * a.c.H * R * splits * D + 2 * row * splits;
-  const float* po = a.workspace + row * splits * D + d0;
   float m = neg_inf(), z = 0.f;
   f32x8 y = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
   if (work) {
-    for (int s = j; s < active; s += J) m = fmaxf(m, ms[2 * s]);
-    const float mu = m == neg_inf() ? 0.f : m;
-    for (int s = j; s < active; s += J) {
-      const float f = __builtin_amdgcn_exp2f(ms[2 * s] - mu);
-      z = __builtin_fmaf(f, ms[2 * s + 1], z);
-      const f32x8 p = *reinterpret_cast<const f32x8*>(po + (int64_t)s * D);
 #pragma unroll
-      for (int t = 0; t < 8; ++t) y[t] = __builtin_fmaf(f, p[t], y[t]);
-    }
+    for (int k = 0; k < K; ++k)
+      if (j + J * k < active) m = fmaxf(m, mz[k][0]);
+    const float mu = m == neg_inf() ? 0.f : m;
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+      if (j + J * k < active) {
+        const float f = __builtin_amdgcn_exp2f(mz[k][0] - mu);
+        z = __builtin_fmaf(f, mz[k][1], z);
+#pragma unroll
+        for (int t = 0; t < 8; ++t) y[t] = __builtin_fmaf(f, part[k][t], y[t]);
+      }
   }
   if constexpr (J > 1) {
     *reinterpret_cast<f32x8*>(&y_sh[rr][j][d0]) = y;
@@ -815,7 +833,7 @@ int launch_attn(const CacheAttnLaunch& L) {
   const int64_t rows = (int64_t)L.c.B * L.Hq * L.N;
   const int tile = p.chunk ? chunk_tile(D) : kTile, least = p.chunk ? 1 : kMinTiles * p.waves;
   constexpr int kMost = 2048 / D;  // rows a workgroup with one group a row
-  if (p.splits >= 4)
+  if (p.splits >= kFewParts)
     hipLaunchKernelGGL((cache_attn_join_kernel<D, 8>), dim3((unsigned)((8 * rows + kMost - 1) / kMost)), dim3(256), 0, st,
                        L, p.splits, tile, least);
   else
