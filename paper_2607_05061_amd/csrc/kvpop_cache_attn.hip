@@ -376,11 +376,12 @@ __global__ __launch_bounds__(64 * W) void cache_attn_kernel(CacheAttnLaunch a, i
 // Three tile buffers: while one is multiplied, with the next one's first logits, the one after
 // is widened, and the bytes of the following one are on their way in registers.
 //
-// 1024 queries of 32 heads over 8 lists of 32768 tokens: 0.56-0.59 ms, 920-970 TFLOP/s (37-39%
-// of the dense peak), D = 64 0.37 ms. Matrix cores are busy on 44% of the cycles, the vector ALU
+// 1024 queries of 32 heads over 8 lists of 32768 tokens: 0.55-0.60 ms, 900-980 TFLOP/s (36-39%
+// of the dense peak), D = 64 0.36 ms. Matrix cores are busy on 44% of the cycles, the vector ALU
 // (exponential, its argument and sum per pair, the widening) on 57%, LDS on 32%. With the
 // numerators of 64 keys after all their logits, and two buffers: 0.70 ms; with the masks of the last
-// tiles as selects in every block, 0.63 ms; with a raised priority around the products, the same.
+// tiles as selects in every block, 0.63 ms; with a maximum per block instead of the sums' test 1%
+// more; with a raised priority around the products, the same.
 constexpr int kChunkWaves = 8, kChunkThreads = 64 * kChunkWaves, kChunkRows = 32 * kChunkWaves;
 constexpr float kSlack = 8.f;  // how far x may pass the reference before the sums are rescaled, in powers of two
 
