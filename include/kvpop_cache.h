@@ -115,7 +115,9 @@ int kvpop_cache_append(const kvpop_cache* cache, const kvpop_append* a, void* st
 /* Attention of the newest N queries of each sequence over its lists. For sequence b
  * with n = q_lens[b] queries (NULL: N; taken into [0, N]), query i < n of query head
  * qh (KV head h = qh / G, G = Hq / Hkv) sees the slots j < held[b, h] - (n - 1 - i): the
- * last n slots are the queries' own tokens, in order. With values k_j, v_j of the list
+ * last n slots are the queries' own tokens, in order. (So several queries at once are for
+ * lists that their tokens were added to at the end; a slot that kvpop_retain_step takes from
+ * another token serves single queries, which see the whole list.) With values k_j, v_j of the list
  *   lse[b, qh, i]  = log sum_j exp(scale <q_i, k_j>)
  *   o[b, qh, i, :] = sum_j exp(scale <q_i, k_j> - lse) v_j.
  * A query that sees nothing, and rows i >= n, get o = 0 and lse = -inf. held is taken

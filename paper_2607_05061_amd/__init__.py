@@ -490,6 +490,12 @@ def kvpop_cache_empty(batch: int, n_kv_heads: int, tokens: int, head_dim: int, p
     """A cache with room for ``tokens`` tokens in each list, its pages dealt to the lists in
     order. dtype: torch.int8 (the default) or torch.float8_e4m3fn."""
     torch = _torch()
+    if page_size not in (16, 32, 64, 128) or head_dim not in (64, 128):
+        raise ValueError("page_size must be 16, 32, 64 or 128, and head_dim 64 or 128")
+    if batch < 1 or n_kv_heads < 1 or tokens < 1:
+        raise ValueError("batch, n_kv_heads and tokens must be positive")
+    if dtype not in (None, torch.int8, torch.float8_e4m3fn):
+        raise TypeError("dtype must be int8 or float8_e4m3fn")
     per = -(-tokens // page_size)
     n = batch * n_kv_heads * per
     dtype = torch.int8 if dtype is None else dtype
@@ -629,7 +635,8 @@ def kvpop_cache_attn_workspace_size(cache: KvpopCache, n_q_heads: int, n_tokens:
 def kvpop_cache_attn(q, cache: KvpopCache, held, scale: float, q_lens=None, o=None, lse=None, workspace=None,
                      stream=None):
     """Attention of the newest queries q (bf16 [B, Hq, N, D]) over the lists: query i of the n =
-    q_lens[b] (None: N) of a sequence sees the slots below held[b, h] - (n - 1 - i). Returns
+    q_lens[b] (None: N) of a sequence sees the slots below held[b, h] - (n - 1 - i), so several
+    queries at once are for lists that their tokens were added to at the end. Returns
     (o bf16 [B, Hq, N, D], lse fp32 [B, Hq, N]); rows from n on, and queries that see
     nothing, get 0 and -inf."""
     torch = _torch()

@@ -155,6 +155,11 @@ def test_binding_refuses_what_the_library_cannot_see():
     c = kv.kvpop_cache_empty(1, 2, 100, 64, 32, device="cpu")
     assert c.page_table.shape == (1, 2, 4) and c.k_pages.shape == (8, 32, 64) and c.k_pages.dtype == torch.int8
     assert kv.kvpop_cache_empty(1, 1, 1, 64, dtype=torch.float8_e4m3fn, device="cpu").v_pages.dtype == torch.float8_e4m3fn
+    for bad, err in ((dict(page_size=48), ValueError), (dict(page_size=0), ValueError), (dict(head_dim=96), ValueError),
+                     (dict(batch=0), ValueError), (dict(tokens=0), ValueError), (dict(n_kv_heads=-1), ValueError),
+                     (dict(dtype=torch.float32), TypeError)):
+        with pytest.raises(err):
+            kv.kvpop_cache_empty(**{**dict(batch=1, n_kv_heads=1, tokens=5, head_dim=64, device="cpu"), **bad})
     with pytest.raises(ValueError, match="GPU"):
         kv.kvpop_cache_attn(torch.zeros(1, 2, 1, 64, dtype=torch.bfloat16), c, torch.zeros(1, 2, dtype=torch.int32), 0.1)
     with pytest.raises(ValueError, match="GPU"):

@@ -155,6 +155,29 @@ def test_not_finite_values_and_the_range_of_scales(fmt):
     host.check(cache)
 
 
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("adjacent", [False, True])
+def test_not_finite_values_that_turn(fmt, adjacent):
+    """An infinity or NaN reaches its pair's two codes and no other, whatever the angle (0 among
+    them), and moves no scale."""
+    rng = np.random.default_rng(12)
+    B, H, N, P, D = 1, 3, 20, 16, 64
+    x = rng.standard_normal((B, H, N, D))
+    x[0, 0, 1, 5], x[0, 0, 2, 6], x[0, 0, 3, 40], x[0, 0, 16, 2] = np.nan, np.inf, -np.inf, np.inf
+    k, k64 = bf16(x)
+    cos, sin, c64, s64 = _table(rng, N, 32)
+    c64[2], s64[2] = 1.0, 0.0
+    c64[16, 2], s64[7, 3] = 0.0, np.inf
+    cos, sin = torch.from_numpy(c64.astype(np.float32)).cuda(), torch.from_numpy(s64.astype(np.float32)).cuda()
+    host = HostCache(rng, B, H, 2, P, D, fmt)
+    cache = host.gpu()
+    kv.kvpop_cache_append(cache, k, k, i32(np.full((B, H), N)), rotary=(cos, sin), adjacent=adjacent)
+    for h in range(H):
+        host.append("k", cc.rotate(k64[0, h], c64, s64, adjacent), N, 0, 0, h)
+        host.append("v", k64[0, h], N, 0, 0, h)
+    host.check(cache)
+
+
 def test_rounding_borders_through_a_rotation():
     """Angles of 0, 90 and 45 degrees put sums on the borders between codes, exactly."""
     D, P = 64, 16
