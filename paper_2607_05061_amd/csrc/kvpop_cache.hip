@@ -46,22 +46,6 @@ __device__ __forceinline__ int needed_exponent(F a) {
   return clampi(e, kExpMin, kExpMax);
 }
 
-// y in 32 bits, rounded to odd where that is inexact, so that a rounding to fewer bits
-// that follows is the one rounding of y.
-__device__ __forceinline__ float to_odd(double y) {
-  const float f = (float)y;
-  const double d = (double)f;
-  uint32_t b = __float_as_uint(f);
-  if (d != y) b = (b - (__builtin_fabs(d) > __builtin_fabs(y) ? 1u : 0u)) | 1u;
-  return __uint_as_float(b);
-}
-
-__device__ __forceinline__ float to_odd(float y) { return y; }
-
-__device__ __forceinline__ double scaled(double y, int e) { return __builtin_ldexp(y, e); }
-__device__ __forceinline__ float scaled(float y, int e) { return __builtin_ldexpf(y, e); }
-__device__ __forceinline__ int nearest(double y) { return (int)__builtin_rint(y); }
-__device__ __forceinline__ int nearest(float y) { return (int)__builtin_rintf(y); }
 __device__ __forceinline__ double larger(double m, double y) { return __builtin_fmax(m, __builtin_fabs(y)); }
 __device__ __forceinline__ float larger(float m, float y) { return __builtin_fmaxf(m, __builtin_fabsf(y)); }
 
@@ -73,17 +57,50 @@ __device__ __forceinline__ float saturated(float y, float q) {
   return y == y ? __builtin_fminf(__builtin_fmaxf(y, -q), q) : 0.f;
 }
 
-// Four codes of y[0..3] (already divided by the scale, and within the codes' range).
+// The nearest whole number of y inv (inv a power of two, the product within the codes' range), in
+// the low byte: one fma with 1.5 2^52 (2^23) rounds it into the last bits of a number.
+__device__ __forceinline__ uint32_t whole(double y, double inv) {
+  return (uint32_t)__double_as_longlong(__builtin_fma(y, inv, 0x1.8p52));
+}
+__device__ __forceinline__ uint32_t whole(float y, float inv) { return __float_as_uint(__builtin_fmaf(y, inv, 0x1.8p23f)); }
+
+// y inv in 32 bits, with every nearer half-way point of the codes on its side: 20 bits of the
+// mantissa, the last one set if more follow (rounded to odd), so that a rounding to 4 bits that follows
+// is the one rounding of y.
+__device__ __forceinline__ float to_odd(double y, double inv) {
+  const uint64_t b = (uint64_t)__double_as_longlong(y * inv);
+  const uint32_t hi = (uint32_t)(b >> 32) | ((uint32_t)b != 0 ? 1u : 0u);
+  return (float)__longlong_as_double((long long)((uint64_t)hi << 32));
+}
+__device__ __forceinline__ float to_odd(float y, float inv) { return y * inv; }
+
+// Four codes of y[0..3] inv, within the codes' range.
 template <int FMT, class F>
-__device__ __forceinline__ uint32_t codes4(const F* y) {
+__device__ __forceinline__ uint32_t codes4(const F* y, F inv) {
   if constexpr (FMT == KVPOP_CACHE_INT8) {
-    const uint32_t lo = __builtin_amdgcn_perm((uint32_t)nearest(y[1]), (uint32_t)nearest(y[0]), 0x0C0C0400u);
-    const uint32_t hi = __builtin_amdgcn_perm((uint32_t)nearest(y[3]), (uint32_t)nearest(y[2]), 0x04000C0Cu);
+    const uint32_t lo = __builtin_amdgcn_perm(whole(y[1], inv), whole(y[0], inv), 0x0C0C0400u);
+    const uint32_t hi = __builtin_amdgcn_perm(whole(y[3], inv), whole(y[2], inv), 0x04000C0Cu);
     return lo | hi;
   } else {
-    const int r = __builtin_amdgcn_cvt_pk_fp8_f32(to_odd(y[0]), to_odd(y[1]), 0, false);
-    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(to_odd(y[2]), to_odd(y[3]), r, true);
+    const int r = __builtin_amdgcn_cvt_pk_fp8_f32(to_odd(y[0], inv), to_odd(y[1], inv), 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(to_odd(y[2], inv), to_odd(y[3], inv), r, true);
   }
+}
+
+// Largest magnitudes of 64-bit values by their high words, doubled (the sign falls out): integers
+// that order as the values do, up to the low words. frac: the 20 high bits of the mantissa.
+__device__ __forceinline__ uint32_t high_key(double y) {
+  return (uint32_t)((uint64_t)__double_as_longlong(y) >> 32) << 1;
+}
+// needed_exponent from the largest key; sure: false where the low words would decide.
+template <int FMT>
+__device__ __forceinline__ int needed_exponent_of_key(uint32_t key, bool& sure) {
+  constexpr uint32_t border = FMT == KVPOP_CACHE_INT8 ? 0xFC000u : 0xC0000u;  // 127/64 - 1, 7/4 - 1
+  const int x = (int)(key >> 21) - 1022;
+  const uint32_t frac = key >> 1 & 0xFFFFFu;
+  sure = frac != border;
+  const int e = FMT == KVPOP_CACHE_INT8 ? x - (frac < border ? 7 : 6) : x - (frac < border ? 9 : 8);
+  return clampi(e, kExpMin, kExpMax);
 }
 
 // Four codes moved to a scale 2^-shift times coarser (shift < 0).
@@ -271,6 +288,7 @@ __device__ __forceinline__ void write_page(const AppendLaunch& a, const PageJob&
   uint8_t* codes = pool + (int64_t)page * a.c.P * D;
   const int was = job.before > 0 || job.after > 0 ? clampi(exps[page], kExpMin, kExpMax) : kExpMin;
   F y[ITER][2][8], big = 0;
+  uint32_t key = 0;
   float odd = 0.f;  // NaN if a value may be NaN or infinite
 #pragma unroll
   for (int it = 0; it < ITER; ++it) {
@@ -279,9 +297,17 @@ __device__ __forceinline__ void write_page(const AppendLaunch& a, const PageJob&
     turned(p, q, pc.turn && rot, g[it], y[it][0], y[it][1]);
     odd += not_finite(p, q, g[it]);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) big = larger(big, y[it][i / 8][i % 8]);  // passes over NaN
+    for (int i = 0; i < 16; ++i) {
+      if constexpr (sizeof(F) == 8)
+        key = max(key, high_key(y[it][i / 8][i % 8]));
+      else
+        big = larger(big, y[it][i / 8][i % 8]);  // passes over NaN
+    }
   }
-  if (odd != odd) {
+  bool sure = sizeof(F) == 4;
+  int need = 0;
+  if constexpr (sizeof(F) == 8) need = needed_exponent_of_key<FMT>(key, sure);
+  if (odd != odd || !sure) {
     big = 0;
 #pragma unroll
     for (int it = 0; it < ITER; ++it)
@@ -290,30 +316,30 @@ __device__ __forceinline__ void write_page(const AppendLaunch& a, const PageJob&
         const F v = larger(0, y[it][i / 8][i % 8]);
         big = v < (F)__builtin_inff() ? larger(big, v) : big;
       }
+    need = needed_exponent<FMT>(big);
+  } else if constexpr (sizeof(F) == 4) {
+    need = needed_exponent<FMT>(big);
   }
-  int need = needed_exponent<FMT>(big);
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) need = max(need, __shfl_xor(need, o));
   if ((tid & 63) == 0) need_sh[tid >> 6] = need;
   __syncthreads();
   for (int i = 0; i < (int)(blockDim.x >> 6); ++i) need = max(need, need_sh[i]);
   const int e = max(need, was);
-#pragma unroll
-  for (int it = 0; it < ITER; ++it)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) y[it][i / 8][i % 8] = scaled(y[it][i / 8][i % 8], -e);
+  const F inv = (F)__builtin_ldexpf(1.f, -e);
   // Within the codes' range, unless a value is not finite or the largest scale does not hold it.
   if (odd != odd || e == kExpMax) {
+    const F most = (F)(FMT == KVPOP_CACHE_INT8 ? 127 : 448) * (F)__builtin_ldexpf(1.f, e);
 #pragma unroll
     for (int it = 0; it < ITER; ++it)
 #pragma unroll
-      for (int i = 0; i < 16; ++i)
-        y[it][i / 8][i % 8] = saturated(y[it][i / 8][i % 8], (F)(FMT == KVPOP_CACHE_INT8 ? 127 : 448));
+      for (int i = 0; i < 16; ++i) y[it][i / 8][i % 8] = saturated(y[it][i / 8][i % 8], most);
   }
 #pragma unroll
   for (int it = 0; it < ITER; ++it) {
     const int r = it * rows + r0;
-    u32x2 lo = {codes4<FMT>(y[it][0]), codes4<FMT>(y[it][0] + 4)}, hi = {codes4<FMT>(y[it][1]), codes4<FMT>(y[it][1] + 4)};
+    u32x2 lo = {codes4<FMT>(y[it][0], inv), codes4<FMT>(y[it][0] + 4, inv)};
+    u32x2 hi = {codes4<FMT>(y[it][1], inv), codes4<FMT>(y[it][1] + 4, inv)};
     if (a.adjacent) {
       const u32x2 u = lo, v = hi;
       lo = u32x2{__builtin_amdgcn_perm(v.x, u.x, 0x05010400u), __builtin_amdgcn_perm(v.x, u.x, 0x07030602u)};
