@@ -372,9 +372,9 @@ __device__ __forceinline__ void write_page(const AppendLaunch& a, const PageJob&
 // workgroups, so nothing depends on their order. Keys that turn are held in
 // 64 bits, others in 32, where bf16 is exact. The workgroups after those turn the queries.
 // HBM bounds large calls: 3 ragged chunks of 20001 tokens (28 query heads, 4 lists each, 1.05 GB)
-// 221 us, 4.7 TB/s; 8 x 4 lists of 8192 with as many query heads 79-93 us (0.31 GB). Small
+// 217-221 us, 4.8 TB/s; 4 x 8 lists of 8192 with as many query heads 76-89 us (0.31 GB). Small
 // ones are the latency of one page's loads: 5 us for one token of 8 lists, 6 us for one of 1024.
-// With the angles read per element and head instead: 455 us for the chunks, 52 instead of 15 us
+// With the angles read per element and head instead: 455 us for the chunks, 52 instead of 14 us
 // for 16 lists that gather 2276 of 32768 tokens.
 template <int D, int FMT, int ITER>
 __global__ __launch_bounds__(512) void cache_append_kernel(AppendLaunch a, int pages, int64_t kv_blocks) {
