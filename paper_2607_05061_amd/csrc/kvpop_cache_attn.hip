@@ -7,8 +7,8 @@
 // One pass with a running maximum. A value's power of two goes into the exponent of its
 // probability: with x = l log2(e) + ve and M the running maximum of x, the numerators
 // p' = 2^(x - M) <= 1 multiply the bare codes, and the normaliser in the same units is
-// sum p' 2^-ve. (In the chunk kernel M may lag, and p' reach 2^15.) So codes enter the products as they are, exact in 16 bits, whatever
-// scales a list's pages have.
+// sum p' 2^-ve. (In the chunk kernel M may lag, and p' reach 2^15.) So codes enter the
+// products as they are, exact in 16 bits, whatever scales a list's pages have.
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
