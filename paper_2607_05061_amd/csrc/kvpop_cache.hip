@@ -352,7 +352,7 @@ __device__ __forceinline__ void write_page(const AppendLaunch& a, const PageJob&
     }
   }
   if (tid == 0) exps[page] = (int8_t)e;
-  const int n_before = max(job.before, 0), n_old = n_before + max(job.after, 0);
+  const int n_before = job.before, n_old = n_before + job.after;
   if (n_old > 0 && e > was) {
     for (int i = r0; i < n_old; i += rows) {
       const int r = i < n_before ? i : job.first_row + job.n_rows + (i - n_before);
@@ -397,7 +397,9 @@ __global__ __launch_bounds__(512) void cache_append_kernel(AppendLaunch a, int p
   const int64_t first = nth * P, lo = max(start, first), hi = min(start + cnt, first + P);
   if (lo >= hi) return;
   job.n_rows = (int)(hi - lo), job.first_row = (int)(lo - first), job.entry = (int)(lo - start);
-  job.before = (int)(min(lo, held) - first), job.after = (int)(min(held, first + P) - hi);
+  // held is any number: these fit 32 bits only once they are within the page.
+  job.before = (int)max(min(lo, held) - first, (int64_t)0);
+  job.after = (int)max(min(held, first + P) - hi, (int64_t)0);
   job.nth = (int)nth;
   if (side == 0 && a.rot)
     write_page<D, FMT, ITER, double>(a, job, a.k, a.rot, a.c.k, a.c.ke, need_sh);
