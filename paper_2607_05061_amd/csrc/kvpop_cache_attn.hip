@@ -7,7 +7,7 @@
 // One pass with a running maximum. A value's power of two goes into the exponent of its
 // probability: with x = l log2(e) + ve and M the running maximum of x, the numerators
 // p' = 2^(x - M) <= 1 multiply the bare codes, and the normaliser in the same units is
-// sum p' 2^-ve. (In the chunk kernel M may lag, and p' reach 2^15.) So codes enter the
+// sum p' 2^-ve. (In the chunk kernel M may lag, and p' reach 2^16.) So codes enter the
 // products as they are, exact in 16 bits, whatever scales a list's pages have.
 
 #include <hip/hip_runtime.h>
@@ -380,7 +380,7 @@ __global__ __launch_bounds__(64 * W) void cache_attn_kernel(CacheAttnLaunch a, i
 // of the dense peak), D = 64 0.36 ms. Matrix cores are busy on 44% of the cycles, the vector ALU
 // (exponential, its argument and sum per pair, the widening) on 57%, LDS on 32%. With the
 // numerators of 64 keys after all their logits, and two buffers: 0.70 ms; with the masks of the last
-// tiles as selects in every block, 0.63 ms; with a maximum per block instead of the sums' test 1%
+// tiles as selects in every block, 0.63 ms; with a maximum per block instead of the sums' test 3-5%
 // more; with a raised priority around the products, the same.
 constexpr int kChunkWaves = 8, kChunkThreads = 64 * kChunkWaves, kChunkRows = 32 * kChunkWaves;
 constexpr float kSlack = 8.f;  // how far x may pass the reference before the sums are rescaled, in powers of two
@@ -551,9 +551,11 @@ __global__ __attribute__((amdgpu_flat_work_group_size(kChunkThreads, kChunkThrea
     return x;
   };
   // Numerators 2^(x - M) of a block of 32 keys from its bare products, summed and in 16 bits. The
-  // usual block is all seen, and none of its numerators passes 2^15 or is NaN: their sums
-  // show it. Any other is done over with its keys that are not seen left out, and M moved
-  // where one passes it by more than kSlack.
+  // usual block is all seen, and none of its numerators passes f16's range or is NaN: their sums
+  // show it. For a query that does not see all of a block, or whose own sums pass the range,
+  // it is done over without the keys that are not seen, and with M moved where one passes it by
+  // more than kSlack. The wave's other queries keep what they have: a query's bits follow
+  // from its own products alone.
   auto numerators = [&](const f32x16& x, int e0, int e1, int key0, f16x8 (&p)[2]) __attribute__((always_inline)) {
     const float kc0 = __builtin_ldexpf(cq, (int16_t)e0), kc1 = __builtin_ldexpf(cq, (int16_t)e1);
     const float v0 = (float)(e0 >> 16), v1 = (float)(e1 >> 16), m0 = v0 - M, m1 = v1 - M;
@@ -566,20 +568,28 @@ __global__ __attribute__((amdgpu_flat_work_group_size(kChunkThreads, kChunkThrea
       s0 += y0, s1 += y1;
       p[0][r] = (_Float16)y0, p[1][r] = (_Float16)y1;
     }
-    const bool whole = key0 + 32 <= sure && e0 != kNoPage && e1 != kNoPage;
-    if (!whole || __builtin_amdgcn_ballot_w64(!(s0 <= 0x1p15f && s1 <= 0x1p15f)) != 0) {
-      int key = key0 + 4 * hi;
-      asm volatile("" : "+v"(key));  // the comparisons stay in this branch
+    const bool pages = e0 != kNoPage && e1 != kNoPage, whole = key0 + 32 <= sure && pages;
+    const uint64_t over = __builtin_amdgcn_ballot_w64(!(s0 <= 65504.f && s1 <= 65504.f));
+    if (!whole || over != 0) {
       f32x16 y;
       float mx = neg_inf();
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         y[r] = __builtin_fmaf(x[r], r < 8 ? kc0 : kc1, r < 8 ? v0 : v1);
-        if ((r < 8 ? e0 : e1) == kNoPage || key + 8 * (r >> 2) + (r & 3) >= seen) y[r] = neg_inf();
-        mx = fmaxf(mx, y[r]);
       }
+      if (!whole) {
+        int key = key0 + 4 * hi;
+        asm volatile("" : "+v"(key));  // the comparisons stay in this branch
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if ((r < 8 ? e0 : e1) == kNoPage || key + 8 * (r >> 2) + (r & 3) >= seen) y[r] = neg_inf();
+      }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, y[r]);
       mx = max_pair(mx);
-      const float m = mx > M + kSlack ? mx : M, mu = m == neg_inf() ? 0.f : m;
+      const bool asks = ((uint32_t)(over | over >> 32) >> col & 1) != 0;  // in either of the query's lanes
+      const bool keep = key0 + 32 <= seen && pages && !asks;
+      const float m = !keep && mx > M + kSlack ? mx : M, mu = m == neg_inf() ? 0.f : m;
       if (__builtin_amdgcn_ballot_w64(m != M) != 0) {
         const float f = __builtin_amdgcn_exp2f(M - mu);
 #pragma unroll
@@ -587,12 +597,14 @@ __global__ __attribute__((amdgpu_flat_work_group_size(kChunkThreads, kChunkThrea
         S *= f;
         M = m;
       }
-      s0 = s1 = 0.f;
+      if (!keep) {
+        s0 = s1 = 0.f;
 #pragma unroll
-      for (int r = 0; r < 8; ++r) {
-        const float y0 = __builtin_amdgcn_exp2f(y[r] - mu), y1 = __builtin_amdgcn_exp2f(y[r + 8] - mu);
-        s0 += y0, s1 += y1;
-        p[0][r] = (_Float16)y0, p[1][r] = (_Float16)y1;
+        for (int r = 0; r < 8; ++r) {
+          const float y0 = __builtin_amdgcn_exp2f(y[r] - mu), y1 = __builtin_amdgcn_exp2f(y[r + 8] - mu);
+          s0 += y0, s1 += y1;
+          p[0][r] = (_Float16)y0, p[1][r] = (_Float16)y1;
+        }
       }
     }
     S = __builtin_fmaf(s0, w0, __builtin_fmaf(s1, w1, S));
