@@ -4,11 +4,15 @@
 //   l(i, j) = scale <q_i, k_j>,  k_j = code 2^ke,  v_j = code 2^ve,
 //   lse_i   = log sum_j exp l(i, j),   o_i = sum_j exp(l(i, j) - lse_i) v_j.
 //
-// One pass with a running maximum. A value's power of two goes into the exponent of its
-// probability: with x = l log2(e) + ve and M the running maximum of x, the numerators
-// p' = 2^(x - M) <= 1 multiply the bare codes, and the normaliser in the same units is
-// sum p' 2^-ve. (In the chunk kernel M may lag, and p' reach 2^16.) So codes enter the
-// products as they are, exact in 16 bits, whatever scales a list's pages have.
+// One pass with a running reference. A value's power of two goes into the exponent of its
+// probability: with x = l log2(e) + ve, the numerators p' = 2^(x - M) multiply the bare codes,
+// and the normaliser in the same units is sum p' 2^-ve. So codes enter the products as they
+// are, exact in 16 bits, whatever scales a list's pages have. Numerators are f16 there (the
+// normaliser sums them in 32 bits): M lies below the running maximum of x, so that a numerator far
+// below the largest one keeps its 11 bits: the largest is at least 2^7, so they reach down to
+// 2^-21 of it (2^-14 is f16's least normal number), and below that what is lost is 2^-32 of it at
+// most. (With M = max x, a sink's 2^27 times larger probability, or a scale 2^24 times another
+// page's, took the other keys out of o and left them in the normaliser.)
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -29,6 +33,9 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kExpMin = -32, kExpMax = 32;
+// Where M moves, the largest numerator becomes 2^kRoom. (A reference 7 below the maximum, rounded to 32 bits, is
+// at most 8 below it, whatever its size, and no numerator passes f16's range; 9 and more can become 16.)
+constexpr float kRoom = 7.f;
 constexpr int kNoPage = 0x7FFF7FFF;  // in the place of a page's exponents
 constexpr int kRows = 16;        // (token, head) rows per workgroup
 constexpr int kTile = 32;        // keys per step of a wave
@@ -262,7 +269,7 @@ __global__ __launch_bounds__(64 * W) void cache_attn_kernel(CacheAttnLaunch a, i
     }
     float mx = fmaxf(fmaxf(fmaxf(l[0][0], l[0][1]), fmaxf(l[0][2], l[0][3])),
                      fmaxf(fmaxf(l[1][0], l[1][1]), fmaxf(l[1][2], l[1][3])));
-    mx = max_groups(mx);
+    mx = max_groups(mx) - kRoom;
     if (__builtin_amdgcn_ballot_w64(mx > M) != 0) {
       const float m = fmaxf(M, mx);
       const float f = __builtin_amdgcn_exp2f(M - (m == neg_inf() ? 0.f : m));
@@ -383,7 +390,7 @@ __global__ __launch_bounds__(64 * W) void cache_attn_kernel(CacheAttnLaunch a, i
 // tiles as selects in every block, 0.63 ms; with a maximum per block instead of the sums' test 3-5%
 // more; with a raised priority around the products, the same.
 constexpr int kChunkWaves = 8, kChunkThreads = 64 * kChunkWaves, kChunkRows = 32 * kChunkWaves;
-constexpr float kSlack = 8.f;  // how far x may pass the reference before the sums are rescaled, in powers of two
+constexpr float kSlack = 12.f;  // how far x may pass M, in powers of two, in a block that a query sees a part of
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
@@ -589,7 +596,7 @@ __global__ __attribute__((amdgpu_flat_work_group_size(kChunkThreads, kChunkThrea
       mx = max_pair(mx);
       const bool asks = ((uint32_t)(over | over >> 32) >> col & 1) != 0;  // in either of the query's lanes
       const bool keep = key0 + 32 <= seen && pages && !asks;
-      const float m = !keep && mx > M + kSlack ? mx : M, mu = m == neg_inf() ? 0.f : m;
+      const float m = !keep && mx > M + kSlack ? mx - kRoom : M, mu = m == neg_inf() ? 0.f : m;
       if (__builtin_amdgcn_ballot_w64(m != M) != 0) {
         const float f = __builtin_amdgcn_exp2f(M - mu);
 #pragma unroll
