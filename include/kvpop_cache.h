@@ -109,7 +109,8 @@ typedef struct kvpop_append {
  * src, q without q_out, or q_out or the cache over an input or each other.
  * KVPOP_EUNSUPPORTED: head_dim, page_size, format, rot_dim not a multiple of 16,
  * strides not multiples of 8, alignment (the int32 arrays need 4 bytes, the
- * exponents 1, the others 16), or more than 2^31 - 1 workgroups. */
+ * exponents 1, the others 16), or more than one launch takes (2^32 - 1 threads, of
+ * which a page that a list may reach into takes 128 or more). */
 int kvpop_cache_append(const kvpop_cache* cache, const kvpop_append* a, void* stream);
 
 /* Attention of the newest N queries of each sequence over its lists. For sequence b
@@ -160,7 +161,10 @@ typedef struct kvpop_retain {
  * with evict from kvpop_running_topk and S >= sinks + window + topk there are none.
  * scores: fp32 [B, H, T] (of kvpop_running_topk); evict: int32 [B, H, T]; log_gamma: fp32
  * [H] or NULL. All of st's arrays are outputs. evict may be that of a longer sequence:
- * a token's place in the mask does not depend on later tokens. */
+ * a token's place in the mask does not depend on later tokens.
+ * KVPOP_EINVAL: a missing pointer, sizes < 1, or an output over an input or another one.
+ * KVPOP_EUNSUPPORTED: T or S > KVPOP_MAX_SEQ_LEN, alignment (4 bytes), or more than one
+ * launch takes (2^32 - 1 threads, 1024 per list and 4096 positions). */
 int kvpop_retain_prompt(const kvpop_retain* st, int32_t seq_len, const int32_t* evict, const float* scores,
                         const float* log_gamma, const int32_t* lens, void* stream);
 
@@ -175,7 +179,9 @@ int kvpop_retain_prompt(const kvpop_retain* st, int32_t seq_len, const int32_t* 
  * list is eligible, or if window = 0 and the new token itself is the least. The new token's
  * prio is 0 until it leaves the window (its own if window = 0). A list so held is
  * what kvpop_running_topk's mask keeps at query q. S >= sinks + window + topk.
- * scores: fp32 [B, H]; q_pos: int32 [B]; slot: int32 [B, H] (output). */
+ * scores: fp32 [B, H]; q_pos: int32 [B]; slot: int32 [B, H] (output).
+ * KVPOP_EINVAL: as above, sinks or window < 0, topk < 1, or S too small for them.
+ * KVPOP_EUNSUPPORTED: as above (256 threads per list). */
 int kvpop_retain_step(const kvpop_retain* st, const float* scores, const float* log_gamma, const int32_t* q_pos,
                       int32_t sinks, int32_t window, int32_t topk, int32_t* slot, void* stream);
 

@@ -252,7 +252,7 @@ int check_cache_attn_dims(const kvpop_cache* c, int32_t Hq, int32_t N, kvpop::Ca
   L->c = make_view(c);
   L->Hq = Hq;
   L->N = N;
-  if (kvpop::cache_attn_blocks(*L) > INT32_MAX || rows > (int64_t)INT32_MAX * 4) return KVPOP_EUNSUPPORTED;
+  if (kvpop::cache_attn_threads(*L) > UINT32_MAX) return KVPOP_EUNSUPPORTED;
   return KVPOP_OK;
 }
 
@@ -570,7 +570,7 @@ int kvpop_cache_append(const kvpop_cache* cache, const kvpop_append* a, void* st
   L.rot = a->rot_dim;
   L.adjacent = a->adjacent;
   L.stream = stream;
-  if (kvpop::cache_append_blocks(L) > INT32_MAX) return KVPOP_EUNSUPPORTED;
+  if (kvpop::cache_append_threads(L) > UINT32_MAX) return KVPOP_EUNSUPPORTED;
   return launch([&] { return kvpop::launch_cache_append(L); });
 }
 
@@ -630,7 +630,7 @@ int kvpop_retain_prompt(const kvpop_retain* s, int32_t seq_len, const int32_t* e
   L.evict = evict;
   L.lens = lens;
   L.T = seq_len;
-  if (lists * ((seq_len + 1023) / 1024) > INT32_MAX) return KVPOP_EUNSUPPORTED;  // more workgroups than a grid holds
+  if (kvpop::retain_prompt_threads(L) > UINT32_MAX) return KVPOP_EUNSUPPORTED;
   return launch([&] { return kvpop::launch_retain_prompt(L); });
 }
 
@@ -652,6 +652,7 @@ int kvpop_retain_step(const kvpop_retain* s, const float* scores, const float* l
   L.window = window;
   L.topk = topk;
   L.slot = slot;
+  if (kvpop::retain_step_threads(L) > UINT32_MAX) return KVPOP_EUNSUPPORTED;
   return launch([&] { return kvpop::launch_retain_step(L); });
 }
 

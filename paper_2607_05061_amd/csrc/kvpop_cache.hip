@@ -423,12 +423,19 @@ AppendShape append_shape(const AppendLaunch& L) {
   return {threads, 2};
 }
 
+int64_t append_blocks(const AppendLaunch& L) {
+  const int64_t kv = 2LL * L.c.B * L.c.H * append_pages(L);
+  const int64_t items = L.q.ptr ? (int64_t)L.c.B * L.N * ((L.Hq + kQHeads - 1) / kQHeads) : 0;
+  const int64_t per = append_shape(L).threads / (L.c.D / 16);
+  return kv + (items + per - 1) / per;
+}
+
 template <int D, int FMT>
 int launch_append(const AppendLaunch& L) {
   const AppendShape s = append_shape(L);
   const int pages = append_pages(L);
   const int64_t kv = 2LL * L.c.B * L.c.H * pages;
-  const dim3 grid((unsigned)cache_append_blocks(L)), block(s.threads);
+  const dim3 grid((unsigned)append_blocks(L)), block(s.threads);
   const hipStream_t st = (hipStream_t)L.stream;
   if (s.iter == 1)
     hipLaunchKernelGGL((cache_append_kernel<D, FMT, 1>), grid, block, 0, st, L, pages, kv);
@@ -575,15 +582,11 @@ __global__ __launch_bounds__(kPromptThreads) void retain_prompt_kernel(RetainLau
   if (tid == 0) a.held[list] = held;
 }
 
+int prompt_parts(const RetainLaunch& L) { return (L.T + kPromptPart - 1) / kPromptPart; }
+
 }  // namespace
 
-int64_t cache_append_blocks(const AppendLaunch& L) {
-  const AppendShape s = append_shape(L);
-  const int64_t kv = 2LL * L.c.B * L.c.H * append_pages(L);
-  const int64_t items = L.q.ptr ? (int64_t)L.c.B * L.N * ((L.Hq + kQHeads - 1) / kQHeads) : 0;
-  const int64_t per = s.threads / (L.c.D / 16);
-  return kv + (items + per - 1) / per;
-}
+int64_t cache_append_threads(const AppendLaunch& L) { return append_blocks(L) * append_shape(L).threads; }
 
 int launch_cache_append(const AppendLaunch& L) {
   const bool i8 = L.c.format == KVPOP_CACHE_INT8;
@@ -592,12 +595,16 @@ int launch_cache_append(const AppendLaunch& L) {
   return i8 ? launch_append<128, KVPOP_CACHE_INT8>(L) : launch_append<128, KVPOP_CACHE_E4M3>(L);
 }
 
+int64_t retain_prompt_threads(const RetainLaunch& L) { return (int64_t)L.B * L.H * prompt_parts(L) * kPromptThreads; }
+
 int launch_retain_prompt(const RetainLaunch& L) {
-  const int parts = (L.T + kPromptPart - 1) / kPromptPart;
+  const int parts = prompt_parts(L);
   hipLaunchKernelGGL(retain_prompt_kernel, dim3((unsigned)(L.B * L.H * parts)), dim3(kPromptThreads), 0,
                      (hipStream_t)L.stream, L, parts);
   return (int)hipGetLastError();
 }
+
+int64_t retain_step_threads(const RetainLaunch& L) { return (int64_t)L.B * L.H * kStepThreads; }
 
 int launch_retain_step(const RetainLaunch& L) {
   hipLaunchKernelGGL(retain_step_kernel, dim3((unsigned)(L.B * L.H)), dim3(kStepThreads), 0, (hipStream_t)L.stream, L);

@@ -840,7 +840,7 @@ Plan plan(const CacheAttnLaunch& L) {
 template <int D, int FMT>
 int launch_attn(const CacheAttnLaunch& L) {
   const Plan p = plan(L);
-  const dim3 grid((unsigned)cache_attn_blocks(L)), block(64 * p.waves);
+  const dim3 grid((unsigned)(L.c.B * L.c.H * p.row_blocks * p.splits)), block(64 * p.waves);
   const hipStream_t st = (hipStream_t)L.stream;
   if (p.chunk)
     hipLaunchKernelGGL((cache_attn_chunk_kernel<D, FMT>), grid, block, 0, st, L, p.row_blocks, p.splits);
@@ -864,9 +864,9 @@ int launch_attn(const CacheAttnLaunch& L) {
 
 }  // namespace
 
-int64_t cache_attn_blocks(const CacheAttnLaunch& L) {
+int64_t cache_attn_threads(const CacheAttnLaunch& L) {
   const Plan p = plan(L);
-  return (int64_t)L.c.B * L.c.H * p.row_blocks * p.splits;
+  return (int64_t)L.c.B * L.c.H * p.row_blocks * p.splits * (64 * p.waves);
 }
 
 int64_t cache_attn_workspace_floats(const CacheAttnLaunch& L) {

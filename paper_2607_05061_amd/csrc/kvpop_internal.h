@@ -119,10 +119,12 @@ int launch_cache_append(const AppendLaunch& L);
 int launch_cache_attn(const CacheAttnLaunch& L);
 int launch_retain_prompt(const RetainLaunch& L);
 int launch_retain_step(const RetainLaunch& L);
-// Workgroups of the launches above (checked against the grid limit), and floats of
-// workspace of the attention.
-int64_t cache_append_blocks(const AppendLaunch& L);
-int64_t cache_attn_blocks(const CacheAttnLaunch& L);
+// Threads of the launches above (a launch takes 2^32 - 1 at most), and floats of workspace
+// of the attention.
+int64_t cache_append_threads(const AppendLaunch& L);
+int64_t cache_attn_threads(const CacheAttnLaunch& L);
+int64_t retain_prompt_threads(const RetainLaunch& L);
+int64_t retain_step_threads(const RetainLaunch& L);
 int64_t cache_attn_workspace_floats(const CacheAttnLaunch& L);
 
 // Each returns 0 on success or the hipError_t of a failed launch.
