@@ -222,6 +222,13 @@ def _on_launch_stream(stream, device):
     return torch.cuda.stream(stream)
 
 
+def _check_workspace(workspace, need: int, device):
+    """A caller's workspace: ``need`` bytes after each other (a view with strides may name as many elements
+    and have less memory) on the device of the inputs."""
+    if workspace.numel() * workspace.element_size() < need or workspace.device != device or not workspace.is_contiguous():
+        raise ValueError("workspace must hold %d contiguous bytes on the device of the inputs" % need)
+
+
 def _prep_inputs(q, k, key_bias):
     torch = _torch()
     _check_tensor(q, "q", torch.bfloat16, None)
@@ -383,8 +390,8 @@ def kvpop_running_topk(scores, sinks: int, window: int, topk: int, log_gamma=Non
         else:
             with _on_launch_stream(stream, scores.device):
                 workspace = torch.empty(need, dtype=torch.uint8, device=scores.device)
-    elif workspace.numel() * workspace.element_size() < need or workspace.device != scores.device:
-        raise ValueError("workspace must hold %d bytes on the device of scores" % need)
+    else:
+        _check_workspace(workspace, need, scores.device)
     out = {n: torch.empty((B, H, T), dtype=torch.int32, device=scores.device) for n in ("rank", "cutoff")}
     if labels:
         out["label"] = torch.empty((B, H, T), dtype=torch.int32, device=scores.device)
@@ -655,8 +662,8 @@ def kvpop_cache_attn(q, cache: KvpopCache, held, scale: float, q_lens=None, o=No
             else:
                 with _on_launch_stream(stream, q.device):
                     workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
-    elif workspace.numel() * workspace.element_size() < need or workspace.device != q.device:
-        raise ValueError("workspace must hold %d bytes on the device of the cache" % need)
+    else:
+        _check_workspace(workspace, need, q.device)
     _call(torch, lib().kvpop_cache_attn, dev, stream, c, Hq, N, float(scale), _ROWS_PACK.pack(*qr),
           _ptr(held, "held", i32, (B, H), dev), _ptr(q_lens, "q_lens", i32, (B,), dev),
           _ptr(o, "o", torch.bfloat16, (B, Hq, N, D), dev), _ptr(lse, "lse", torch.float32, (B, Hq, N), dev),
