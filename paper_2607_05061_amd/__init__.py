@@ -118,51 +118,60 @@ def lib() -> ctypes.CDLL:
             raise RuntimeError("libkvpop.so not found at %s: build it with "
                                "`python -m paper_2607_05061_amd.build`" % path)
         L = ctypes.CDLL(path)
-        P, I32, F = ctypes.c_void_p, ctypes.c_int32, ctypes.c_float
-        D = ctypes.POINTER(KvpopDims)
-        L.kvpop_row_lse.argtypes = [D, P, P, P, P, P]
-        L.kvpop_row_lse.restype = ctypes.c_int
-        L.kvpop_future_attn_from_lse.argtypes = [D, P, P, P, P, I32, I32, P, P]
-        L.kvpop_future_attn_from_lse.restype = ctypes.c_int
-        L.kvpop_future_attn_bands.argtypes = [D, P, P, P, P, I32, ctypes.POINTER(I32), ctypes.POINTER(I32),
-                                              ctypes.POINTER(P), P]
-        L.kvpop_future_attn_bands.restype = ctypes.c_int
-        L.kvpop_future_attn_target.argtypes = [D, P, P, P, I32, I32, P, P, P]
-        L.kvpop_future_attn_target.restype = ctypes.c_int
-        L.kvpop_future_attn_scores.argtypes = [D, P, P, P, P, I32, I32, I32, F, I32, P, P, P]
-        L.kvpop_future_attn_scores.restype = ctypes.c_int
-        L.kvpop_internal_scores_spread.argtypes = [D, I32, I32]
-        L.kvpop_internal_scores_spread.restype = ctypes.c_int
-        L.kvpop_running_topk_workspace_size.argtypes = [ctypes.POINTER(KvpopTopkDims)]
-        L.kvpop_running_topk_workspace_size.restype = ctypes.c_size_t
-        L.kvpop_running_topk.argtypes = [ctypes.POINTER(KvpopTopkDims), P, P, I32, I32, I32, P, P, P, P, P, P,
-                                         ctypes.c_size_t, P]
-        L.kvpop_running_topk.restype = ctypes.c_int
-        L.kvpop_running_topk_noalloc.argtypes = [ctypes.POINTER(KvpopTopkDims), P, P, I32, I32, I32, P, P, P, P, P,
-                                                 P]
-        L.kvpop_running_topk_noalloc.restype = ctypes.c_int
-        L.kvpop_sparse_attn_fwd.argtypes = [ctypes.POINTER(KvpopDims), P, P, P, P, P, P, P, P]
-        L.kvpop_sparse_attn_fwd.restype = ctypes.c_int
-        # Structures go by address: a ctypes mirror by reference, or its packed bytes.
-        C = R = S = P
-        L.kvpop_cache_append.argtypes = [C, P, P]
-        L.kvpop_cache_append.restype = ctypes.c_int
-        L.kvpop_cache_attn_workspace_size.argtypes = [C, I32, I32]
-        L.kvpop_cache_attn_workspace_size.restype = ctypes.c_size_t
-        L.kvpop_cache_attn.argtypes = [C, I32, I32, F, R, P, P, P, P, P, ctypes.c_size_t, P]
-        L.kvpop_cache_attn.restype = ctypes.c_int
-        L.kvpop_retain_prompt.argtypes = [S, I32, P, P, P, P, P]
-        L.kvpop_retain_prompt.restype = ctypes.c_int
-        L.kvpop_retain_step.argtypes = [S, P, P, P, I32, I32, I32, P, P]
-        L.kvpop_retain_step.restype = ctypes.c_int
-        L.kvpop_strerror.argtypes = [ctypes.c_int]
-        L.kvpop_strerror.restype = ctypes.c_char_p
-        L.kvpop_abi_version.argtypes = []
-        L.kvpop_abi_version.restype = ctypes.c_int
-        if L.kvpop_abi_version() != ABI_VERSION:
-            raise RuntimeError("libkvpop ABI version %d, binding expects %d" % (L.kvpop_abi_version(), ABI_VERSION))
+        try:
+            _set_types(L)
+        except AttributeError as e:  # a library of an older build has fewer entry points
+            raise RuntimeError("libkvpop.so at %s is not the one this binding was written for (%s): rebuild it with "
+                               "`python -m paper_2607_05061_amd.build`" % (path, e)) from None
         _LIB = L
     return _LIB
+
+
+def _set_types(L: ctypes.CDLL):
+    """Checks the library's version and sets its entry points' types."""
+    L.kvpop_abi_version.argtypes = []
+    L.kvpop_abi_version.restype = ctypes.c_int
+    if L.kvpop_abi_version() != ABI_VERSION:
+        raise RuntimeError("libkvpop ABI version %d, binding expects %d" % (L.kvpop_abi_version(), ABI_VERSION))
+    P, I32, F = ctypes.c_void_p, ctypes.c_int32, ctypes.c_float
+    D = ctypes.POINTER(KvpopDims)
+    L.kvpop_row_lse.argtypes = [D, P, P, P, P, P]
+    L.kvpop_row_lse.restype = ctypes.c_int
+    L.kvpop_future_attn_from_lse.argtypes = [D, P, P, P, P, I32, I32, P, P]
+    L.kvpop_future_attn_from_lse.restype = ctypes.c_int
+    L.kvpop_future_attn_bands.argtypes = [D, P, P, P, P, I32, ctypes.POINTER(I32), ctypes.POINTER(I32),
+                                          ctypes.POINTER(P), P]
+    L.kvpop_future_attn_bands.restype = ctypes.c_int
+    L.kvpop_future_attn_target.argtypes = [D, P, P, P, I32, I32, P, P, P]
+    L.kvpop_future_attn_target.restype = ctypes.c_int
+    L.kvpop_future_attn_scores.argtypes = [D, P, P, P, P, I32, I32, I32, F, I32, P, P, P]
+    L.kvpop_future_attn_scores.restype = ctypes.c_int
+    L.kvpop_internal_scores_spread.argtypes = [D, I32, I32]
+    L.kvpop_internal_scores_spread.restype = ctypes.c_int
+    L.kvpop_running_topk_workspace_size.argtypes = [ctypes.POINTER(KvpopTopkDims)]
+    L.kvpop_running_topk_workspace_size.restype = ctypes.c_size_t
+    L.kvpop_running_topk.argtypes = [ctypes.POINTER(KvpopTopkDims), P, P, I32, I32, I32, P, P, P, P, P, P,
+                                     ctypes.c_size_t, P]
+    L.kvpop_running_topk.restype = ctypes.c_int
+    L.kvpop_running_topk_noalloc.argtypes = [ctypes.POINTER(KvpopTopkDims), P, P, I32, I32, I32, P, P, P, P, P,
+                                             P]
+    L.kvpop_running_topk_noalloc.restype = ctypes.c_int
+    L.kvpop_sparse_attn_fwd.argtypes = [ctypes.POINTER(KvpopDims), P, P, P, P, P, P, P, P]
+    L.kvpop_sparse_attn_fwd.restype = ctypes.c_int
+    # Structures go by address: a ctypes mirror by reference, or its packed bytes.
+    C = R = S = P
+    L.kvpop_cache_append.argtypes = [C, P, P]
+    L.kvpop_cache_append.restype = ctypes.c_int
+    L.kvpop_cache_attn_workspace_size.argtypes = [C, I32, I32]
+    L.kvpop_cache_attn_workspace_size.restype = ctypes.c_size_t
+    L.kvpop_cache_attn.argtypes = [C, I32, I32, F, R, P, P, P, P, P, ctypes.c_size_t, P]
+    L.kvpop_cache_attn.restype = ctypes.c_int
+    L.kvpop_retain_prompt.argtypes = [S, I32, P, P, P, P, P]
+    L.kvpop_retain_prompt.restype = ctypes.c_int
+    L.kvpop_retain_step.argtypes = [S, P, P, P, I32, I32, I32, P, P]
+    L.kvpop_retain_step.restype = ctypes.c_int
+    L.kvpop_strerror.argtypes = [ctypes.c_int]
+    L.kvpop_strerror.restype = ctypes.c_char_p
 
 
 def kvpop_strerror(status: int) -> str:
