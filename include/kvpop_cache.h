@@ -99,12 +99,13 @@ typedef struct kvpop_append {
  * held[b, h] that it does not write), the page takes the larger of this and its own
  * exponent and their codes move to it; if not, it takes this one. A code is x 2^-e
  * rounded to nearest, ties to even, saturated at qmax; NaN becomes 0 and an infinity
- * the largest code of its sign. Rotation is in 64 bits, so that the code is the one
- * rounding of the value. Slots at or past max_pages * P are not written. A token
- * outside [0, N) or at a position outside [0, n_positions) (with rot_dim > 0) is
- * stored as zeros. Slots that no token uses keep their bytes.
- * q_out[b, h, n, :] = R(pos0[b] + n) q[b, h, n, :] rounded to bf16 (zeros at a position
- * outside the table), for all N tokens.
+ * the largest code of its sign. Keys are rotated in 64 bits, so that the code is the
+ * one rounding of the value. Slots at or past max_pages * P are not written. A token
+ * outside [0, N) is stored as zeros, key and value. At a position outside
+ * [0, n_positions) (with rot_dim > 0) the key is stored as zeros and the value as it is, so
+ * that attention finds the token with a logit of 0. Slots that no token uses keep their bytes.
+ * q_out[b, h, n, :] = R(pos0[b] + n) q[b, h, n, :], rotated in 32 bits and rounded to bf16
+ * (zeros at a position outside the table), for all N tokens.
  * KVPOP_EINVAL: a missing pointer, dimensions or strides out of range, M != N without
  * src, q without q_out, or q_out or the cache over an input or each other.
  * KVPOP_EUNSUPPORTED: head_dim, page_size, format, rot_dim not a multiple of 16,
@@ -125,8 +126,12 @@ int kvpop_cache_append(const kvpop_cache* cache, const kvpop_append* a, void* st
  * into [0, max_pages * P]. Bytes of slots that a query does not see do not matter,
  * except an e4m3 NaN (which kvpop_cache_append never writes) in a slot that another
  * query of the same call sees. Products are of 16-bit operands with fp32 sums: codes
- * are exact there, a query's elements are exact down to 2^-28 of its largest, and
- * probabilities are rounded to 11 bits; the normaliser sums them unrounded.
+ * are exact there, and a query's elements are exact down to 2^-28 of its largest. A
+ * probability times 2^e of its values' page is rounded to 11 bits where it is above 2^-21
+ * of the largest such number of its query, and to 2^-32 of that one below; the
+ * normaliser sums the probabilities unrounded. Logits are fp32: they, and scale |q| 2^e of a
+ * query's largest element and any page's e of keys, have to lie within +-2^125. What a query
+ * with an element that is not finite gets means nothing; the others' results stay the same.
  * q: bf16 [B, Hq, N, D]; o: bf16 [B, Hq, N, D] contiguous; lse: fp32 [B, Hq, N].
  * workspace: kvpop_cache_attn_workspace_size bytes of device memory, 16-byte aligned
  * (may be NULL if that is 0); its contents on entry do not matter. Calls that may run
