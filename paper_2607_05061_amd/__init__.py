@@ -588,11 +588,22 @@ def _rows(torch, x, name: str, B: int, heads, N, D: int, dev: int):
     return (x.data_ptr(), sb if B > 1 else 0, sh if h > 1 else 0, st if n > 1 else 0), h, n
 
 
+def _current(torch, dev: int):
+    """(handle of GPU ``dev``'s current stream, current GPU). torch's own short ways, 0.2 us where the
+    public ones take 1.4; those serve where a version of torch lacks the others."""
+    try:
+        return torch._C._cuda_getCurrentRawStream(dev), torch._C._cuda_getDevice()
+    except AttributeError:
+        return int(torch.cuda.current_stream(dev).cuda_stream), torch.cuda.current_device()
+
+
 def _call(torch, f, dev: int, stream, *args):
     """Calls entry point ``f`` on ``stream`` or the current one of GPU ``dev``, which is made the current
     device: the default stream's handle is that of whichever device is current."""
-    handle = torch._C._cuda_getCurrentRawStream(dev) if stream is None else int(stream.cuda_stream)
-    if dev == torch._C._cuda_getDevice():
+    handle, current = _current(torch, dev)
+    if stream is not None:
+        handle = int(stream.cuda_stream)
+    if dev == current:
         st = f(*args, handle)
     else:
         with torch.cuda.device(dev):
