@@ -124,8 +124,9 @@ __device__ __forceinline__ int split_tiles(int n, int splits, int least) {
 // product for the head dims t, t + D / 16, ...: no value passes through LDS.
 // HBM bounds it: 8 KB of a tile are on their way while one is multiplied. 32 x 8 lists of 16384
 // tokens of 128 dims (1.07 GB) take 185-195 us, 5.5-5.8 TB/s (part of the pool stays in
-// the 256 MB cache), 128 x 8 of 2276 115 us, 5.2 TB/s. Two tiles on their way (172 registers instead
-// of 142): 113 us, but 9.1 instead of 7.6 us for 64 x 8 lists of 100.
+// the 256 MB cache), 128 x 8 of 2276 113-115 us, 5.2 TB/s. For D = 128 the form of 8 waves takes 142
+// registers (3 waves a SIMD), that of 4 waves 140 and 36 accumulator registers (2 waves). Two tiles on
+// their way (172 registers): 113 us, but 9.1 instead of 7.6 us for 64 x 8 lists of 100.
 template <int D, int FMT, int W>
 __global__ __launch_bounds__(64 * W) void cache_attn_kernel(CacheAttnLaunch a, int row_blocks, int splits) {
   constexpr int KS = D / 32;  // k-steps of the logits
@@ -383,12 +384,14 @@ __global__ __launch_bounds__(64 * W) void cache_attn_kernel(CacheAttnLaunch a, i
 // Three tile buffers: while one is multiplied, with the next one's first logits, the one after
 // is widened, and the bytes of the following one are on their way in registers.
 //
-// 1024 queries of 32 heads over 8 lists of 32768 tokens: 0.55-0.60 ms, 900-980 TFLOP/s (36-39%
-// of the dense peak), D = 64 0.36 ms. Matrix cores are busy on 44% of the cycles, the vector ALU
-// (exponential, its argument and sum per pair, the widening) on 57%, LDS on 32%. With the
-// numerators of 64 keys after all their logits, and two buffers: 0.70 ms; with the masks of the last
-// tiles as selects in every block, 0.63 ms; with a maximum per block instead of the sums' test 3-5%
-// more; with a raised priority around the products, the same.
+// 1024 queries of 32 heads over 8 lists of 32768 tokens, a workgroup for each CU: 0.55-0.58 ms, 940-980
+// TFLOP/s (37-39% of the dense peak), D = 64 0.38 ms; other numbers of queries reach 550-810 (the
+// times beside `plan`). Matrix cores are busy on 43% of the cycles, the vector ALU (exponential, its
+// argument and sum per pair, the widening) on 54%, LDS on 31%. With the numerators of 64 keys after
+// all their logits, and two buffers: 0.70 ms; with the masks of the last tiles as selects in every
+// block, 0.63 ms; with a maximum per block instead of the sums' test 3-5% more; with a raised
+// priority around the products, the same. With M moved for all queries of a wave as soon as one asks for it 1-3%
+// less (D = 64 5%), but then what a query gets depends on the others.
 constexpr int kChunkWaves = 8, kChunkThreads = 64 * kChunkWaves, kChunkRows = 32 * kChunkWaves;
 constexpr float kSlack = 12.f;  // how far x may pass M, in powers of two, in a block that a query sees a part of
 
@@ -793,7 +796,10 @@ __global__ __launch_bounds__(256) void cache_attn_join_kernel(CacheAttnLaunch a,
 // 256; the other one reads a list once per 16 rows. Lists of 4096 tokens, (lists, rows), chunk
 // and other: (8, 80) 19.8 and 17.1, (16, 80) 24.1 and 23.5; (32, 48) 24.8 and 25.8, (32, 32)
 // 23.1 and 20.8; (64, 48) 36.6 and 36.6, (128, 48) 57.5 and 69.3, (128, 32) 55.6 and 43.9; of
-// 8192, (8, 96) 26.0 and 28.1. It gets one workgroup per CU, parts of at least 4 tiles.
+// 8192, (8, 96) 26.0 and 28.1. It gets one workgroup per CU, parts of at least 4 tiles. The number
+// of parts is rounded down, so that a call whose workgroups are not a divisor of 256 leaves CUs without
+// work: 32 heads over 8 lists of 32768, 1024 queries (128 workgroups x 2 parts) 559, 2048 1051, 4096 2000,
+// but 700 (88 x 2) 525, 1025 (136) 990, 1536 (192) 998, 2304 (288) 1995; 512 (64 x 4, more to join) 353.
 //
 // The other kernel's time is the lists' bytes. With at most one workgroup per CU it takes 8 waves
 // (lists of 2276 tokens: 256 of them 27.7, 4 waves 32.0; 136 22.6 and 29.8); beyond, as
