@@ -599,7 +599,8 @@ __global__ __attribute__((amdgpu_flat_work_group_size(kChunkThreads, kChunkThrea
       mx = max_pair(mx);
       const bool asks = ((uint32_t)(over | over >> 32) >> col & 1) != 0;  // in either of the query's lanes
       const bool keep = key0 + 32 <= seen && pages && !asks;
-      const float m = !keep && mx > M + kSlack ? mx - kRoom : M, mu = m == neg_inf() ? 0.f : m;
+      // (The difference is exact where it matters; M + kSlack can round to M + 16, whose numerator is infinite.)
+      const float m = !keep && mx - M > kSlack ? mx - kRoom : M, mu = m == neg_inf() ? 0.f : m;
       if (__builtin_amdgcn_ballot_w64(m != M) != 0) {
         const float f = __builtin_amdgcn_exp2f(M - mu);
 #pragma unroll

@@ -107,3 +107,29 @@ def test_logits_of_any_size(D, N, size):
         300 * math.exp(-20) * 254 + 2.0 ** -11
     assert (np.abs(o[0, 0].double().cpu().numpy() - want) <= bound).all()
     assert (np.abs(lse[0, 0].double().cpu().numpy() - top) <= 2.0 ** -21 * top + math.tanh(eps)).all()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("N", [1, 40, 100])
+@pytest.mark.parametrize("size", [17, 18, 19, 20, 21, 22])
+@pytest.mark.parametrize("step", [1, 2, 4])
+def test_large_logits_that_grow(D, N, size, step):
+    """Logits around 127 2^size that grow along the list by steps of what 32 bits tell apart there, so that
+    the reference is behind by each small multiple of that. All values are 100, and so is every answer,
+    whatever the weights."""
+    P, L = 32, 300
+    host = HostCache(np.random.default_rng(D), 1, 1, -(-L // P), P, D, "int8", exps=(0, 0))
+    k = host.side["k"][0].view(np.int8)
+    host.side["v"][0][:] = 100
+    k[:] = 0
+    for j in range(L):
+        k[host.table[0, 0, j // P], j % P, :2] = 127, -127 + 254 * j // L
+    q = np.zeros((1, 1, N, D))
+    q[..., 0], q[..., 1] = 1.0, 2.0 ** -21 * step
+    o, lse = kv.kvpop_cache_attn(bf16(q)[0], host.gpu(), i32([[L]]), 2.0 ** size)
+    # numerators are rounded to 11 bits each, and o to bf16
+    assert ((o.double() - 100).abs() <= 100 * (2.0 ** -8 + 2.0 ** -11)).all()
+    # the largest logit that a query sees, and the log of at most L like it
+    c = -127 + 254 * (L - N + np.arange(N)) // L
+    top = torch.as_tensor((127 + c * q[0, 0, 0, 1]) * 2.0 ** size).cuda()
+    assert ((lse[0, 0].double() - top).abs() <= 2.0 ** -20 * top + math.log(L)).all()
