@@ -384,8 +384,8 @@ __global__ __launch_bounds__(64 * W) void cache_attn_kernel(CacheAttnLaunch a, i
 // Three tile buffers: while one is multiplied, with the next one's first logits, the one after
 // is widened, and the bytes of the following one are on their way in registers.
 //
-// 1024 queries of 32 heads over 8 lists of 32768 tokens, a workgroup for each CU: 0.55-0.58 ms, 940-980
-// TFLOP/s (37-39% of the dense peak), D = 64 0.38 ms; other numbers of queries reach 550-810 (the
+// 1024 queries of 32 heads over 8 lists of 32768 tokens, a workgroup for each CU: 0.55-0.60 ms, 910-980
+// TFLOP/s (36-39% of the dense peak), D = 64 0.38-0.39 ms; other numbers of queries reach 550-810 (the
 // times beside `plan`). Matrix cores are busy on 43% of the cycles, the vector ALU (exponential, its
 // argument and sum per pair, the widening) on 54%, LDS on 31%. With the numerators of 64 keys after
 // all their logits, and two buffers: 0.70 ms; with the masks of the last tiles as selects in every
