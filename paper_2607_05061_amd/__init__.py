@@ -35,6 +35,7 @@ __all__ = [
     "KVPOP_CACHE_INT8", "KVPOP_CACHE_E4M3", "KvpopCache", "KvpopCacheC", "KvpopRowsC", "KvpopAppendC", "KvpopRetainC",
     "kvpop_cache_empty", "kvpop_cache_append", "kvpop_cache_attn", "kvpop_cache_attn_workspace_size",
     "kvpop_retain_prompt", "kvpop_retain_step",
+    "kvpop_cache_mass", "kvpop_mass_prompt", "kvpop_mass_prompt_workspace_size", "kvpop_mass_step",
 ]
 
 KVPOP_OK = 0
@@ -170,6 +171,14 @@ def _set_types(L: ctypes.CDLL):
     L.kvpop_retain_prompt.restype = ctypes.c_int
     L.kvpop_retain_step.argtypes = [S, P, P, P, I32, I32, I32, P, P]
     L.kvpop_retain_step.restype = ctypes.c_int
+    L.kvpop_cache_mass.argtypes = [C, I32, I32, F, R, P, P, P, F, I32, P, P]
+    L.kvpop_cache_mass.restype = ctypes.c_int
+    L.kvpop_mass_prompt.argtypes = [S, I32, I32, P, P, I32, I32, I32, P, ctypes.c_size_t, P]
+    L.kvpop_mass_prompt.restype = ctypes.c_int
+    L.kvpop_mass_prompt_workspace_size.argtypes = [I32, I32, I32, I32]
+    L.kvpop_mass_prompt_workspace_size.restype = ctypes.c_size_t
+    L.kvpop_mass_step.argtypes = [S, P, I32, I32, I32, P, P]
+    L.kvpop_mass_step.restype = ctypes.c_int
     L.kvpop_strerror.argtypes = [ctypes.c_int]
     L.kvpop_strerror.restype = ctypes.c_char_p
 
@@ -612,6 +621,18 @@ def _call(torch, f, dev: int, stream, *args):
         raise KvpopError(st, f.__name__)
 
 
+def _workspace(torch, workspace, need: int, device, stream):
+    """The caller's workspace checked, or one of ``need`` bytes in the memory of the launch's stream (None for 0)."""
+    if workspace is not None:
+        _check_workspace(workspace, need, device)
+    elif need:
+        if stream is None:
+            return torch.empty(need, dtype=torch.uint8, device=device)
+        with _on_launch_stream(stream, device):
+            return torch.empty(need, dtype=torch.uint8, device=device)
+    return workspace
+
+
 def kvpop_cache_append(cache: KvpopCache, k, v, held, count=None, start=None, src=None, q=None, rotary=None,
                        pos0=None, adjacent: bool = False, q_out=None, stream=None):
     """New keys and values into the lists' pages, the keys (and queries) turned by their
@@ -675,15 +696,7 @@ def kvpop_cache_attn(q, cache: KvpopCache, held, scale: float, q_lens=None, o=No
     if lse is None:
         lse = torch.empty((B, Hq, N), dtype=torch.float32, device=q.device)
     need = lib().kvpop_cache_attn_workspace_size(c, Hq, N)
-    if workspace is None:
-        if need:
-            if stream is None:
-                workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
-            else:
-                with _on_launch_stream(stream, q.device):
-                    workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
-    else:
-        _check_workspace(workspace, need, q.device)
+    workspace = _workspace(torch, workspace, need, q.device, stream)
     _call(torch, lib().kvpop_cache_attn, dev, stream, c, Hq, N, float(scale), _ROWS_PACK.pack(*qr),
           _ptr(held, "held", i32, (B, H), dev), _ptr(q_lens, "q_lens", i32, (B,), dev),
           _ptr(o, "o", torch.bfloat16, (B, Hq, N, D), dev), _ptr(lse, "lse", torch.float32, (B, Hq, N), dev),
@@ -736,5 +749,81 @@ def kvpop_retain_step(scores, q_pos, pos, prio, held, sinks: int, window: int, t
     st = _RETAIN_PACK.pack(B, H, S, pos.data_ptr(), _ptr(prio, "prio", f32, shape, dev), _ptr(held, "held", i32, lists, dev))
     _call(torch, lib().kvpop_retain_step, dev, stream, st, _ptr(scores, "scores", f32, lists, dev),
           _ptr(log_gamma, "log_gamma", f32, (H,), dev), _ptr(q_pos, "q_pos", i32, (B,), dev), int(sinks), int(window),
+          int(topk), _ptr(slot, "slot", i32, lists, dev))
+    return slot
+
+
+# ---------------------------------------------------------------------------
+# Eviction by accumulated attention weight (include/kvpop_mass.h)
+# ---------------------------------------------------------------------------
+
+def kvpop_cache_mass(q, cache: KvpopCache, held, lse, scale: float, mass, q_lens=None, decay: float = 1.0, stream=None):
+    """Adds the attention weight that the newest queries give each slot of the lists to ``mass`` (fp32
+    [B, H, slots], updated in place and returned), which is multiplied by ``decay`` first. q, held and
+    q_lens are those of the kvpop_cache_attn call that returned lse (fp32 [B, Hq, N])."""
+    torch = _torch()
+    i32, f32 = torch.int32, torch.float32
+    c, B, H, D, dev = _cache_parts(torch, cache)
+    qr, Hq, N = _rows(torch, q, "q", B, None, None, D, dev)
+    _check_tensor(mass, "mass", f32, q.device)
+    S = mass.shape[2] if mass.dim() == 3 else 0
+    _call(torch, lib().kvpop_cache_mass, dev, stream, c, Hq, N, float(scale), _ROWS_PACK.pack(*qr),
+          _ptr(held, "held", i32, (B, H), dev), _ptr(q_lens, "q_lens", i32, (B,), dev),
+          _ptr(lse, "lse", f32, (B, Hq, N), dev), float(decay), S, _ptr(mass, "mass", f32, (B, H, S), dev))
+    return mass
+
+
+def kvpop_mass_prompt_workspace_size(batch: int, n_heads: int, n_q_heads: int, seq_len: int) -> int:
+    """Bytes of workspace of a kvpop_mass_prompt call with mass [batch, n_q_heads, seq_len]."""
+    return int(lib().kvpop_mass_prompt_workspace_size(batch, n_heads, n_q_heads, seq_len))
+
+
+def kvpop_mass_prompt(mass, n_kv_heads: int, budget: int, sinks: int, window: int, topk: int, lens=None, pos=None,
+                      kept=None, held=None, workspace=None, stream=None):
+    """The tokens that a prompt's end keeps by their masses (fp32 [B, Hq, T], as kvpop_future_attn_target
+    with window 0 returns them): the sinks, the newest ``window`` and of the others the ``topk`` whose
+    masses, summed over the query heads of a KV head, are largest. Returns (pos int32 [B, H, budget],
+    kept fp32 [B, H, budget]: their masses, held int32 [B, H]), ascending positions, then -1 and 0.
+    lens: int32 [B], the prompts' lengths (None: T)."""
+    torch = _torch()
+    i32, f32 = torch.int32, torch.float32
+    _check_tensor(mass, "mass", f32, None)
+    _need(mass.dim() == 3, "mass must be [B, Hq, T]")
+    device, dev = mass.device, mass.get_device()
+    B, Hq, T = mass.shape
+    H, S = int(n_kv_heads), int(budget)
+    _need(H >= 1 and S >= 1, "n_kv_heads and budget must be positive")
+    if pos is None:
+        pos = torch.empty((B, H, S), dtype=i32, device=device)
+    if kept is None:
+        kept = torch.empty((B, H, S), dtype=f32, device=device)
+    if held is None:
+        held = torch.empty((B, H), dtype=i32, device=device)
+    st = _RETAIN_PACK.pack(B, H, S, _ptr(pos, "pos", i32, (B, H, S), dev), _ptr(kept, "kept", f32, (B, H, S), dev),
+                           _ptr(held, "held", i32, (B, H), dev))
+    need = lib().kvpop_mass_prompt_workspace_size(B, H, Hq, T)
+    workspace = _workspace(torch, workspace, need, device, stream)
+    _call(torch, lib().kvpop_mass_prompt, dev, stream, st, T, Hq, mass.data_ptr(), _ptr(lens, "lens", i32, (B,), dev),
+          int(sinks), int(window), int(topk), workspace.data_ptr() if workspace is not None else 0, need)
+    return pos, kept, held
+
+
+def kvpop_mass_step(q_pos, pos, mass, held, sinks: int, window: int, topk: int, slot=None, stream=None):
+    """Which slot (int32 [B, H], -1 for none) the token at q_pos (int32 [B], negative for an idle
+    sequence) takes in each list of at most sinks + window + topk tokens: a free one, or that of the
+    token of least mass that is neither a sink nor one of the last ``window``. Updates pos, mass
+    ([B, H, S]) and held ([B, H]) in place; the new token's mass is 0."""
+    torch = _torch()
+    i32, f32 = torch.int32, torch.float32
+    _check_tensor(pos, "pos", i32, None)
+    shape = pos.shape
+    _need(len(shape) == 3, "pos must be [B, H, S]")
+    dev = pos.get_device()
+    B, H, S = shape
+    lists = (B, H)
+    if slot is None:
+        slot = torch.empty(lists, dtype=i32, device=pos.device)
+    st = _RETAIN_PACK.pack(B, H, S, pos.data_ptr(), _ptr(mass, "mass", f32, shape, dev), _ptr(held, "held", i32, lists, dev))
+    _call(torch, lib().kvpop_mass_step, dev, stream, st, _ptr(q_pos, "q_pos", i32, (B,), dev), int(sinks), int(window),
           int(topk), _ptr(slot, "slot", i32, lists, dev))
     return slot

@@ -1,8 +1,9 @@
 // C ABI of the KVpop future-attention target library: argument validation, error
 // reporting and dispatch to the gfx950 kernels. The semantics of every entry point
-// are specified in include/kvpop.h and include/kvpop_cache.h.
+// are specified in include/kvpop.h, include/kvpop_cache.h and include/kvpop_mass.h.
 #include "kvpop.h"
 #include "kvpop_cache.h"
+#include "kvpop_mass.h"
 
 #include <hip/hip_runtime_api.h>
 
@@ -275,6 +276,14 @@ kvpop::RetainLaunch make_retain(const kvpop_retain* s, const float* scores, cons
   L.log_gamma = log_gamma;
   L.stream = stream;
   return L;
+}
+
+// Sizes of a prompt's masses [B, Hq, T] (*rows of them).
+int check_mass_prompt_dims(int64_t B, int64_t H, int64_t Hq, int64_t T, int64_t* rows) {
+  if (B < 1 || H < 1 || Hq < 1 || T < 1 || Hq % H != 0) return KVPOP_EINVAL;
+  if (T > KVPOP_MAX_SEQ_LEN) return KVPOP_EUNSUPPORTED;
+  if (!mul_ok(B * Hq, T, rows) || *rows > INT64_MAX / 16) return KVPOP_EINVAL;
+  return KVPOP_OK;
 }
 
 }  // namespace
@@ -654,6 +663,109 @@ int kvpop_retain_step(const kvpop_retain* s, const float* scores, const float* l
   L.slot = slot;
   if (kvpop::retain_step_threads(L) > UINT32_MAX) return KVPOP_EUNSUPPORTED;
   return launch([&] { return kvpop::launch_retain_step(L); });
+}
+
+int kvpop_cache_mass(const kvpop_cache* cache, int32_t n_q_heads, int32_t n_tokens, float scale, const kvpop_rows* q,
+                     const int32_t* held, const int32_t* q_lens, const float* lse, float decay, int32_t n_slots,
+                     float* mass, void* stream) {
+  kvpop::CacheAttnLaunch dims;
+  int st = check_cache_attn_dims(cache, n_q_heads, n_tokens, &dims);
+  if (st != KVPOP_OK) return st;
+  if ((st = check_cache(cache)) != KVPOP_OK) return st;
+  if (!q || !held || !lse || !mass || n_slots < 1 || !std::isfinite(scale) || !(scale > 0.f) || !(decay >= 0.f && decay <= 1.f))
+    return KVPOP_EINVAL;
+  if (n_slots > KVPOP_MAX_SEQ_LEN) return KVPOP_EUNSUPPORTED;
+  int64_t qb;
+  if ((st = check_rows(*q, cache->batch, n_q_heads, n_tokens, cache->head_dim, &qb)) != KVPOP_OK) return st;
+  if (!aligned4(mass) || !aligned4(lse) || !aligned4(held) || !aligned4(q_lens)) return KVPOP_EUNSUPPORTED;
+  const int64_t rows = (int64_t)cache->batch * n_q_heads * n_tokens, lists = cache_lists(cache);
+  const Span outs[] = {{mass, lists * n_slots * 4}};
+  const Span ins[] = {{q->ptr, qb}, {held, lists * 4}, {q_lens, (int64_t)cache->batch * 4}, {lse, rows * 4},
+                      {cache->k_pages, pool_bytes(cache)}, {cache->k_exp, cache->n_pages},
+                      {cache->page_table, lists * cache->max_pages * 4}};
+  if (!disjoint(outs, ins)) return KVPOP_EINVAL;
+  kvpop::CacheMassLaunch L{};
+  L.c = dims.c;
+  L.q = make_rows(*q);
+  L.held = held;
+  L.q_lens = q_lens;
+  L.lse = lse;
+  L.mass = mass;
+  L.Hq = n_q_heads;
+  L.N = n_tokens;
+  L.S = n_slots;
+  L.scale = scale;
+  L.decay = decay;
+  L.stream = stream;
+  if (kvpop::cache_mass_threads(L) > UINT32_MAX) return KVPOP_EUNSUPPORTED;
+  return launch([&] { return kvpop::launch_cache_mass(L); });
+}
+
+size_t kvpop_mass_prompt_workspace_size(int32_t batch, int32_t n_heads, int32_t n_q_heads, int32_t seq_len) {
+  int64_t rows;
+  if (check_mass_prompt_dims(batch, n_heads, n_q_heads, seq_len, &rows) != KVPOP_OK) return 0;
+  return (size_t)kvpop::mass_prompt_workspace_floats(batch, n_heads, n_q_heads, seq_len) * 4;
+}
+
+int kvpop_mass_prompt(const kvpop_retain* s, int32_t seq_len, int32_t n_q_heads, const float* mass,
+                      const int32_t* lens, int32_t sinks, int32_t window, int32_t topk, void* workspace,
+                      size_t workspace_bytes, void* stream) {
+  int st = check_retain(s);
+  if (st != KVPOP_OK) return st;
+  int64_t rows;
+  if ((st = check_mass_prompt_dims(s->batch, s->n_heads, n_q_heads, seq_len, &rows)) != KVPOP_OK) return st;
+  if (!mass || sinks < 0 || window < 0 || topk < 1 || (int64_t)sinks + window + topk > s->slots) return KVPOP_EINVAL;
+  if (!aligned4(mass) || !aligned4(lens)) return KVPOP_EUNSUPPORTED;
+  const int64_t need = kvpop::mass_prompt_workspace_floats(s->batch, s->n_heads, n_q_heads, seq_len) * 4;
+  if (need > 0) {
+    if (!workspace || workspace_bytes < (size_t)need) return KVPOP_EINVAL;
+    if (!aligned16(workspace)) return KVPOP_EUNSUPPORTED;
+  }
+  const int64_t lists = (int64_t)s->batch * s->n_heads;
+  const Span outs[] = {{s->pos, lists * s->slots * 4}, {s->prio, lists * s->slots * 4}, {s->held, lists * 4},
+                       {need ? workspace : nullptr, need}};
+  const Span ins[] = {{mass, rows * 4}, {lens, (int64_t)s->batch * 4}};
+  if (!disjoint(outs, ins)) return KVPOP_EINVAL;
+  kvpop::MassPromptLaunch L{};
+  L.B = s->batch;
+  L.H = s->n_heads;
+  L.Hq = n_q_heads;
+  L.T = seq_len;
+  L.S = s->slots;
+  L.mass = mass;
+  L.lens = lens;
+  L.workspace = static_cast<float*>(workspace);
+  L.pos = s->pos;
+  L.prio = s->prio;
+  L.held = s->held;
+  L.sinks = sinks;
+  L.window = window;
+  L.topk = topk;
+  L.stream = stream;
+  if (kvpop::mass_prompt_threads(L) > UINT32_MAX) return KVPOP_EUNSUPPORTED;
+  return launch([&] { return kvpop::launch_mass_prompt(L); });
+}
+
+int kvpop_mass_step(const kvpop_retain* s, const int32_t* q_pos, int32_t sinks, int32_t window, int32_t topk,
+                    int32_t* slot, void* stream) {
+  int st = check_retain(s);
+  if (st != KVPOP_OK) return st;
+  if (!q_pos || !slot || sinks < 0 || window < 0 || topk < 1) return KVPOP_EINVAL;
+  if ((int64_t)sinks + window + topk > s->slots) return KVPOP_EINVAL;
+  if (!aligned4(q_pos) || !aligned4(slot)) return KVPOP_EUNSUPPORTED;
+  const int64_t lists = (int64_t)s->batch * s->n_heads;
+  const Span outs[] = {{s->pos, lists * s->slots * 4}, {s->prio, lists * s->slots * 4}, {s->held, lists * 4},
+                       {slot, lists * 4}};
+  const Span ins[] = {{q_pos, (int64_t)s->batch * 4}};
+  if (!disjoint(outs, ins)) return KVPOP_EINVAL;
+  kvpop::RetainLaunch L = make_retain(s, nullptr, nullptr, stream);
+  L.q_pos = q_pos;
+  L.sinks = sinks;
+  L.window = window;
+  L.topk = topk;
+  L.slot = slot;
+  if (kvpop::mass_step_threads(L) > UINT32_MAX) return KVPOP_EUNSUPPORTED;
+  return launch([&] { return kvpop::launch_mass_step(L); });
 }
 
 }  // extern "C"

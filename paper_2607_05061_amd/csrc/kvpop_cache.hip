@@ -6,20 +6,16 @@
 #include <stdint.h>
 
 #include "kvpop_cache.h"
+#include "kvpop_cache_codes.h"
 #include "kvpop_internal.h"
 
 namespace kvpop {
 namespace {
 
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef float f32x8 __attribute__((ext_vector_type(8)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
-constexpr int kExpMin = -32, kExpMax = 32;
 
-__device__ __forceinline__ int clampi(int x, int lo, int hi) { return min(max(x, lo), hi); }
 
 __device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
@@ -447,13 +443,6 @@ int launch_append(const AppendLaunch& L) {
 // ---------------------------------------------------------------------------
 // Retention
 // ---------------------------------------------------------------------------
-
-// The order of kvpop_running_topk: larger keys are lower priorities, -0 = +0.
-__device__ __forceinline__ uint32_t desc_key(float f) {
-  uint32_t u = __float_as_uint(f);
-  if (u == 0x80000000u) u = 0u;
-  return (u & 0x80000000u) ? u : ~(u | 0x80000000u);
-}
 
 // fl(r - fl(t * lg)): two roundings, never fused.
 __device__ __forceinline__ float static_priority(float r, float t, float lg) {

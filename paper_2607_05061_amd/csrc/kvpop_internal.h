@@ -115,6 +115,39 @@ struct RetainLaunch {
   void* stream;
 };
 
+// Eviction by accumulated attention weight (kvpop_mass.hip).
+struct CacheMassLaunch {
+  CacheView c;              // keys only
+  Rows q;
+  const int32_t *held, *q_lens;
+  const float* lse;         // [B, Hq, N]
+  float* mass;              // [B, H, S]
+  int32_t Hq, N, S;
+  float scale, decay;
+  void* stream;
+};
+
+struct MassPromptLaunch {
+  int32_t B, H, Hq, T, S;
+  const float* mass;        // [B, Hq, T]
+  const int32_t* lens;      // [B] or nullptr
+  const float* sums;        // [B, H, T]: mass itself or workspace
+  float* workspace;
+  int32_t* pos;             // [B, H, S]
+  float* prio;              // [B, H, S]
+  int32_t* held;            // [B, H]
+  int32_t sinks, window, topk;
+  void* stream;
+};
+
+int launch_cache_mass(const CacheMassLaunch& L);
+int launch_mass_prompt(const MassPromptLaunch& L);
+int launch_mass_step(const RetainLaunch& L);
+int64_t cache_mass_threads(const CacheMassLaunch& L);
+int64_t mass_prompt_threads(const MassPromptLaunch& L);
+int64_t mass_step_threads(const RetainLaunch& L);
+int64_t mass_prompt_workspace_floats(int64_t B, int64_t H, int64_t Hq, int64_t T);
+
 int launch_cache_append(const AppendLaunch& L);
 int launch_cache_attn(const CacheAttnLaunch& L);
 int launch_retain_prompt(const RetainLaunch& L);

@@ -1,0 +1,139 @@
+"""Eviction by accumulated attention weight: what the header declares is exported, bad arguments are rejected
+with the documented status before anything is launched (no GPU; the device addresses are fake), and the oracle is
+pinned by hand."""
+import ctypes
+import math
+import os
+import re
+
+import numpy as np
+import pytest
+
+import paper_2607_05061_amd as kv
+from oracle import mass as om
+
+HEADER = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "kvpop_mass.h")
+built = pytest.mark.skipif(not os.path.exists(kv.lib_path()),
+                           reason="libkvpop.so not built (python -m paper_2607_05061_amd.build)")
+EINVAL, EUNS = kv.KVPOP_EINVAL, kv.KVPOP_EUNSUPPORTED
+GB = 1 << 30
+
+
+def cache(B=2, H=2, D=128, fmt=0, P=64, n=40, per=4, k=1 * GB, v=2 * GB, ke=3 * GB, ve=4 * GB, table=5 * GB):
+    return kv.KvpopCacheC(B, H, D, fmt, P, n, per, k, v, ke, ve, table)
+
+
+def rows(ptr, sb=10240, sh=1280, st=128):
+    return kv.KvpopRowsC(ptr, sb, sh, st)
+
+
+def add(c=None, Hq=4, N=3, scale=0.1, q=None, held=8 * GB, lens=None, lse=9 * GB, decay=1.0, S=256, mass=10 * GB):
+    q = rows(6 * GB) if q is None else q
+    return kv.lib().kvpop_cache_mass(ctypes.byref(c or cache()), Hq, N, scale, ctypes.byref(q), held, lens, lse, decay, S, mass, None)
+
+
+def retained(B=2, H=2, S=20, pos=1 * GB, prio=2 * GB, held=3 * GB):
+    return kv.KvpopRetainC(B, H, S, pos, prio, held)
+
+
+def prompt(s=None, T=50, Hq=4, mass=4 * GB, lens=None, sinks=2, w=3, k=15, ws=5 * GB, size=None):
+    s = s or retained()
+    size = kv.kvpop_mass_prompt_workspace_size(s.batch, s.n_heads, Hq, T) if size is None else size
+    return kv.lib().kvpop_mass_prompt(ctypes.byref(s), T, Hq, mass, lens, sinks, w, k, ws, size, None)
+
+
+def step(s=None, q=4 * GB, sinks=2, w=3, k=15, slot=5 * GB):
+    return kv.lib().kvpop_mass_step(ctypes.byref(s or retained()), q, sinks, w, k, slot, None)
+
+
+@built
+def test_declared_functions_are_exported():
+    src = re.sub(r"/\*.*?\*/", "", open(HEADER).read(), flags=re.S)
+    names = set(re.findall(r"^\s*(?:int|size_t)\s+(kvpop_\w+)\s*\(", src, flags=re.M))
+    assert names == {"kvpop_cache_mass", "kvpop_mass_prompt", "kvpop_mass_prompt_workspace_size", "kvpop_mass_step"}
+    for n in names:
+        assert ctypes.cast(getattr(kv.lib(), n), ctypes.c_void_p).value
+        assert n in kv.__all__
+
+
+@built
+def test_mass_checks():
+    for kw in (dict(B=0), dict(H=0), dict(D=0), dict(P=0), dict(n=0), dict(per=0), dict(k=None), dict(table=None)):
+        assert add(cache(**kw)) == EINVAL, kw
+    for kw in (dict(D=96), dict(P=8), dict(fmt=2), dict(per=(1 << 24) // 64 + 1), dict(k=GB + 8), dict(table=5 * GB + 2)):
+        assert add(cache(**kw)) == EUNS, kw
+    for kw in (dict(Hq=0), dict(Hq=3), dict(N=0), dict(scale=0.0), dict(scale=math.inf), dict(scale=math.nan), dict(q=rows(None)),
+               dict(held=None), dict(lse=None), dict(mass=None), dict(S=0), dict(S=-1), dict(decay=-0.1), dict(decay=1.1),
+               dict(decay=math.nan), dict(q=rows(6 * GB, sh=-8)), dict(mass=9 * GB), dict(mass=8 * GB), dict(mass=6 * GB),
+               dict(mass=1 * GB + 4096), dict(mass=5 * GB), dict(mass=3 * GB)):
+        assert add(**kw) == EINVAL, kw
+    for kw in (dict(q=rows(6 * GB + 2)), dict(q=rows(6 * GB, st=12)), dict(lse=9 * GB + 2), dict(mass=10 * GB + 1),
+               dict(held=8 * GB + 1), dict(lens=12 * GB + 2), dict(Hq=2 * 1025), dict(N=(1 << 24) + 1), dict(S=(1 << 24) + 1)):
+        assert add(**kw) == EUNS, kw
+    big = cache(B=1 << 14, H=1 << 14, per=1, table=1000 * GB)
+    assert add(big, Hq=1 << 14, held=10000 * GB, lse=20000 * GB, mass=30000 * GB, S=1 << 10) == EUNS  # more threads than a launch takes
+
+
+@built
+def test_prompt_and_step_checks():
+    for call in (prompt, step):
+        for kw in (dict(B=0), dict(H=0), dict(S=0), dict(pos=None), dict(prio=None), dict(held=None), dict(prio=1 * GB + 64),
+                   dict(held=2 * GB + 64)):
+            assert call(retained(**kw)) == EINVAL, kw
+        for kw in (dict(pos=GB + 2), dict(prio=2 * GB + 1), dict(held=3 * GB + 2), dict(S=(1 << 24) + 1)):
+            assert call(retained(**kw)) == EUNS, kw
+        for kw in (dict(sinks=-1), dict(w=-1), dict(k=0), dict(k=16), dict(sinks=2 ** 31 - 1, w=2 ** 31 - 1, k=2 ** 31 - 1)):
+            assert call(**kw) == EINVAL, kw
+    for kw in (dict(T=0), dict(Hq=0), dict(Hq=3), dict(mass=None), dict(mass=2 * GB), dict(ws=None), dict(size=0), dict(ws=4 * GB),
+               dict(ws=1 * GB)):
+        assert prompt(**kw) == EINVAL, kw
+    for kw in (dict(T=(1 << 24) + 1), dict(mass=4 * GB + 2), dict(lens=8 * GB + 1), dict(ws=5 * GB + 8)):
+        assert prompt(**kw) == EUNS, kw
+    assert kv.kvpop_mass_prompt_workspace_size(2, 2, 4, 50) == 2 * 2 * 50 * 4
+    assert kv.kvpop_mass_prompt_workspace_size(2, 2, 2, 50) == 0
+    assert kv.kvpop_mass_prompt_workspace_size(0, 2, 4, 50) == kv.kvpop_mass_prompt_workspace_size(2, 2, 3, 50) == 0
+    for kw in (dict(q=None), dict(slot=None), dict(slot=4 * GB), dict(slot=3 * GB), dict(q=1 * GB)):
+        assert step(**kw) == EINVAL, kw
+    for kw in (dict(q=4 * GB + 2), dict(slot=5 * GB + 2)):
+        assert step(**kw) == EUNS, kw
+    many = retained(B=1 << 15, H=1 << 15, pos=1 * GB, prio=1000000 * GB, held=2000000 * GB)
+    assert step(many, q=3000000 * GB, slot=4000000 * GB) == EUNS
+
+
+@built
+def test_forced_hip_error(monkeypatch):
+    monkeypatch.setenv("KVPOP_TEST_FORCE_EHIP", "719")
+    for call in (add, prompt, step):
+        assert call() == kv.KVPOP_EHIP
+    assert add(N=0) == EINVAL
+
+
+@built
+def test_binding_refuses_what_the_library_cannot_see():
+    torch = pytest.importorskip("torch")
+    c = kv.kvpop_cache_empty(1, 2, 100, 64, 32, device="cpu")
+    with pytest.raises(ValueError, match="GPU"):
+        kv.kvpop_cache_mass(torch.zeros(1, 2, 1, 64, dtype=torch.bfloat16), c, torch.zeros(1, 2, dtype=torch.int32),
+                            torch.zeros(1, 2, 1), 0.1, torch.zeros(1, 2, 100))
+    with pytest.raises(ValueError, match="GPU"):
+        kv.kvpop_mass_prompt(torch.zeros(1, 2, 8), 1, 4, 1, 1, 2)
+    with pytest.raises(ValueError, match="GPU"):
+        kv.kvpop_mass_step(torch.zeros(1, dtype=torch.int32), torch.zeros(1, 1, 4, dtype=torch.int32), torch.zeros(1, 1, 4),
+                           torch.zeros(1, 1, dtype=torch.int32), 1, 1, 1)
+
+
+def test_oracle_by_hand():
+    assert om.prompt_keeps(np.float32([5, 1, 9, 3, 3, 3, 0, 2]), 1, 2, 2) == [0, 2, 3, 6, 7]
+    assert om.prompt_keeps(np.float32([1, 2]), 4, 3, 1) == [0, 1]
+    assert om.prompt_keeps(np.float32([1, -0.0, 0.0, np.nan, np.inf]), 0, 0, 3) == [0, 3, 4]
+    assert om.prompt_keeps(np.float32([-0.0, 0.0, 0.0]), 0, 0, 1) == [0]
+    st = {}
+    assert [om.step(st, q, 1, 1, 1) for q in range(3)] == [0, 1, 2]
+    st[1][1], st[2][1] = np.float32(0.5), np.float32(0.25)
+    assert om.step(st, 3, 1, 1, 1) == 2 and st[2][0] == 3      # position 2 has left the window and the least mass
+    assert om.step(st, 4, 1, 1, 1) == 2                        # 3 with mass 0 beats 1 with 0.5
+    assert om.step(st, -1, 1, 1, 1) == -1
+    k = np.eye(2)
+    got = om.add_mass(np.array([1.0, 1.0]), np.array([[0.0, 0.0]]), k, np.array([[True, False]]), np.array([math.log(2)]), 1.0, 0.5)
+    np.testing.assert_allclose(got, [1.0, 0.5])
+    np.testing.assert_array_equal(om.group_mass(np.float32([[1, 2 ** 25], [2 ** -30, 1]])), np.float32([1, 2 ** 25]))
