@@ -67,7 +67,7 @@ typedef struct kvpop_mlstm_state {
  * > 0, strides < 0, too small a workspace, or an output over an input or another one.
  * KVPOP_EUNSUPPORTED: head_dim, strides of q, k, v not multiples of 8, alignment (q, k, v, o, C, z
  * 16 bytes, the others that of their type), T > KVPOP_MAX_SEQ_LEN, or more than a launch takes
- * (2^32 - 1 threads; 256 per head and 64 tokens). */
+ * (2^32 - 1 threads; 1024 per head and 64 tokens). */
 int kvpop_mlstm_fwd(const kvpop_mlstm* a, const kvpop_mlstm_state* state, void* o, float* lse, void* workspace,
                     size_t workspace_bytes, void* stream);
 size_t kvpop_mlstm_fwd_workspace_size(const kvpop_mlstm* a);

@@ -29,12 +29,12 @@ count normalisation, App. B.1-B.2) is in ``oracle.target``.
 
 The compact cache of a served model (8-bit pages, append, attention over page lists,
 retention one token at a time) is in ``oracle.compact_cache``; eviction by accumulated
-attention weight in ``oracle.mass``.
+attention weight in ``oracle.mass``; the mLSTM scorer's recurrence in ``oracle.mlstm``.
 
 Every function here is pinned by tests against closed forms, hand enumeration and
 brute force (tests/test_oracle_pins.py, tests/test_oracle_*.py); no function is "parity unpinned".
 """
-from . import compact_cache, mass  # noqa: F401
+from . import compact_cache, mass, mlstm  # noqa: F401
 from .future_mass import (  # noqa: F401
     bf16_bits_to_f64,
     causal_logits,

@@ -36,6 +36,8 @@ __all__ = [
     "kvpop_cache_empty", "kvpop_cache_append", "kvpop_cache_attn", "kvpop_cache_attn_workspace_size",
     "kvpop_retain_prompt", "kvpop_retain_step",
     "kvpop_cache_mass", "kvpop_mass_prompt", "kvpop_mass_prompt_workspace_size", "kvpop_mass_step",
+    "KvpopMlstmC", "KvpopMlstmStateC", "KvpopMlstmGradsC", "KvpopMlstmState", "kvpop_mlstm_empty", "kvpop_mlstm_fwd",
+    "kvpop_mlstm_fwd_workspace_size", "kvpop_mlstm_bwd", "kvpop_mlstm_bwd_workspace_size", "kvpop_mlstm_step", "kvpop_mlstm",
 ]
 
 KVPOP_OK = 0
@@ -98,6 +100,26 @@ class KvpopRetainC(ctypes.Structure):
     """Mirror of ``kvpop_retain`` in include/kvpop_cache.h."""
     _fields_ = [("batch", ctypes.c_int32), ("n_heads", ctypes.c_int32), ("slots", ctypes.c_int32),
                 ("pos", ctypes.c_void_p), ("prio", ctypes.c_void_p), ("held", ctypes.c_void_p)]
+
+
+class KvpopMlstmC(ctypes.Structure):
+    """Mirror of ``kvpop_mlstm`` in include/kvpop_mlstm.h."""
+
+    _fields_ = [(n, ctypes.c_int32) for n in ("batch", "n_heads", "seq_len", "head_dim", "delay", "normalize")]
+    _fields_ += [("scale", ctypes.c_float)] + [(n, KvpopRowsC) for n in ("q", "k", "v", "ig", "fg")]
+    _fields_ += [("lens", ctypes.c_void_p)]
+
+
+class KvpopMlstmStateC(ctypes.Structure):
+    """Mirror of ``kvpop_mlstm_state`` in include/kvpop_mlstm.h."""
+
+    _fields_ = [(n, ctypes.c_void_p) for n in ("C", "z", "m")]
+
+
+class KvpopMlstmGradsC(ctypes.Structure):
+    """Mirror of ``kvpop_mlstm_grads`` in include/kvpop_mlstm.h."""
+
+    _fields_ = [(n, ctypes.c_void_p) for n in ("dq", "dk", "dv", "dig", "dfg")]
 
 
 class KvpopError(RuntimeError):
@@ -179,6 +201,17 @@ def _set_types(L: ctypes.CDLL):
     L.kvpop_mass_prompt_workspace_size.restype = ctypes.c_size_t
     L.kvpop_mass_step.argtypes = [S, P, I32, I32, I32, P, P]
     L.kvpop_mass_step.restype = ctypes.c_int
+    M = P
+    L.kvpop_mlstm_fwd.argtypes = [M, P, P, P, P, ctypes.c_size_t, P]
+    L.kvpop_mlstm_fwd.restype = ctypes.c_int
+    L.kvpop_mlstm_fwd_workspace_size.argtypes = [M]
+    L.kvpop_mlstm_fwd_workspace_size.restype = ctypes.c_size_t
+    L.kvpop_mlstm_bwd.argtypes = [M, R, P, P, P, P, ctypes.c_size_t, P]
+    L.kvpop_mlstm_bwd.restype = ctypes.c_int
+    L.kvpop_mlstm_bwd_workspace_size.argtypes = [M]
+    L.kvpop_mlstm_bwd_workspace_size.restype = ctypes.c_size_t
+    L.kvpop_mlstm_step.argtypes = [M, P, P, P]
+    L.kvpop_mlstm_step.restype = ctypes.c_int
     L.kvpop_strerror.argtypes = [ctypes.c_int]
     L.kvpop_strerror.restype = ctypes.c_char_p
 
@@ -535,6 +568,9 @@ _CACHE_PACK = struct.Struct("7i4x5P")
 _ROWS_PACK = struct.Struct("P3q")
 _APPEND_PACK = struct.Struct("2i P3q P3q 7P 4i P3q P")
 _RETAIN_PACK = struct.Struct("3i4x3P")
+_MLSTM_PACK = struct.Struct("6if4x P3q P3q P3q P3q P3q P")
+_THREE_PACK = struct.Struct("3P")
+_FIVE_PACK = struct.Struct("5P")
 
 
 def _need(ok: bool, text: str):
@@ -827,3 +863,174 @@ def kvpop_mass_step(q_pos, pos, mass, held, sinks: int, window: int, topk: int, 
     _call(torch, lib().kvpop_mass_step, dev, stream, st, _ptr(q_pos, "q_pos", i32, (B,), dev), int(sinks), int(window),
           int(topk), _ptr(slot, "slot", i32, lists, dev))
     return slot
+
+
+# ---------------------------------------------------------------------------
+# The mLSTM scorer's recurrence (include/kvpop_mlstm.h)
+# ---------------------------------------------------------------------------
+
+class KvpopMlstmState(NamedTuple):
+    """What the recurrence holds of B sequences of H heads, divided by e ** m: C fp32 [B, H, D, D], z fp32
+    [B, H, D], m fp32 [B, H]."""
+    C: Any
+    z: Any
+    m: Any
+
+
+def kvpop_mlstm_empty(batch: int, n_heads: int, head_dim: int, device="cuda") -> KvpopMlstmState:
+    """Nothing held."""
+    torch = _torch()
+    _need(batch >= 1 and n_heads >= 1, "batch and n_heads must be positive")
+    _need(head_dim in (64, 128), "head_dim must be 64 or 128")
+    f32 = dict(dtype=torch.float32, device=device)
+    return KvpopMlstmState(torch.zeros((batch, n_heads, head_dim, head_dim), **f32), torch.zeros((batch, n_heads, head_dim), **f32),
+                           torch.full((batch, n_heads), float("-inf"), **f32))
+
+
+def _gate(torch, x, name: str, B: int, H: int, T: int, dev: int):
+    """A bf16 tensor [B, H, T] of any strides: (address, strides)."""
+    if not isinstance(x, torch.Tensor):
+        raise TypeError("%s must be a torch.Tensor" % name)
+    if x.get_device() != dev:
+        raise ValueError("%s must be on the GPU device of q" % name)
+    if x.dtype is not torch.bfloat16:
+        raise TypeError("%s must be %s, got %s" % (name, torch.bfloat16, x.dtype))
+    if tuple(x.shape) != (B, H, T):
+        raise ValueError("%s must be [B, H, T] = %s, got %s" % (name, [B, H, T], list(x.shape)))
+    sb, sh, st = x.stride()
+    return x.data_ptr(), sb if B > 1 else 0, sh if H > 1 else 0, st if T > 1 else 0
+
+
+def _mlstm_parts(torch, q, k, v, ig, fg, scale, delay, normalize, lens):
+    """The call's arrays checked: (packed kvpop_mlstm, B, H, T, D, GPU index)."""
+    _need(isinstance(q, torch.Tensor) and q.dim() == 4, "q must be a tensor [B, H, T, D]")
+    B, H, T, D = q.shape
+    _need(min(B, H, T) >= 1, "q must not be empty")
+    if not q.is_cuda:
+        raise ValueError("q must be on a GPU device")
+    dev = q.get_device()
+    rows = [x for n, t in (("q", q), ("k", k), ("v", v)) for x in _rows(torch, t, n, B, H, T, D, dev)[0]]
+    gates = [x for n, t in (("ig", ig), ("fg", fg)) for x in _gate(torch, t, n, B, H, T, dev)]
+    return _MLSTM_PACK.pack(B, H, T, D, int(delay), 1 if normalize else 0, float(scale), *rows, *gates,
+                            _ptr(lens, "lens", torch.int32, (B,), dev)), B, H, T, D, dev
+
+
+def _state_ptrs(torch, state, B, H, D, dev):
+    if state is None:
+        return None
+    C, z, m = state
+    f32 = torch.float32
+    _need(C is not None and z is not None and m is not None, "a state has C, z and m")
+    return _THREE_PACK.pack(_ptr(C, "C", f32, (B, H, D, D), dev), _ptr(z, "z", f32, (B, H, D), dev), _ptr(m, "m", f32, (B, H), dev))
+
+
+def kvpop_mlstm_fwd_workspace_size(batch: int, n_heads: int, seq_len: int, head_dim: int) -> int:
+    """Bytes of workspace of a kvpop_mlstm_fwd call with q [batch, n_heads, seq_len, head_dim]."""
+    a = _MLSTM_PACK.pack(batch, n_heads, seq_len, head_dim, 0, 1, 1.0, *([0] * 21))
+    return int(lib().kvpop_mlstm_fwd_workspace_size(a))
+
+
+def kvpop_mlstm_bwd_workspace_size(batch: int, n_heads: int, seq_len: int, head_dim: int) -> int:
+    """Bytes of workspace of a kvpop_mlstm_bwd call with q [batch, n_heads, seq_len, head_dim]."""
+    a = _MLSTM_PACK.pack(batch, n_heads, seq_len, head_dim, 0, 1, 1.0, *([0] * 21))
+    return int(lib().kvpop_mlstm_bwd_workspace_size(a))
+
+
+def kvpop_mlstm_fwd(q, k, v, ig, fg, scale: float = 1.0, delay: int = 0, normalize: bool = True, lens=None, state=None,
+                    o=None, lse=None, workspace=None, stream=None):
+    """The read-outs of the delayed mLSTM scorer (App. E.3-E.5): query t reads what is held when token t +
+    ``delay`` has come, C <- sigmoid(fg) C + exp(ig) k v^T and z alike, as (q C) / (q . z), or q C with
+    ``normalize`` off. q, k, v: bf16 [B, H, T, D], D 64 or 128 (strides that are multiples of 8, last
+    dimension contiguous); ig, fg: bf16 [B, H, T] of any strides; lens: int32 [B], the sequences' lengths
+    (None: T); state: a KvpopMlstmState, updated in place (None: nothing is held before). Returns
+    (o bf16 [B, H, T, D], lse fp32 [B, H, T]: the normaliser's logarithm); rows that are not read get
+    0 and -inf."""
+    torch = _torch()
+    a, B, H, T, D, dev = _mlstm_parts(torch, q, k, v, ig, fg, scale, delay, normalize, lens)
+    st = _state_ptrs(torch, state, B, H, D, dev)
+    if o is None:
+        o = torch.empty((B, H, T, D), dtype=torch.bfloat16, device=q.device)
+    if lse is None:
+        lse = torch.empty((B, H, T), dtype=torch.float32, device=q.device)
+    need = lib().kvpop_mlstm_fwd_workspace_size(a)
+    workspace = _workspace(torch, workspace, need, q.device, stream)
+    _call(torch, lib().kvpop_mlstm_fwd, dev, stream, a, st, _ptr(o, "o", torch.bfloat16, (B, H, T, D), dev),
+          _ptr(lse, "lse", torch.float32, (B, H, T), dev), workspace.data_ptr() if workspace is not None else 0, need)
+    return o, lse
+
+
+def kvpop_mlstm_bwd(do, q, k, v, ig, fg, o, lse, scale: float = 1.0, delay: int = 0, normalize: bool = True, lens=None,
+                    grads=None, workspace=None, stream=None):
+    """The gradients (dq, dk, dv bf16 [B, H, T, D], dig, dfg bf16 [B, H, T]) of a kvpop_mlstm_fwd call without a
+    state that returned o and lse, given that of o (bf16 [B, H, T, D], strided as q may be). ``grads``: the five
+    tensors preallocated."""
+    torch = _torch()
+    bf16 = torch.bfloat16
+    a, B, H, T, D, dev = _mlstm_parts(torch, q, k, v, ig, fg, scale, delay, normalize, lens)
+    dr, _, _ = _rows(torch, do, "do", B, H, T, D, dev)
+    shapes = [(B, H, T, D)] * 3 + [(B, H, T)] * 2
+    if grads is None:
+        grads = tuple(torch.empty(s, dtype=bf16, device=q.device) for s in shapes)
+    _need(len(grads) == 5, "grads are dq, dk, dv, dig, dfg")
+    _need(all(x is not None for x in (o, lse, *grads)), "o, lse and the gradients must be tensors")
+    out = _FIVE_PACK.pack(*(_ptr(x, n, bf16, s, dev) for x, n, s in zip(grads, ("dq", "dk", "dv", "dig", "dfg"), shapes)))
+    need = lib().kvpop_mlstm_bwd_workspace_size(a)
+    workspace = _workspace(torch, workspace, need, q.device, stream)
+    _call(torch, lib().kvpop_mlstm_bwd, dev, stream, a, _ROWS_PACK.pack(*dr), _ptr(o, "o", bf16, (B, H, T, D), dev),
+          _ptr(lse, "lse", torch.float32, (B, H, T), dev), out, workspace.data_ptr() if workspace is not None else 0, need)
+    return tuple(grads)
+
+
+def kvpop_mlstm_step(q, k, v, ig, fg, state: KvpopMlstmState, scale: float = 1.0, normalize: bool = True, active=None,
+                     o=None, stream=None):
+    """One token of each sequence: k, v (bf16 [B, H, D]) and the gates (bf16 [B, H]) go into ``state``,
+    which is updated in place, then q (bf16 [B, H, D]: that of the token ``delay`` before) reads it.
+    active: int32 [B], 0 for idle sequences, which keep what they hold (None: all are active). Returns
+    o bf16 [B, H, D], 0 for idle sequences."""
+    torch = _torch()
+    _need(isinstance(q, torch.Tensor) and q.dim() == 3, "q must be a tensor [B, H, D]")
+    _need(all(isinstance(x, torch.Tensor) and x.dim() == 3 for x in (k, v)), "k and v must be tensors [B, H, D]")
+    _need(all(isinstance(x, torch.Tensor) and x.dim() == 2 for x in (ig, fg)), "ig and fg must be tensors [B, H]")
+    a, B, H, _, D, dev = _mlstm_parts(torch, q.unsqueeze(2), k.unsqueeze(2), v.unsqueeze(2), ig.unsqueeze(2), fg.unsqueeze(2),
+                                      scale, 0, normalize, active)
+    _need(state is not None, "a step needs a state")
+    st = _state_ptrs(torch, state, B, H, D, dev)
+    if o is None:
+        o = torch.empty((B, H, D), dtype=torch.bfloat16, device=q.device)
+    _call(torch, lib().kvpop_mlstm_step, dev, stream, a, st, _ptr(o, "o", torch.bfloat16, (B, H, D), dev))
+    return o
+
+
+_MLSTM_FUNCTION = None
+
+
+def _mlstm_function():
+    """torch's differentiable form of the recurrence, made when it is first needed."""
+    global _MLSTM_FUNCTION
+    if _MLSTM_FUNCTION is None:
+        torch = _torch()
+
+        class Mlstm(torch.autograd.Function):
+            @staticmethod
+            def forward(ctx, q, k, v, ig, fg, scale, delay, normalize, lens):
+                o, lse = kvpop_mlstm_fwd(q, k, v, ig, fg, scale, delay, normalize, lens)
+                ctx.save_for_backward(q, k, v, ig, fg, o, lse, lens)
+                ctx.args = scale, delay, normalize
+                return o
+
+            @staticmethod
+            @torch.autograd.function.once_differentiable
+            def backward(ctx, do):
+                q, k, v, ig, fg, o, lse, lens = ctx.saved_tensors
+                if do.stride(-1) != 1 or any(s % 8 for s in do.stride()[:-1]) or do.data_ptr() % 16:
+                    do = do.contiguous()
+                return (*kvpop_mlstm_bwd(do, q, k, v, ig, fg, o, lse, *ctx.args, lens), None, None, None, None)
+
+        _MLSTM_FUNCTION = Mlstm
+    return _MLSTM_FUNCTION
+
+
+def kvpop_mlstm(q, k, v, ig, fg, scale: float = 1.0, delay: int = 0, normalize: bool = True, lens=None):
+    """kvpop_mlstm_fwd as a differentiable torch function (of q, k, v, ig and fg, once): returns o. Runs on
+    the current stream."""
+    return _mlstm_function().apply(q, k, v, ig, fg, float(scale), int(delay), bool(normalize), lens)

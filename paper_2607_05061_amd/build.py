@@ -19,7 +19,8 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB_NAME = "libkvpop.so"
 LIB_PATH = os.path.join(PKG_DIR, LIB_NAME)
 SOURCES = ["kvpop_api.cpp", "kvpop_kernels.hip", "kvpop_topk.hip", "kvpop_sparse_attn.hip",
-           "kvpop_cache.hip", "kvpop_cache_attn.hip", "kvpop_mass.hip"]
+           "kvpop_cache.hip", "kvpop_cache_attn.hip", "kvpop_mass.hip",
+           "kvpop_mlstm.hip"]
 
 # Packed fp32 VALU forms are disabled for all device code.
 HIP_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

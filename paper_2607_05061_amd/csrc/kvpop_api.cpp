@@ -1,9 +1,10 @@
 // C ABI of the KVpop future-attention target library: argument validation, error
 // reporting and dispatch to the gfx950 kernels. The semantics of every entry point
-// are specified in include/kvpop.h, include/kvpop_cache.h and include/kvpop_mass.h.
+// are specified in the headers in include/.
 #include "kvpop.h"
 #include "kvpop_cache.h"
 #include "kvpop_mass.h"
+#include "kvpop_mlstm.h"
 
 #include <hip/hip_runtime_api.h>
 
@@ -284,6 +285,81 @@ int check_mass_prompt_dims(int64_t B, int64_t H, int64_t Hq, int64_t T, int64_t*
   if (T > KVPOP_MAX_SEQ_LEN) return KVPOP_EUNSUPPORTED;
   if (!mul_ok(B * Hq, T, rows) || *rows > INT64_MAX / 16) return KVPOP_EINVAL;
   return KVPOP_OK;
+}
+
+// ---------------------------------------------------------------------------
+// The mLSTM scorer's recurrence (kvpop_mlstm.h)
+// ---------------------------------------------------------------------------
+
+// Sizes (pointers are not looked at); fills what the plan depends on.
+int check_mlstm_dims(const kvpop_mlstm* a, kvpop::MlstmLaunch* L) {
+  if (!a) return KVPOP_EINVAL;
+  if (a->batch < 1 || a->n_heads < 1 || a->seq_len < 1 || a->head_dim < 1 || a->delay < 0) return KVPOP_EINVAL;
+  if ((a->normalize != 0 && a->normalize != 1) || !std::isfinite(a->scale) || !(a->scale > 0.f)) return KVPOP_EINVAL;
+  if (a->head_dim != 64 && a->head_dim != 128) return KVPOP_EUNSUPPORTED;
+  if (a->seq_len > KVPOP_MAX_SEQ_LEN || (int64_t)a->batch * a->n_heads > INT32_MAX) return KVPOP_EUNSUPPORTED;
+  *L = kvpop::MlstmLaunch{};
+  L->B = a->batch;
+  L->H = a->n_heads;
+  L->T = a->seq_len;
+  L->D = a->head_dim;
+  L->delay = a->delay;
+  L->normalize = a->normalize;
+  L->scale = a->scale;
+  if (kvpop::mlstm_threads(*L) > UINT32_MAX) return KVPOP_EUNSUPPORTED;
+  return KVPOP_OK;
+}
+
+// A strided bf16 array [B, H, T] of gates.
+int check_gate(const kvpop_rows& r, int64_t B, int64_t H, int64_t T, int64_t* bytes) {
+  if (!r.ptr || r.stride_b < 0 || r.stride_h < 0 || r.stride_t < 0) return KVPOP_EINVAL;
+  int64_t x, y, z;
+  if (!mul_ok(B - 1, r.stride_b, &x) || !mul_ok(H - 1, r.stride_h, &y) || !mul_ok(T - 1, r.stride_t, &z) ||
+      x > INT64_MAX / 16 || y > INT64_MAX / 16 || z > INT64_MAX / 16)
+    return KVPOP_EINVAL;
+  if ((reinterpret_cast<uintptr_t>(r.ptr) & 1u) != 0) return KVPOP_EUNSUPPORTED;
+  *bytes = 2 * (x + y + z + 1);
+  return KVPOP_OK;
+}
+
+struct MlstmSpans {
+  int64_t q, k, v, ig, fg;
+};
+
+// Sizes and input arrays.
+int check_mlstm(const kvpop_mlstm* a, kvpop::MlstmLaunch* L, MlstmSpans* s) {
+  int st = check_mlstm_dims(a, L);
+  if (st != KVPOP_OK) return st;
+  const int64_t B = a->batch, H = a->n_heads, T = a->seq_len, D = a->head_dim;
+  if ((st = check_rows(a->q, B, H, T, D, &s->q)) != KVPOP_OK) return st;
+  if ((st = check_rows(a->k, B, H, T, D, &s->k)) != KVPOP_OK) return st;
+  if ((st = check_rows(a->v, B, H, T, D, &s->v)) != KVPOP_OK) return st;
+  if ((st = check_gate(a->ig, B, H, T, &s->ig)) != KVPOP_OK) return st;
+  if ((st = check_gate(a->fg, B, H, T, &s->fg)) != KVPOP_OK) return st;
+  if (!aligned4(a->lens)) return KVPOP_EUNSUPPORTED;
+  L->q = make_rows(a->q);
+  L->k = make_rows(a->k);
+  L->v = make_rows(a->v);
+  L->ig = make_rows(a->ig);
+  L->fg = make_rows(a->fg);
+  L->lens = a->lens;
+  return KVPOP_OK;
+}
+
+int check_state(const kvpop_mlstm_state* s, kvpop::MlstmLaunch* L) {
+  if (!s->C || !s->z || !s->m) return KVPOP_EINVAL;
+  if (!aligned16(s->C) || !aligned16(s->z) || !aligned4(s->m)) return KVPOP_EUNSUPPORTED;
+  L->C = s->C;
+  L->z = s->z;
+  L->m = s->m;
+  L->m_in = s->m;
+  return KVPOP_OK;
+}
+
+int check_workspace(const void* workspace, size_t bytes, int64_t need) {
+  if (need == 0) return KVPOP_OK;
+  if (!workspace || bytes < (size_t)need) return KVPOP_EINVAL;
+  return aligned16(workspace) ? KVPOP_OK : KVPOP_EUNSUPPORTED;
 }
 
 }  // namespace
@@ -766,6 +842,92 @@ int kvpop_mass_step(const kvpop_retain* s, const int32_t* q_pos, int32_t sinks, 
   L.slot = slot;
   if (kvpop::mass_step_threads(L) > UINT32_MAX) return KVPOP_EUNSUPPORTED;
   return launch([&] { return kvpop::launch_mass_step(L); });
+}
+
+size_t kvpop_mlstm_fwd_workspace_size(const kvpop_mlstm* a) {
+  kvpop::MlstmLaunch L;
+  if (check_mlstm_dims(a, &L) != KVPOP_OK) return 0;
+  return (size_t)kvpop::mlstm_fwd_workspace_floats(L) * 4;
+}
+
+size_t kvpop_mlstm_bwd_workspace_size(const kvpop_mlstm* a) {
+  kvpop::MlstmLaunch L;
+  if (check_mlstm_dims(a, &L) != KVPOP_OK) return 0;
+  return (size_t)kvpop::mlstm_bwd_workspace_floats(L) * 4;
+}
+
+int kvpop_mlstm_fwd(const kvpop_mlstm* a, const kvpop_mlstm_state* state, void* o, float* lse, void* workspace,
+                    size_t workspace_bytes, void* stream) {
+  kvpop::MlstmLaunch L;
+  MlstmSpans s;
+  int st = check_mlstm(a, &L, &s);
+  if (st != KVPOP_OK) return st;
+  if (!o) return KVPOP_EINVAL;
+  if (state && (st = check_state(state, &L)) != KVPOP_OK) return st;
+  if (!aligned16(o) || !aligned4(lse)) return KVPOP_EUNSUPPORTED;
+  const int64_t need = kvpop::mlstm_fwd_workspace_floats(L) * 4;
+  if ((st = check_workspace(workspace, workspace_bytes, need)) != KVPOP_OK) return st;
+  const int64_t lists = (int64_t)L.B * L.H, rows = lists * L.T, D = L.D;
+  const Span outs[] = {{o, rows * D * 2}, {lse, rows * 4}, {L.C, lists * D * D * 4}, {L.z, lists * D * 4},
+                       {L.m, lists * 4}, {need ? workspace : nullptr, need}};
+  const Span ins[] = {{a->q.ptr, s.q}, {a->k.ptr, s.k}, {a->v.ptr, s.v}, {a->ig.ptr, s.ig}, {a->fg.ptr, s.fg},
+                      {a->lens, (int64_t)L.B * 4}};
+  if (!disjoint(outs, ins)) return KVPOP_EINVAL;
+  L.o = static_cast<uint16_t*>(o);
+  L.lse_out = lse;
+  L.workspace = static_cast<float*>(workspace);
+  L.stream = stream;
+  return launch([&] { return kvpop::launch_mlstm_fwd(L); });
+}
+
+int kvpop_mlstm_bwd(const kvpop_mlstm* a, const kvpop_rows* do_, const void* o, const float* lse,
+                    const kvpop_mlstm_grads* g, void* workspace, size_t workspace_bytes, void* stream) {
+  kvpop::MlstmLaunch L;
+  MlstmSpans s;
+  int st = check_mlstm(a, &L, &s);
+  if (st != KVPOP_OK) return st;
+  if (!do_ || !o || !lse || !g || !g->dq || !g->dk || !g->dv || !g->dig || !g->dfg) return KVPOP_EINVAL;
+  int64_t db;
+  if ((st = check_rows(*do_, L.B, L.H, L.T, L.D, &db)) != KVPOP_OK) return st;
+  if (!aligned16(o) || !aligned4(lse) || !aligned16(g->dq) || !aligned16(g->dk) || !aligned16(g->dv)) return KVPOP_EUNSUPPORTED;
+  if (((reinterpret_cast<uintptr_t>(g->dig) | reinterpret_cast<uintptr_t>(g->dfg)) & 1u) != 0) return KVPOP_EUNSUPPORTED;
+  const int64_t need = kvpop::mlstm_bwd_workspace_floats(L) * 4;
+  if ((st = check_workspace(workspace, workspace_bytes, need)) != KVPOP_OK) return st;
+  const int64_t rows = (int64_t)L.B * L.H * L.T, D = L.D;
+  const Span outs[] = {{g->dq, rows * D * 2}, {g->dk, rows * D * 2}, {g->dv, rows * D * 2}, {g->dig, rows * 2},
+                       {g->dfg, rows * 2}, {need ? workspace : nullptr, need}};
+  const Span ins[] = {{a->q.ptr, s.q}, {a->k.ptr, s.k}, {a->v.ptr, s.v}, {a->ig.ptr, s.ig}, {a->fg.ptr, s.fg},
+                      {a->lens, (int64_t)L.B * 4}, {do_->ptr, db}, {o, rows * D * 2}, {lse, rows * 4}};
+  if (!disjoint(outs, ins)) return KVPOP_EINVAL;
+  L.go = make_rows(*do_);
+  L.o_in = static_cast<const uint16_t*>(o);
+  L.lse = lse;
+  L.dq = static_cast<uint16_t*>(g->dq);
+  L.dk = static_cast<uint16_t*>(g->dk);
+  L.dv = static_cast<uint16_t*>(g->dv);
+  L.dig = static_cast<uint16_t*>(g->dig);
+  L.dfg = static_cast<uint16_t*>(g->dfg);
+  L.workspace = static_cast<float*>(workspace);
+  L.stream = stream;
+  return launch([&] { return kvpop::launch_mlstm_bwd(L); });
+}
+
+int kvpop_mlstm_step(const kvpop_mlstm* a, const kvpop_mlstm_state* state, void* o, void* stream) {
+  kvpop::MlstmLaunch L;
+  MlstmSpans s;
+  int st = check_mlstm(a, &L, &s);
+  if (st != KVPOP_OK) return st;
+  if (!o || !state || a->seq_len != 1 || a->delay != 0) return KVPOP_EINVAL;
+  if ((st = check_state(state, &L)) != KVPOP_OK) return st;
+  if (!aligned16(o)) return KVPOP_EUNSUPPORTED;
+  const int64_t lists = (int64_t)L.B * L.H, D = L.D;
+  const Span outs[] = {{o, lists * D * 2}, {L.C, lists * D * D * 4}, {L.z, lists * D * 4}, {L.m, lists * 4}};
+  const Span ins[] = {{a->q.ptr, s.q}, {a->k.ptr, s.k}, {a->v.ptr, s.v}, {a->ig.ptr, s.ig}, {a->fg.ptr, s.fg},
+                      {a->lens, (int64_t)L.B * 4}};
+  if (!disjoint(outs, ins)) return KVPOP_EINVAL;
+  L.o = static_cast<uint16_t*>(o);
+  L.stream = stream;
+  return launch([&] { return kvpop::launch_mlstm_step(L); });
 }
 
 }  // extern "C"

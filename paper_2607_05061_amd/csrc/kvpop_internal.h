@@ -140,6 +140,35 @@ struct MassPromptLaunch {
   void* stream;
 };
 
+// The mLSTM scorer's recurrence (kvpop_mlstm.hip).
+struct MlstmLaunch {
+  int32_t B, H, T, D, delay, normalize;
+  float scale;
+  Rows q, k, v, ig, fg;     // ig, fg: bf16 [B, H, T]
+  Rows go;                  // backward: do
+  const int32_t* lens;      // [B] or nullptr
+  float *C, *z, *m;         // what is held, updated, or nullptr
+  const float* m_in;        // m
+  uint16_t* o;              // forward, step: [B, H, T, D]
+  float* lse_out;           // forward: [B, H, T] or nullptr
+  const uint16_t* o_in;     // backward: o and lse
+  const float* lse;
+  uint16_t *dq, *dk, *dv, *dig, *dfg;
+  float* workspace;
+  void* stream;
+  // plan
+  int32_t segs, seg_chunks; // segments of each head and their chunks of 64 tokens
+  float* parts;             // [directions, B, H, segs] parts
+  float *dots, *dig32;      // backward: [B, H, T]
+};
+
+int launch_mlstm_fwd(MlstmLaunch L);
+int launch_mlstm_bwd(MlstmLaunch L);
+int launch_mlstm_step(const MlstmLaunch& L);
+int64_t mlstm_threads(const MlstmLaunch& L);
+int64_t mlstm_fwd_workspace_floats(MlstmLaunch L);
+int64_t mlstm_bwd_workspace_floats(MlstmLaunch L);
+
 int launch_cache_mass(const CacheMassLaunch& L);
 int launch_mass_prompt(const MassPromptLaunch& L);
 int launch_mass_step(const RetainLaunch& L);

@@ -1,0 +1,1032 @@
+// gfx950 kernels of the mLSTM scorer's recurrence (include/kvpop_mlstm.h): read-outs of whole
+// sequences, their gradients, one token at a time.
+//
+// Chunks of 64 tokens. With b the running sum of log f since the chunk's start, a token's weight in a
+// later read-out of the chunk is exp(b_u - b_t + ig_t): a factor of the row times one of the column.
+// So a chunk is
+//   out = (far o (A S)) + (W o (A B^T)) C,   S <- keep S + B^T (w o C),
+// one product with what is held (S, D x D, in registers), a masked product within the chunk, and the
+// update. All four sweeps are this: the read-outs (A, B, C = q, k, v), dq (do, v, k) forwards,
+// dv (k, q, do) and dk (v, do, q) backwards in time, where what is held is the gradient of C_t.
+// Exponents are sums of 64-bit running sums in units of log2: no weight loses bits to a large |b|.
+//
+// Sequences are cut into segments for parallelism: a first sweep finds what each segment adds to
+// what is held, a scan over the segments what each one starts from, then every segment runs alone.
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "kvpop_internal.h"
+
+namespace kvpop {
+namespace {
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
+
+constexpr double kLog2e = 1.4426950408889634074, kLog2eInv = 0.69314718055994530942;
+constexpr int kChunk = 64;       // tokens of a chunk
+constexpr int kBlock = 4;        // chunks whose gates are worked out at once, one by each wave
+constexpr int kGates = kChunk * kBlock;
+
+enum { kFwd = 0, kDq = 1, kDkv = 2 };
+
+__device__ __forceinline__ int clampi(int x, int lo, int hi) { return min(max(x, lo), hi); }
+__device__ __forceinline__ float neg_inf() { return -__builtin_inff(); }
+__device__ __forceinline__ bool gone(double x) { return x == -__builtin_inf(); }
+__device__ __forceinline__ float bf16_value(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
+__device__ __forceinline__ uint16_t bf16_bits(float x) {
+  union { __bf16 h; uint16_t u; } y;
+  y.h = (__bf16)x;
+  return y.u;
+}
+// 2^x of a sum of 64-bit exponents; 0 where one of them is -inf and none NaN.
+__device__ __forceinline__ float pow2(double x) { return __builtin_amdgcn_exp2f((float)x); }
+
+__device__ __forceinline__ f32x4 mfma(const bf16x8& a, const bf16x8& b, const f32x4& c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+// The sum over the lanes l % 16 + 16 k, on all of them.
+__device__ __forceinline__ float sum_groups(float x) {
+  x += __shfl_xor(x, 16);
+  return x + __shfl_xor(x, 32);
+}
+
+// log2 sigmoid(x); 0 for +inf.
+__device__ __forceinline__ double log2_sigmoid(float x) {
+  return -(double)(fmaxf(-x, 0.f) + log1pf(expf(-fabsf(x)))) * kLog2e;
+}
+
+union Frag {
+  bf16x8 v;
+  bf16x4 h[2];
+  u32x2 d[2];
+  u32x4 u;
+};
+
+// 8 elements of a row, 16 bytes.
+__device__ __forceinline__ bf16x8 row8(const uint16_t* at) { return *reinterpret_cast<const bf16x8*>(at); }
+// Elements at, at + 1 .. + 3 and at + 16 .. + 19: the order of two accumulator tiles' rows.
+__device__ __forceinline__ bf16x8 row4x2(const uint16_t* at) {
+  Frag f;
+  f.d[0] = *reinterpret_cast<const u32x2*>(at);
+  f.d[1] = *reinterpret_cast<const u32x2*>(at + 16);
+  return f.v;
+}
+// Column c (of 16) of the 8 rows 8 g .. 8 g + 7 at `at` (a row of `stride` elements), lane = 16 g + c:
+// a transposed load gives lane c of a group the elements c of the four rows that its lanes name.
+__device__ __forceinline__ bf16x8 column8(const uint16_t* at, int stride, int g, int c) {
+  const uint16_t* p = at + (8 * g + (c >> 2)) * stride + 4 * (c & 3);
+  Frag f;
+  f.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)p);
+  f.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(p + 4 * stride));
+  return f.v;
+}
+
+// ---------------------------------------------------------------------------
+// Gates
+// ---------------------------------------------------------------------------
+
+// Of kBlock chunks, in units of log2, running sums from each chunk's start.
+struct Gates {
+  double u[kGates];    // ig - b
+  double r[kGates];    // kFwd: the largest u since the last reset; else b - lse (-inf: not read)
+  double b[kGates];
+  int rid[kGates];     // resets (fg = -inf) up to here
+  float d[kGates];     // backward: d_u, of the query that reads here
+  double sum[kBlock];  // b at the chunk's end
+  double top[kBlock];  // the largest exponent that the chunk adds to what is held
+  int resets[kBlock];
+  int odd_k[kBlock], odd_q[kBlock];  // tokens whose k, v (q, do) have no weight
+};
+
+// The wave's chunk into place `slot`.
+template <int MODE>
+__device__ __forceinline__ void chunk_gates(const MlstmLaunch& a, Gates& G, int b, int h, int n, int chunk, int slot,
+                                            int lane) {
+  const int t = chunk * kChunk + lane, i = slot * kChunk + lane;
+  const bool in = t < n;
+  float ig = neg_inf(), fg = -neg_inf();
+  if (in) {
+    ig = bf16_value(a.ig.ptr[b * a.ig.sb + h * a.ig.sh + t * a.ig.st]);
+    fg = bf16_value(a.fg.ptr[b * a.fg.sb + h * a.fg.sh + t * a.fg.st]);
+  }
+  const bool read = in && t >= a.delay;
+  float lse = neg_inf(), dot = 0.f;
+  if (MODE != kFwd && read) {
+    const int64_t row = ((int64_t)b * a.H + h) * a.T + t - a.delay;
+    lse = a.lse[row];
+    if (a.normalize) dot = -a.dots[row];
+  }
+  const bool reset = fg == neg_inf();
+  const uint64_t resets = __builtin_amdgcn_ballot_w64(reset), mine = resets & ((2ull << lane) - 1);
+  const int rid = __builtin_popcountll(mine), all = __builtin_popcountll(resets);
+  double s = reset ? 0.0 : log2_sigmoid(fg);
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const double y = __shfl_up(s, o);
+    if (lane >= o) s += y;
+  }
+  const double u = (double)ig * kLog2e - s;
+  double r, top;
+  if (MODE == kFwd) {
+    const int first = mine ? 63 - __builtin_clzll(mine) : 0;
+    r = u;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const double y = __shfl_up(r, o);
+      if (lane - o >= first) r = fmax(r, y);
+    }
+    top = r;
+  } else {
+    r = lse == neg_inf() ? -__builtin_inf() : s - (double)lse * kLog2e;
+    top = MODE == kDq ? (rid == all ? u : -__builtin_inf()) : (rid == 0 ? r : -__builtin_inf());
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) top = fmax(top, __shfl_xor(top, o));
+    if (gone(r)) dot = 0.f;
+  }
+  G.u[i] = u;
+  G.r[i] = r;
+  G.b[i] = s;
+  G.rid[i] = rid;
+  if (MODE != kFwd) G.d[i] = dot;
+  const uint64_t odd_k = __builtin_amdgcn_ballot_w64(in && gone(u));
+  const uint64_t odd_q = __builtin_amdgcn_ballot_w64(MODE != kFwd && read && gone(r));
+  if (lane == 63) {
+    G.sum[slot] = s;
+    G.top[slot] = top;
+    G.resets[slot] = all;
+    G.odd_k[slot] = odd_k != 0;
+    G.odd_q[slot] = odd_q != 0;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// What is held between chunks
+// ---------------------------------------------------------------------------
+
+// A segment's part of the workspace: a matrix [D, D], a vector [D], then these.
+struct SegmentScalars {
+  double add;   // the exponent of what the segment adds
+  double sum;   // log f over the segment, -inf with a reset
+  double from;  // the exponent of what it starts from
+};
+__host__ __device__ constexpr int segment_floats(int D) { return D * D + D + 8; }
+__device__ __forceinline__ SegmentScalars* scalars(float* part, int D) {
+  return reinterpret_cast<SegmentScalars*>(part + D * D + D);
+}
+
+// One array's chunks of rows, on their way to LDS. Rows at times outside [first, n) are zeros.
+template <int D, int THREADS>
+struct Tile {
+  static constexpr int kPer = kChunk * D / 8 / THREADS;
+  static constexpr int kStride = D + 8;  // elements of a row in LDS: 16 rows spread over all banks
+  u32x4 x[kPer];
+  __device__ __forceinline__ void load(const Rows& a, int b, int h, int t0, int shift, int n, int tid) {
+    const uint16_t* p = a.ptr + b * a.sb + h * a.sh + 8 * (tid % (D / 8));
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int t = t0 + tid / (D / 8) + i * (THREADS * 8 / D);
+      x[i] = u32x4{0, 0, 0, 0};
+      if (t >= shift && t < n) x[i] = *reinterpret_cast<const u32x4*>(p + (int64_t)(t - shift) * a.st);
+    }
+  }
+  __device__ __forceinline__ void store(uint16_t* sh, int tid) const {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i)
+      *reinterpret_cast<u32x4*>(sh + (tid / (D / 8) + i * (THREADS * 8 / D)) * kStride + 8 * (tid % (D / 8))) = x[i];
+  }
+};
+
+// Rows of a chunk that have no weight become zeros, so that nothing in them (NaN) matters.
+template <int D>
+__device__ __forceinline__ void clear_rows(uint16_t* sh, const double* weight, int tid, int threads) {
+  for (int i = tid; i < kChunk * D; i += threads)
+    if (gone(weight[i / D])) sh[(i / D) * (D + 8) + i % D] = 0;
+}
+
+// The exponents of a chunk's update: what is held before (m), after (next), and a token's.
+template <bool REV>
+struct Update {
+  double next, shift;
+  float keep;
+  int want;
+  __device__ __forceinline__ Update(const Gates& G, int slot, double m) {
+    const int all = G.resets[slot];
+    const double old = all == 0 ? m + G.sum[slot] : -__builtin_inf();
+    const double top = REV ? G.top[slot] : G.top[slot] + G.sum[slot];
+    next = fmax(old, top);
+    keep = gone(old) ? 0.f : pow2(old - next);
+    shift = gone(next) ? 0.0 : (REV ? -next : G.sum[slot] - next);
+    want = REV ? 0 : all;
+  }
+  __device__ __forceinline__ float weight(const Gates& G, int i) const {
+    return G.rid[i] == want ? pow2((REV ? G.r[i] : G.u[i]) + shift) : 0.f;
+  }
+};
+
+// S <- keep S + B^T (w o C) on this wave's NT * 16 columns of C. w o C is taken as the sum of two bf16
+// (16 bits), so that what is held keeps fp32's meaning; rounded once, it would be off by 2^-9.
+template <int D, int NT>
+__device__ __forceinline__ void update_state(f32x4 (&S)[D / 16][NT], float keep, const uint16_t* b_sh,
+                                             const bf16x8 (&cf)[2][NT], const float* w_sh, int g, int c) {
+  constexpr int LS = D + 8;
+  bf16x8 hi[2][NT], lo[2][NT];
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    float w[8];
+    *reinterpret_cast<f32x4*>(w) = *reinterpret_cast<const f32x4*>(w_sh + 32 * s + 8 * g);
+    *reinterpret_cast<f32x4*>(w + 4) = *reinterpret_cast<const f32x4*>(w_sh + 32 * s + 8 * g + 4);
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float x = (float)cf[s][t][i] * w[i];
+        hi[s][t][i] = (__bf16)x;
+        lo[s][t][i] = (__bf16)(x - (float)hi[s][t][i]);
+      }
+  }
+#pragma unroll
+  for (int i = 0; i < D / 16; ++i) {
+    bf16x8 bf[2];
+#pragma unroll
+    for (int s = 0; s < 2; ++s) bf[s] = column8(b_sh + 32 * s * LS + 16 * i, LS, g, c);
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      S[i][t] = keep == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : S[i][t] * keep;  // what is forgotten may be anything
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        S[i][t] = mfma(bf[s], hi[s][t], S[i][t]);
+        S[i][t] = mfma(bf[s], lo[s][t], S[i][t]);
+      }
+    }
+  }
+}
+
+// sum_t w_t b_t over the 16 columns of B at b_sh, row 4 g + r of them: columns 0 and 1 of a product whose other
+// operand is (w's high part, its low part).
+template <int D>
+__device__ __forceinline__ f32x4 weighted_rows(const uint16_t* b_sh, const float* w_sh, int g, int c) {
+  f32x4 z = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    bf16x8 wf;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float w = w_sh[32 * s + 8 * g + i], hi = (float)(__bf16)w;
+      wf[i] = (__bf16)(c == 0 ? w : c == 1 ? w - hi : 0.f);
+    }
+    z = mfma(column8(b_sh + 32 * s * (D + 8), D + 8, g, c), wf, z);
+  }
+#pragma unroll
+  for (int r = 0; r < 4; ++r) z[r] += __shfl_xor(z[r], 1);
+  return z;
+}
+
+// ---------------------------------------------------------------------------
+// First sweep: what each segment adds to what is held
+// ---------------------------------------------------------------------------
+
+// One workgroup per segment of a head and direction (blockIdx.y: 0 forwards, k and v; 1 backwards, q
+// and do). Wave w holds columns [w D / 4, (w + 1) D / 4) of the matrix.
+template <int D>
+__global__ __launch_bounds__(256) void mlstm_segment_kernel(MlstmLaunch a) {
+  constexpr int NT = D / 64, LS = D + 8, NZ = D / 64;
+  __shared__ __align__(16) uint16_t b_sh[kChunk * LS], c_sh[kChunk * LS];
+  __shared__ Gates G;
+  __shared__ __align__(16) float w_sh[kChunk], wz_sh[kChunk];
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, c = lane & 15;
+  const int seg = blockIdx.x % a.segs, list = blockIdx.x / a.segs, b = list / a.H, h = list % a.H;
+  const int n = a.lens ? clampi(a.lens[b], 0, a.T) : a.T, chunks = (n + kChunk - 1) / kChunk;
+  const bool rev = blockIdx.y != 0;
+  const int first = min(seg * a.seg_chunks, chunks), count = min((seg + 1) * a.seg_chunks, chunks) - first;
+  const Rows& rb = rev ? a.q : a.k;
+  const Rows& rc = rev ? a.go : a.v;
+  const int shift = rev ? a.delay : 0;
+
+  f32x4 S[D / 16][NT];
+#pragma unroll
+  for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+    for (int t = 0; t < NT; ++t) S[i][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  f32x4 z[NZ];
+#pragma unroll
+  for (int j = 0; j < NZ; ++j) z[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  double m = -__builtin_inf(), sum = 0.0;
+  auto chunk_at = [&](int i) { return rev ? first + count - 1 - i : first + i; };
+
+  Tile<D, 256> tb, tc;
+  if (count > 0) {
+    tb.load(rb, b, h, chunk_at(0) * kChunk, shift, n, tid);
+    tc.load(rc, b, h, chunk_at(0) * kChunk, shift, n, tid);
+  }
+  for (int i = 0; i < count; ++i) {
+    const int slot = i % kBlock;
+    if (slot == 0 && i + wave < count) {
+      if (rev)
+        chunk_gates<kDkv>(a, G, b, h, n, chunk_at(i + wave), wave, lane);
+      else
+        chunk_gates<kFwd>(a, G, b, h, n, chunk_at(i + wave), wave, lane);
+    }
+    tb.store(b_sh, tid);
+    tc.store(c_sh, tid);
+    __syncthreads();
+    if (rev ? G.odd_q[slot] : G.odd_k[slot]) {
+      clear_rows<D>(b_sh, (rev ? G.r : G.u) + slot * kChunk, tid, 256);
+      clear_rows<D>(c_sh, (rev ? G.r : G.u) + slot * kChunk, tid, 256);
+      __syncthreads();
+    }
+    if (i + 1 < count) {
+      tb.load(rb, b, h, chunk_at(i + 1) * kChunk, shift, n, tid);
+      tc.load(rc, b, h, chunk_at(i + 1) * kChunk, shift, n, tid);
+    }
+    double next;
+    float keep;
+    if (rev) {
+      const Update<true> up(G, slot, m);
+      next = up.next, keep = up.keep;
+      if (tid < kChunk) w_sh[tid] = up.weight(G, slot * kChunk + tid), wz_sh[tid] = w_sh[tid] * G.d[slot * kChunk + tid];
+    } else {
+      const Update<false> up(G, slot, m);
+      next = up.next, keep = up.keep;
+      if (tid < kChunk) wz_sh[tid] = w_sh[tid] = up.weight(G, slot * kChunk + tid);
+    }
+    sum = G.resets[slot] ? -__builtin_inf() : sum + G.sum[slot];
+    __syncthreads();
+    bf16x8 cf[2][NT];
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int t = 0; t < NT; ++t) cf[s][t] = column8(c_sh + 32 * s * LS + (wave * NT + t) * 16, LS, g, c);
+    update_state<D, NT>(S, keep, b_sh, cf, w_sh, g, c);
+#pragma unroll
+    for (int j = 0; j < NZ; ++j) {
+      const f32x4 add = weighted_rows<D>(b_sh + (wave * NZ + j) * 16, wz_sh, g, c);
+      z[j] = (keep == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : z[j] * keep) + add;
+    }
+    m = next;
+    __syncthreads();
+  }
+
+  float* part = a.parts + ((int64_t)blockIdx.y * a.B * a.H * a.segs + blockIdx.x) * segment_floats(D);
+#pragma unroll
+  for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) part[(16 * i + 4 * g + r) * D + (wave * NT + t) * 16 + c] = S[i][t][r];
+#pragma unroll
+  for (int j = 0; j < NZ; ++j)
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      if (c == 0) part[D * D + (wave * NZ + j) * 16 + 4 * g + r] = z[j][r];
+  if (tid == 0) {
+    scalars(part, D)->add = m;
+    scalars(part, D)->sum = sum;
+    if (seg == (rev ? a.segs - 1 : 0)) scalars(part, D)->from = !rev && a.C ? (double)a.m_in[list] * kLog2e : -__builtin_inf();
+  }
+}
+
+// ---------------------------------------------------------------------------
+// What each segment starts from
+// ---------------------------------------------------------------------------
+
+// One thread per 4 elements of a head's matrix and vector, which it carries over the segments: a part is
+// replaced by what its segment starts from. Forwards, a given state is where it starts and ends.
+template <int D>
+__global__ __launch_bounds__(256) void mlstm_scan_kernel(MlstmLaunch a, int blocks) {
+  const int list = blockIdx.x / blocks, e = ((blockIdx.x % blocks) * 256 + threadIdx.x) * 4;
+  if (e >= D * D + D) return;
+  const bool rev = blockIdx.y != 0;
+  float* parts = a.parts + ((int64_t)blockIdx.y * a.B * a.H + list) * a.segs * segment_floats(D);
+  float* held = nullptr;
+  f32x4 x = {0.f, 0.f, 0.f, 0.f};
+  if (!rev && a.C) {
+    held = e < D * D ? a.C + (int64_t)list * D * D + e : a.z + (int64_t)list * D + (e - D * D);
+    x = *reinterpret_cast<const f32x4*>(held);
+  }
+  constexpr int kAhead = 4;  // parts on their way
+  f32x4 next[kAhead];
+  auto part = [&](int i) { return parts + (int64_t)(rev ? a.segs - 1 - i : i) * segment_floats(D); };
+  double m = scalars(part(0), D)->from;
+#pragma unroll
+  for (int j = 0; j < kAhead; ++j)
+    if (j < a.segs) next[j] = *reinterpret_cast<const f32x4*>(part(j) + e);
+  for (int i0 = 0; i0 < a.segs; i0 += kAhead) {
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      const int i = i0 + j;
+      if (i >= a.segs) break;
+      float* p = part(i);
+      SegmentScalars* s = scalars(p, D);
+      const f32x4 add = next[j];
+      if (i + kAhead < a.segs) next[j] = *reinterpret_cast<const f32x4*>(part(i + kAhead) + e);
+      *reinterpret_cast<f32x4*>(p + e) = x;
+      if (e == 0 && i > 0) s->from = m;
+      const double old = m + s->sum, now = fmax(old, s->add);
+      const float keep = gone(old) ? 0.f : pow2(old - now), put = gone(s->add) ? 0.f : pow2(s->add - now);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) x[r] = (keep == 0.f ? 0.f : x[r] * keep) + add[r] * put;
+      m = now;
+    }
+  }
+  if (held) {
+    *reinterpret_cast<f32x4*>(held) = x;
+    if (e == 0) a.m[list] = (float)(m * kLog2eInv);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// The sweeps
+// ---------------------------------------------------------------------------
+
+template <int D, int MODE>
+struct Shared {
+  static constexpr int kTiles = MODE == kDkv ? 4 : 3, kRoles = MODE == kDkv ? 2 : 1;
+  __align__(16) uint16_t tile[kTiles][kChunk * (D + 8)];
+  __align__(16) uint16_t p[kRoles][kChunk * (kChunk + 8)];
+  Gates G;
+  __align__(16) float w[kChunk], wz[kChunk];
+  __align__(16) float far[kRoles][kChunk], far_z[kRoles][kChunk], out[kChunk];
+  __align__(16) float z[kRoles][D];
+  float dig[4][kChunk];
+};
+
+// One workgroup per segment of a head. 4 waves (for dk and dv 4 each, over the same tiles): wave w takes
+// rows [16 w, 16 w + 16) of the masked product, which it leaves in LDS, and columns [w D / 4, (w + 1) D / 4) of
+// what is held, of the output and of the update. Products are transposed throughout, so that what is held
+// serves as an operand from the registers that accumulate it (its rows are the contraction, in the
+// order of two accumulator tiles' rows) and a lane's outputs are 4 neighbours of a row.
+template <int D, int MODE>
+__global__ __launch_bounds__(MODE == kDkv ? 512 : 256) void mlstm_kernel(MlstmLaunch a) {
+  constexpr bool REV = MODE == kDkv;
+  constexpr int NT = D / 64, LS = D + 8, PS = kChunk + 8, NZ = D / 64, THREADS = REV ? 512 : 256;
+  __shared__ Shared<D, MODE> sh;
+  Gates& G = sh.G;
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, c = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane((tid >> 6) & 3), role = REV ? __builtin_amdgcn_readfirstlane(tid >> 8) : 0;
+  const int seg = blockIdx.x % a.segs, list = blockIdx.x / a.segs, b = list / a.H, h = list % a.H;
+  const int n = a.lens ? clampi(a.lens[b], 0, a.T) : a.T, chunks = (n + kChunk - 1) / kChunk;
+  const int first = min(seg * a.seg_chunks, chunks), count = min((seg + 1) * a.seg_chunks, chunks) - first;
+  auto chunk_at = [&](int i) { return REV ? first + count - 1 - i : first + i; };
+  // kFwd: q, k, v. kDq: do, v, k. kDkv: k, v, q, do.
+  const Rows& r0 = MODE == kFwd ? a.q : MODE == kDq ? a.go : a.k;
+  const Rows& r1 = MODE == kFwd ? a.k : a.v;
+  const Rows& r2 = MODE == kFwd ? a.v : MODE == kDq ? a.k : a.q;
+  const int late0 = REV ? 0 : a.delay, late2 = REV ? a.delay : 0;
+  const uint16_t* a_sh = sh.tile[REV && role ? 1 : 0];
+  const uint16_t* b_sh = sh.tile[!REV ? 1 : role ? 3 : 2];
+  const uint16_t* c_sh = sh.tile[!REV ? 2 : role ? 2 : 3];
+  // What multiplies with the vector that is held beside the matrix: nothing for dv.
+  const bool with_z = MODE != kDkv || role;
+  // The state's rows are C's dk and its columns dv, or the other way round.
+  const bool turned = MODE == kDq || (REV && role);
+  uint16_t* out = MODE == kFwd ? a.o : MODE == kDq ? a.dq : role ? a.dk : a.dv;
+
+  // What the segment starts from.
+  f32x4 S[D / 16][NT];
+  double m = -__builtin_inf();
+  const float* from_S = nullptr;
+  const float* from_z = nullptr;
+  if (a.segs > 1) {
+    float* part = a.parts + (((int64_t)(REV ? a.B * a.H : 0) + list) * a.segs + seg) * segment_floats(D);
+    from_S = part, from_z = part + D * D;
+    m = scalars(part, D)->from;
+  } else if (MODE == kFwd && a.C) {
+    from_S = a.C + (int64_t)list * D * D, from_z = a.z + (int64_t)list * D;
+    m = (double)a.m_in[list] * kLog2e;
+  }
+#pragma unroll
+  for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int row = 16 * i + 4 * g + r, col = (wave * NT + t) * 16 + c;
+        S[i][t][r] = from_S ? from_S[turned ? col * D + row : row * D + col] : 0.f;
+      }
+  if ((tid & 255) < D) sh.z[role][tid & 255] = from_z ? from_z[tid & 255] : 0.f;
+
+  Tile<D, THREADS> t0, t1, t2, t3;
+  auto load = [&](int chunk) __attribute__((always_inline)) {
+    t0.load(r0, b, h, chunk * kChunk, late0, n, tid);
+    t1.load(r1, b, h, chunk * kChunk, 0, n, tid);
+    t2.load(r2, b, h, chunk * kChunk, late2, n, tid);
+    if (REV) t3.load(a.go, b, h, chunk * kChunk, a.delay, n, tid);
+  };
+  if (count > 0) load(chunk_at(0));
+
+  for (int it = 0; it < count; ++it) {
+    const int chunk = chunk_at(it), slot = it % kBlock, at = slot * kChunk;
+    if (slot == 0 && role == 0 && it + wave < count) chunk_gates<MODE>(a, G, b, h, n, chunk_at(it + wave), wave, lane);
+    t0.store(sh.tile[0], tid);
+    t1.store(sh.tile[1], tid);
+    t2.store(sh.tile[2], tid);
+    if (REV) t3.store(sh.tile[REV ? 3 : 0], tid);
+    __syncthreads();
+    if (G.odd_k[slot] | (MODE != kFwd ? G.odd_q[slot] : 0)) {
+      if (MODE == kFwd) {
+        clear_rows<D>(sh.tile[1], G.u + at, tid, THREADS);
+        clear_rows<D>(sh.tile[2], G.u + at, tid, THREADS);
+      } else if (MODE == kDq) {
+        clear_rows<D>(sh.tile[0], G.r + at, tid, THREADS);
+        clear_rows<D>(sh.tile[1], G.u + at, tid, THREADS);
+        clear_rows<D>(sh.tile[2], G.u + at, tid, THREADS);
+      } else {
+        clear_rows<D>(sh.tile[0], G.u + at, tid, THREADS);
+        clear_rows<D>(sh.tile[1], G.u + at, tid, THREADS);
+        clear_rows<D>(sh.tile[2], G.r + at, tid, THREADS);
+        clear_rows<D>(sh.tile[REV ? 3 : 0], G.r + at, tid, THREADS);
+      }
+      __syncthreads();
+    }
+    if (it + 1 < count) load(chunk_at(it + 1));
+
+    const Update<REV> up(G, slot, m);
+    if (tid < kChunk) {
+      const float w = up.weight(G, at + tid);
+      sh.w[tid] = w;
+      sh.wz[tid] = REV ? w * G.d[at + tid] : w;
+    }
+    {  // The masked product, transposed: this lane has row j and columns 4 g + r of each 16.
+      const int j = 16 * wave + c, rid = G.rid[at + j];
+      double rho;   // the row's exponent within the chunk
+      float far;    // its factor of what is held
+      if (MODE == kFwd) {
+        const double M = rid == 0 ? fmax(m, G.r[at + j]) : G.r[at + j];
+        rho = gone(M) ? 0.0 : -M;
+        far = rid == 0 && !gone(m) ? pow2(m + rho) : 0.f;
+      } else if (MODE == kDq) {
+        rho = G.r[at + j];
+        far = rid == 0 && !gone(m) ? pow2(rho + m) : 0.f;
+      } else {
+        rho = G.u[at + j];
+        far = rid == G.resets[slot] && !gone(m) ? pow2(rho + G.sum[slot] + m) : 0.f;
+      }
+      const float alpha = MODE == kDq ? G.d[at + j] : 0.f;
+      bf16x8 af[D / 32];
+#pragma unroll
+      for (int s = 0; s < D / 32; ++s) af[s] = row8(a_sh + j * LS + 32 * s + 8 * g);
+      float den = 0.f;
+      const int k0 = REV ? wave & ~1 : 0, k1 = REV ? 4 : (wave | 1) + 1;
+#pragma unroll
+      for (int kt = 0; kt < 4; ++kt) {
+        if (kt < k0 || kt >= k1) continue;
+        bf16x4 p = {(__bf16)0.f, (__bf16)0.f, (__bf16)0.f, (__bf16)0.f};
+        if (REV ? kt >= wave : kt <= wave) {
+          f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int s = 0; s < D / 32; ++s) acc = mfma(row8(b_sh + (16 * kt + c) * LS + 32 * s + 8 * g), af[s], acc);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int key = 16 * kt + 4 * g + r;
+            const bool in = (REV ? key >= j : key <= j) && G.rid[at + key] == rid;
+            const double e = (REV ? G.r[at + key] : G.u[at + key]) + rho;
+            float x = acc[r];
+            if (MODE == kDq) x += alpha;
+            if (REV && role) x += G.d[at + key];
+            x = in ? x * pow2(e) : 0.f;
+            den += x;
+            p[r] = (__bf16)x;
+          }
+        }
+        *reinterpret_cast<bf16x4*>(sh.p[role] + j * PS + 16 * kt + 4 * g) = p;
+      }
+      if (MODE == kFwd) {
+        float qz = 0.f;
+#pragma unroll
+        for (int s = 0; s < D / 32; ++s)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) qz += (float)af[s][i] * sh.z[0][32 * s + 8 * g + i];
+        den = sum_groups(den + (far == 0.f ? 0.f : far * qz)) * a.scale;
+        const double e = G.b[at + j] - rho;  // that of the row's common factor
+        float fac, lse;
+        if (a.normalize) {
+          const bool some = den > 0.f;
+          fac = some ? a.scale / den : 0.f;
+          lse = some ? logf(den) + (float)(e * kLog2eInv) : neg_inf();
+          if (den != den) fac = lse = den;
+        } else {
+          fac = a.scale * pow2(e);
+          lse = 0.f;
+        }
+        const int t = chunk * kChunk + j;
+        if (g == 0) {
+          sh.out[j] = fac;
+          if (a.lse_out && t >= a.delay && t < n) a.lse_out[((int64_t)b * a.H + h) * a.T + t - a.delay] = lse;
+        }
+      }
+      if (g == 0) {
+        sh.far[role][j] = far;
+        if (MODE != kFwd) sh.far_z[role][j] = MODE == kDq ? far * alpha : far;
+      }
+    }
+    __syncthreads();
+
+    bf16x8 cf[2][NT];
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int t = 0; t < NT; ++t) cf[s][t] = column8(c_sh + 32 * s * LS + (wave * NT + t) * 16, LS, g, c);
+    f32x4 acc[4][NT];
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+#pragma unroll
+      for (int t = 0; t < NT; ++t) acc[q][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    // What is held, rounded to bf16 for the product (its terms' errors are independent; out is rounded too).
+#pragma unroll
+    for (int s = 0; s < D / 32; ++s) {
+      bf16x8 sf[NT];
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sf[t][i] = (__bf16)S[2 * s + i / 4][t][i % 4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const bf16x8 af = row4x2(a_sh + (16 * q + c) * LS + 32 * s + 4 * g);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) acc[q][t] = mfma(sf[t], af, acc[q][t]);
+      }
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int j = 16 * q + c, time = chunk * kChunk + j;
+      const float far = sh.far[role][j], fac = MODE == kFwd ? sh.out[j] : a.scale;
+      const float far_z = MODE != kFwd && with_z ? sh.far_z[role][j] : 0.f;
+      float dot = 0.f;
+      const int row = REV ? time : time - a.delay;
+      const bool live = time < n && row >= 0;
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        const int col = (wave * NT + t) * 16 + 4 * g;
+        acc[q][t] = far == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : acc[q][t] * far;
+        if (MODE != kFwd && with_z) {
+          const f32x4 z = *reinterpret_cast<const f32x4*>(sh.z[role] + col);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) acc[q][t][r] += far_z == 0.f ? 0.f : far_z * z[r];
+        }
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+          if (REV ? 32 * s + 31 >= 16 * q : 32 * s <= 16 * q)
+            acc[q][t] = mfma(cf[s][t], row8(sh.p[role] + j * PS + 32 * s + 8 * g), acc[q][t]);
+        bf16x4 y;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float x = acc[q][t][r] * fac;
+          y[r] = (__bf16)x;
+          if (REV) dot += x * bf16_value(sh.tile[0][j * LS + col + r]);
+        }
+        if (live) *reinterpret_cast<bf16x4*>(out + (((int64_t)b * a.H + h) * a.T + row) * D + col) = y;
+      }
+      if (REV && role) {
+        dot = sum_groups(dot);
+        if (g == 0) sh.dig[wave][j] = dot;
+      }
+    }
+
+    update_state<D, NT>(S, up.keep, b_sh, cf, sh.w, g, c);
+    if (MODE == kFwd) {
+#pragma unroll
+      for (int i = 0; i < NZ; ++i) {
+        const f32x4 add = weighted_rows<D>(b_sh + (wave * NZ + i) * 16, sh.w, g, c);
+        float* z = sh.z[0] + (wave * NZ + i) * 16 + 4 * g;
+        if (c == 0)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) z[r] = (up.keep == 0.f ? 0.f : z[r] * up.keep) + add[r];
+      }
+    } else if (with_z) {  // a vector over this wave's own columns: sum w_t c_t
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        float x = 0.f;
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x += (float)cf[s][t][i] * sh.wz[32 * s + 8 * g + i];
+        x = sum_groups(x);
+        float* z = sh.z[role] + (wave * NT + t) * 16 + c;
+        if (g == 0) *z = (up.keep == 0.f ? 0.f : *z * up.keep) + x;
+      }
+    }
+    m = up.next;
+    __syncthreads();
+    if (REV && tid < kChunk) {
+      const int t = chunk * kChunk + tid;
+      if (t < n) {
+        const float x = sh.dig[0][tid] + sh.dig[1][tid] + sh.dig[2][tid] + sh.dig[3][tid];
+        a.dig32[(int64_t)list * a.T + t] = x;
+        a.dig[(int64_t)list * a.T + t] = bf16_bits(x);
+      }
+    }
+  }
+
+  // Rows that nothing reads, and tokens past the sequence's end.
+  const int c0 = seg * a.seg_chunks, c1 = min((seg + 1) * a.seg_chunks, (a.T + kChunk - 1) / kChunk);
+  const int z0 = max(c0 * kChunk, max(0, REV ? n : n - a.delay)), z1 = min(c1 * kChunk, a.T);
+  for (int64_t i = (int64_t)z0 * (D / 8) + (tid & 255); i < (int64_t)z1 * (D / 8); i += 256)
+    *reinterpret_cast<u32x4*>(out + (int64_t)list * a.T * D + i * 8) = u32x4{0, 0, 0, 0};
+  for (int i = z0 + tid; i < z1; i += THREADS) {
+    if (MODE == kFwd && a.lse_out) a.lse_out[(int64_t)list * a.T + i] = neg_inf();
+    if (REV) a.dig[(int64_t)list * a.T + i] = 0;
+  }
+
+  if (MODE == kFwd && a.segs == 1 && a.C) {
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          a.C[(int64_t)list * D * D + (16 * i + 4 * g + r) * D + (wave * NT + t) * 16 + c] = S[i][t][r];
+    if (tid < D) a.z[(int64_t)list * D + tid] = sh.z[0][tid];
+    if (tid == 0) a.m[list] = (float)(m * kLog2eInv);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// The rest of the backward pass
+// ---------------------------------------------------------------------------
+
+// do . o of each row: D / 8 threads a row.
+template <int D>
+__global__ __launch_bounds__(256) void mlstm_dots_kernel(MlstmLaunch a, int64_t rows) {
+  constexpr int W = D / 8;
+  const int64_t row = (int64_t)blockIdx.x * (256 / W) + threadIdx.x / W;
+  if (row >= rows) return;
+  const int list = (int)(row / a.T), t = (int)(row % a.T), b = list / a.H, h = list % a.H, i = threadIdx.x % W;
+  const int n = a.lens ? clampi(a.lens[b], 0, a.T) : a.T;
+  float s = 0.f;
+  if (t < n - a.delay) {
+    Frag x, y;
+    x.u = *reinterpret_cast<const u32x4*>(a.go.ptr + b * a.go.sb + h * a.go.sh + t * a.go.st + 8 * i);
+    y.u = *reinterpret_cast<const u32x4*>(a.o_in + row * D + 8 * i);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s += (float)x.v[j] * (float)y.v[j];
+  }
+#pragma unroll
+  for (int o = 1; o < W; o <<= 1) s += __shfl_xor(s, o);
+  if (i == 0) a.dots[row] = s;
+}
+
+__device__ __forceinline__ double block_sum(double x, double* sh) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = x;
+  __syncthreads();
+  return sh[0] + sh[1] + sh[2] + sh[3];
+}
+
+// The forget gates' gradients, one workgroup per segment. d log f_t is the sum over the pairs s < t <= u
+// that t lies between. At a segment's start that is the product of what is held there and its gradient,
+// and from token to token it changes by x . dx - k . dk of the token, where x . dx is 0 (a normalised
+// read-out does not change with x's length) or do . o. The running sum of k . dk, whose terms were
+// rounded on the way, starts from the one product and is made to end in the next, in proportion: its
+// errors do not pile up along the sequence.
+template <int D>
+__global__ __launch_bounds__(256) void mlstm_forget_kernel(MlstmLaunch a) {
+  __shared__ double sum_sh[4], edge_sh[4];
+  __shared__ int reset_sh[4];
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  const int seg = blockIdx.x % a.segs, list = blockIdx.x / a.segs, b = list / a.H, h = list % a.H;
+  const int n = a.lens ? clampi(a.lens[b], 0, a.T) : a.T;
+  const int t0 = min(seg * a.seg_chunks * kChunk, a.T), t1 = min((seg + 1) * a.seg_chunks * kChunk, a.T), end = min(t1, n);
+  auto edge = [&](int s) {  // at the start of segment s
+    if (s <= 0 || s >= a.segs) return 0.0;
+    float* x = a.parts + ((int64_t)list * a.segs + s) * segment_floats(D);
+    float* y = a.parts + (((int64_t)a.B * a.H + list) * a.segs + s - 1) * segment_floats(D);
+    const double e = scalars(x, D)->from + scalars(y, D)->from;
+    float part = 0.f;
+    for (int i = tid * 4; i < D * D + D; i += 1024) {
+      const f32x4 p = *reinterpret_cast<const f32x4*>(x + i), q = *reinterpret_cast<const f32x4*>(y + i);
+      part += p.x * q.x + p.y * q.y + p.z * q.z + p.w * q.w;
+    }
+    const double all = block_sum((double)part, sum_sh) * a.scale;
+    return gone(e) ? 0.0 : all * (double)pow2(e);
+  };
+  const double start = edge(seg), stop = edge(seg + 1);
+  // a token's step: x . dx - k . dk
+  auto step = [&](int t) -> double {
+    if (t >= end) return 0.0;
+    double x = -(double)a.dig32[(int64_t)list * a.T + t];
+    if (!a.normalize && t >= a.delay) x += a.dots[(int64_t)list * a.T + t - a.delay];
+    return x;
+  };
+  auto fg = [&](int t) { return bf16_value(a.fg.ptr[b * a.fg.sb + h * a.fg.sh + t * a.fg.st]); };
+  double total = 0.0, resets = 0.0;
+  for (int t = t0 + tid; t < end; t += 256) {
+    total += step(t);
+    resets += fg(t) == neg_inf();
+  }
+  total = block_sum(total, sum_sh);
+  resets = block_sum(resets, sum_sh);
+  const double drift = resets > 0.0 || end <= t0 ? 0.0 : (start - total - stop) / (end - t0);
+  double carry = start;  // before this block's tokens
+  for (int base = t0; base < end; base += 256) {
+    const int t = base + tid;
+    const bool in = t < end;
+    const float f = in ? fg(t) : 0.f;
+    const bool reset = in && f == neg_inf();
+    const double mine = step(t);
+    // the running sum of steps before t, since the last reset at or before t
+    double s = mine;
+    const uint64_t r = __builtin_amdgcn_ballot_w64(reset), upto = r & ((2ull << lane) - 1);
+    const int first = upto ? 63 - __builtin_clzll(upto) : -1;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const double y = __shfl_up(s, o);
+      if (lane - o >= max(first, 0)) s += y;
+    }
+    __syncthreads();
+    if (lane == 63) edge_sh[wave] = s, reset_sh[wave] = r != 0;
+    __syncthreads();
+    double before = carry;  // at this wave's start
+    for (int w = 0; w < wave; ++w) before = (reset_sh[w] ? 0.0 : before) - edge_sh[w];
+    const double d = (first >= 0 ? 0.0 : before) - (s - mine) - drift * (t - t0);
+    if (in) a.dfg[(int64_t)list * a.T + t] = bf16_bits(reset ? 0.f : (float)d / (1.f + expf(f)));
+    for (int w = wave; w < 4; ++w) before = (reset_sh[w] ? 0.0 : before) - edge_sh[w];
+    carry = before;
+  }
+  for (int t = max(t0, n) + tid; t < t1; t += 256) a.dfg[(int64_t)list * a.T + t] = 0;
+}
+
+// ---------------------------------------------------------------------------
+// One token
+// ---------------------------------------------------------------------------
+
+constexpr int kStepThreads = 512;
+
+// One workgroup per head: the matrix is read, updated, written and multiplied with q in one pass.
+template <int D>
+__global__ __launch_bounds__(kStepThreads) void mlstm_step_kernel(MlstmLaunch a) {
+  constexpr int COLS = D / 4, ROWS = kStepThreads / COLS, PER = D / ROWS, W = kStepThreads / 64;
+  __shared__ __align__(16) float num_sh[W][D];
+  __shared__ float den_sh[W];
+  const int list = blockIdx.x, b = list / a.H, h = list % a.H, tid = threadIdx.x, wave = tid >> 6;
+  uint16_t* o = a.o + (int64_t)list * D;
+  if (a.lens && a.lens[b] <= 0) {
+    if (tid < D) o[tid] = 0;
+    return;
+  }
+  const int col = 4 * (tid % COLS), row0 = tid / COLS;
+  float* C = a.C + (int64_t)list * D * D + col;
+  f32x4 x[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) x[i] = *reinterpret_cast<const f32x4*>(C + (row0 + i * ROWS) * D);
+  const float ig = bf16_value(a.ig.ptr[b * a.ig.sb + h * a.ig.sh]), fg = bf16_value(a.fg.ptr[b * a.fg.sb + h * a.fg.sh]);
+  const uint16_t* q = a.q.ptr + b * a.q.sb + h * a.q.sh;
+  const uint16_t* k = a.k.ptr + b * a.k.sb + h * a.k.sh;
+  const uint16_t* v = a.v.ptr + b * a.v.sb + h * a.v.sh;
+  const float m = a.m_in[list];
+  const double old = fg == neg_inf() ? -__builtin_inf() : (double)m * kLog2e + log2_sigmoid(fg), put = (double)ig * kLog2e;
+  const double now = fmax(old, put);
+  const bool masked = ig == neg_inf();
+  const float keep = gone(old) ? 0.f : pow2(old - now), in = masked ? 0.f : pow2(put - now);
+  float vi[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) vi[j] = masked ? 0.f : in * bf16_value(v[col + j]);
+  f32x4 num = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int row = row0 + i * ROWS;
+    const float kr = masked ? 0.f : bf16_value(k[row]), qr = bf16_value(q[row]);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      x[i][j] = (keep == 0.f ? 0.f : keep * x[i][j]) + kr * vi[j];
+      num[j] += qr * x[i][j];
+    }
+    *reinterpret_cast<f32x4*>(C + row * D) = x[i];
+  }
+  float den = 0.f;
+  if (tid < D) {
+    float* z = a.z + (int64_t)list * D + tid;
+    const float zr = (keep == 0.f ? 0.f : keep * *z) + (masked ? 0.f : in * bf16_value(k[tid]));
+    *z = zr;
+    den = bf16_value(q[tid]) * zr;
+  }
+#pragma unroll
+  for (int s = 32; s > 0; s >>= 1) den += __shfl_xor(den, s);
+#pragma unroll
+  for (int s = COLS; s < 64; s <<= 1)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) num[j] += __shfl_xor(num[j], s);
+  if ((tid & 63) < COLS) *reinterpret_cast<f32x4*>(&num_sh[wave][col]) = num;
+  if ((tid & 63) == 0) den_sh[wave] = den;
+  __syncthreads();
+  if (tid == 0) a.m[list] = (float)(now * kLog2eInv);
+  if (tid >= D) return;
+  float y = 0.f;
+#pragma unroll
+  for (int w = 0; w < W; ++w) y += num_sh[w][tid];
+  if (a.normalize) {
+    den = den_sh[0] + (D > 64 ? den_sh[1] : 0.f);
+    y = den > 0.f ? y / den : den != den ? den : 0.f;
+  } else {
+    y *= a.scale * pow2(now);
+  }
+  o[tid] = bf16_bits(y);
+}
+
+// ---------------------------------------------------------------------------
+// Plans
+// ---------------------------------------------------------------------------
+
+int chunk_count(const MlstmLaunch& L) { return (L.T + kChunk - 1) / kChunk; }
+
+// Segments: enough for two workgroups a CU.
+constexpr int kWantGroups = 512, kFewChunks = 4;
+void plan(MlstmLaunch& L) {
+  const int chunks = chunk_count(L);
+  const int64_t lists = (int64_t)L.B * L.H;
+  int64_t segs = lists >= kWantGroups || chunks <= kFewChunks ? 1 : (kWantGroups + lists - 1) / lists;
+  if (segs > chunks) segs = chunks;
+  L.seg_chunks = (int)((chunks + segs - 1) / segs);
+  L.segs = (chunks + L.seg_chunks - 1) / L.seg_chunks;
+}
+
+template <int D>
+int launch_states(const MlstmLaunch& L, int directions) {
+  const hipStream_t st = (hipStream_t)L.stream;
+  const unsigned lists = (unsigned)L.B * L.H;
+  hipLaunchKernelGGL((mlstm_segment_kernel<D>), dim3(lists * L.segs, directions), dim3(256), 0, st, L);
+  int e = (int)hipGetLastError();
+  if (e != 0) return e;
+  const int blocks = (D * D + D + 1023) / 1024;
+  hipLaunchKernelGGL((mlstm_scan_kernel<D>), dim3(lists * blocks, directions), dim3(256), 0, st, L, blocks);
+  return (int)hipGetLastError();
+}
+
+template <int D>
+int launch_fwd(const MlstmLaunch& L) {
+  if (L.segs > 1) {
+    const int e = launch_states<D>(L, 1);
+    if (e != 0) return e;
+  }
+  hipLaunchKernelGGL((mlstm_kernel<D, kFwd>), dim3((unsigned)(L.B * L.H * L.segs)), dim3(256), 0, (hipStream_t)L.stream, L);
+  return (int)hipGetLastError();
+}
+
+template <int D>
+int launch_bwd(const MlstmLaunch& L) {
+  const hipStream_t st = (hipStream_t)L.stream;
+  const unsigned groups = (unsigned)(L.B * L.H * L.segs);
+  const int64_t rows = (int64_t)L.B * L.H * L.T, per = 256 / (D / 8);
+  int e;
+  hipLaunchKernelGGL((mlstm_dots_kernel<D>), dim3((unsigned)((rows + per - 1) / per)), dim3(256), 0, st, L, rows);
+  if ((e = (int)hipGetLastError()) != 0) return e;
+  if (L.segs > 1 && (e = launch_states<D>(L, 2)) != 0) return e;
+  hipLaunchKernelGGL((mlstm_kernel<D, kDq>), dim3(groups), dim3(256), 0, st, L);
+  if ((e = (int)hipGetLastError()) != 0) return e;
+  hipLaunchKernelGGL((mlstm_kernel<D, kDkv>), dim3(groups), dim3(512), 0, st, L);
+  if ((e = (int)hipGetLastError()) != 0) return e;
+  hipLaunchKernelGGL((mlstm_forget_kernel<D>), dim3(groups), dim3(256), 0, st, L);
+  return (int)hipGetLastError();
+}
+
+// Floats of a direction's parts, rounded up to 16 bytes by segment_floats' own size.
+int64_t part_floats(const MlstmLaunch& L) {
+  return L.segs > 1 ? (int64_t)L.B * L.H * L.segs * segment_floats(L.D) : 0;
+}
+int64_t row_floats(const MlstmLaunch& L) { return ((int64_t)L.B * L.H * L.T + 3) / 4 * 4; }
+
+}  // namespace
+
+int64_t mlstm_threads(const MlstmLaunch& L) { return (int64_t)L.B * L.H * chunk_count(L) * 1024; }
+
+int64_t mlstm_fwd_workspace_floats(MlstmLaunch L) {
+  plan(L);
+  return part_floats(L);
+}
+int64_t mlstm_bwd_workspace_floats(MlstmLaunch L) {
+  plan(L);
+  return 2 * part_floats(L) + 2 * row_floats(L);
+}
+
+int launch_mlstm_fwd(MlstmLaunch L) {
+  plan(L);
+  L.parts = L.workspace;
+  return L.D == 64 ? launch_fwd<64>(L) : launch_fwd<128>(L);
+}
+
+int launch_mlstm_bwd(MlstmLaunch L) {
+  plan(L);
+  L.dots = L.workspace;
+  L.dig32 = L.dots + row_floats(L);
+  L.parts = L.dig32 + row_floats(L);
+  return L.D == 64 ? launch_bwd<64>(L) : launch_bwd<128>(L);
+}
+
+int launch_mlstm_step(const MlstmLaunch& L) {
+  const dim3 grid((unsigned)(L.B * L.H)), block(kStepThreads);
+  if (L.D == 64)
+    hipLaunchKernelGGL((mlstm_step_kernel<64>), grid, block, 0, (hipStream_t)L.stream, L);
+  else
+    hipLaunchKernelGGL((mlstm_step_kernel<128>), grid, block, 0, (hipStream_t)L.stream, L);
+  return (int)hipGetLastError();
+}
+
+}  // namespace kvpop
