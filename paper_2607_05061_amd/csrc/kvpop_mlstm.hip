@@ -175,6 +175,7 @@ struct SegmentScalars {
   double add;   // the exponent of what the segment adds
   double sum;   // log f over the segment, -inf with a reset
   double from;  // the exponent of what it starts from
+  double top;   // forwards: what m is after the segment alone
 };
 __host__ __device__ constexpr int segment_floats(int D) { return D * D + D + 8; }
 __device__ __forceinline__ SegmentScalars* scalars(float* part, int D) {
@@ -210,6 +211,11 @@ __device__ __forceinline__ void clear_rows(uint16_t* sh, const double* weight, i
     if (gone(weight[i / D])) sh[(i / D) * (D + 8) + i % D] = 0;
 }
 
+// What is held carries a power of two, 2^m. It moves with the gates, and beyond that only where a chunk's
+// weights would pass 2^kRoom beside it: bf16 and fp32 have the room, and 64 registers are not multiplied
+// in every chunk.
+constexpr double kRoom = 24.0;
+
 // The exponents of a chunk's update: what is held before (m), after (next), and a token's.
 template <bool REV>
 struct Update {
@@ -219,16 +225,23 @@ struct Update {
   __device__ __forceinline__ Update(const Gates& G, int slot, double m) {
     const int all = G.resets[slot];
     const double old = all == 0 ? m + G.sum[slot] : -__builtin_inf();
-    const double top = REV ? G.top[slot] : G.top[slot] + G.sum[slot];
-    next = fmax(old, top);
-    keep = gone(old) ? 0.f : pow2(old - next);
+    const double top = added(G, slot);
+    next = gone(old) || top > old + kRoom ? top : old;
+    keep = gone(old) ? 0.f : next == old ? 1.f : pow2(old - next);
     shift = gone(next) ? 0.0 : (REV ? -next : G.sum[slot] - next);
     want = REV ? 0 : all;
+  }
+  // The largest exponent that the chunk adds.
+  static __device__ __forceinline__ double added(const Gates& G, int slot) {
+    return REV ? G.top[slot] : G.top[slot] + G.sum[slot];
   }
   __device__ __forceinline__ float weight(const Gates& G, int i) const {
     return G.rid[i] == want ? pow2((REV ? G.r[i] : G.u[i]) + shift) : 0.f;
   }
 };
+
+// m as the header defines it: after a chunk or a segment.
+__device__ __forceinline__ double held_m(double m, double sum, double top) { return fmax(m + sum, top); }
 
 // S <- keep S + B^T (w o C) on this wave's NT * 16 columns of C. w o C is taken as the sum of two bf16
 // (16 bits), so that what is held keeps fp32's meaning; rounded once, it would be off by 2^-9.
@@ -236,20 +249,31 @@ template <int D, int NT>
 __device__ __forceinline__ void update_state(f32x4 (&S)[D / 16][NT], float keep, const uint16_t* b_sh,
                                              const bf16x8 (&cf)[2][NT], const float* w_sh, int g, int c) {
   constexpr int LS = D + 8;
-  bf16x8 hi[2][NT], lo[2][NT];
+  Frag hi[2][NT], lo[2][NT];
 #pragma unroll
   for (int s = 0; s < 2; ++s) {
     float w[8];
     *reinterpret_cast<f32x4*>(w) = *reinterpret_cast<const f32x4*>(w_sh + 32 * s + 8 * g);
     *reinterpret_cast<f32x4*>(w + 4) = *reinterpret_cast<const f32x4*>(w_sh + 32 * s + 8 * g + 4);
 #pragma unroll
-    for (int t = 0; t < NT; ++t)
+    for (int t = 0; t < NT; ++t) {
+      Frag v;
+      v.v = cf[s][t];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float x = (float)cf[s][t][i] * w[i];
-        hi[s][t][i] = (__bf16)x;
-        lo[s][t][i] = (__bf16)(x - (float)hi[s][t][i]);
+      for (int i = 0; i < 4; ++i) {
+        const float x = __uint_as_float(v.u[i] << 16) * w[2 * i], y = __uint_as_float(v.u[i] & 0xFFFF0000u) * w[2 * i + 1];
+        const uint32_t a = __float_as_uint(x), b = __float_as_uint(y);
+        hi[s][t].u[i] = __builtin_amdgcn_perm(b, a, 0x07060302u);  // cut off, not rounded: the rest is the low part
+        lo[s][t].v[2 * i] = (__bf16)(x - __uint_as_float(a & 0xFFFF0000u));
+        lo[s][t].v[2 * i + 1] = (__bf16)(y - __uint_as_float(b & 0xFFFF0000u));
       }
+    }
+  }
+  if (keep != 1.f) {  // what is forgotten may be anything
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+      for (int t = 0; t < NT; ++t) S[i][t] = keep == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : S[i][t] * keep;
   }
 #pragma unroll
   for (int i = 0; i < D / 16; ++i) {
@@ -258,34 +282,45 @@ __device__ __forceinline__ void update_state(f32x4 (&S)[D / 16][NT], float keep,
     for (int s = 0; s < 2; ++s) bf[s] = column8(b_sh + 32 * s * LS + 16 * i, LS, g, c);
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      S[i][t] = keep == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : S[i][t] * keep;  // what is forgotten may be anything
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
-        S[i][t] = mfma(bf[s], hi[s][t], S[i][t]);
-        S[i][t] = mfma(bf[s], lo[s][t], S[i][t]);
+        S[i][t] = mfma(bf[s], hi[s][t].v, S[i][t]);
+        S[i][t] = mfma(bf[s], lo[s][t].v, S[i][t]);
       }
     }
   }
 }
 
-// sum_t w_t b_t over the 16 columns of B at b_sh, row 4 g + r of them: columns 0 and 1 of a product whose other
-// operand is (w's high part, its low part).
-template <int D>
-__device__ __forceinline__ f32x4 weighted_rows(const uint16_t* b_sh, const float* w_sh, int g, int c) {
-  f32x4 z = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-  for (int s = 0; s < 2; ++s) {
-    bf16x8 wf;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float w = w_sh[32 * s + 8 * g + i], hi = (float)(__bf16)w;
-      wf[i] = (__bf16)(c == 0 ? w : c == 1 ? w - hi : 0.f);
-    }
-    z = mfma(column8(b_sh + 32 * s * (D + 8), D + 8, g, c), wf, z);
+// Weights as an operand of two columns: the high and the low bf16 part.
+struct Weights {
+  static constexpr int kStride = kChunk + 8;
+  uint16_t part[2 * kStride];
+  __device__ __forceinline__ void set(int i, float w) {
+    const float hi = (float)(__bf16)w;
+    part[i] = bf16_bits(w);
+    part[kStride + i] = bf16_bits(w - hi);
   }
+  __device__ __forceinline__ bf16x8 frag(int s, int g, int c) const { return row8(part + (c & 1) * kStride + 32 * s + 8 * g); }
+};
+
+// The two columns' sum, in lanes of even c.
+__device__ __forceinline__ f32x4 both_columns(f32x4 z) {
 #pragma unroll
   for (int r = 0; r < 4; ++r) z[r] += __shfl_xor(z[r], 1);
   return z;
+}
+
+// sum_t w_t b_t over the 16 columns of B at b_sh: rows 4 g + r of them.
+template <int D>
+__device__ __forceinline__ f32x4 weighted_rows(const uint16_t* b_sh, const Weights& w, int g, int c) {
+  f32x4 z = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int s = 0; s < 2; ++s) z = mfma(column8(b_sh + 32 * s * (D + 8), D + 8, g, c), w.frag(s, g, c), z);
+  return both_columns(z);
+}
+
+__device__ __forceinline__ f32x4 scaled(f32x4 x, float keep) {
+  return keep == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : x * keep;
 }
 
 // ---------------------------------------------------------------------------
@@ -295,11 +330,12 @@ __device__ __forceinline__ f32x4 weighted_rows(const uint16_t* b_sh, const float
 // One workgroup per segment of a head and direction (blockIdx.y: 0 forwards, k and v; 1 backwards, q
 // and do). Wave w holds columns [w D / 4, (w + 1) D / 4) of the matrix.
 template <int D>
-__global__ __launch_bounds__(256) void mlstm_segment_kernel(MlstmLaunch a) {
+__global__ __launch_bounds__(256, 2) void mlstm_segment_kernel(MlstmLaunch a) {
   constexpr int NT = D / 64, LS = D + 8, NZ = D / 64;
   __shared__ __align__(16) uint16_t b_sh[kChunk * LS], c_sh[kChunk * LS];
   __shared__ Gates G;
-  __shared__ __align__(16) float w_sh[kChunk], wz_sh[kChunk];
+  __shared__ __align__(16) float w_sh[kChunk];
+  __shared__ __align__(16) Weights wz;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, c = lane & 15;
   const int seg = blockIdx.x % a.segs, list = blockIdx.x / a.segs, b = list / a.H, h = list % a.H;
   const int n = a.lens ? clampi(a.lens[b], 0, a.T) : a.T, chunks = (n + kChunk - 1) / kChunk;
@@ -317,7 +353,7 @@ __global__ __launch_bounds__(256) void mlstm_segment_kernel(MlstmLaunch a) {
   f32x4 z[NZ];
 #pragma unroll
   for (int j = 0; j < NZ; ++j) z[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  double m = -__builtin_inf(), sum = 0.0;
+  double m = -__builtin_inf(), sum = 0.0, top = -__builtin_inf();
   auto chunk_at = [&](int i) { return rev ? first + count - 1 - i : first + i; };
 
   Tile<D, 256> tb, tc;
@@ -350,11 +386,20 @@ __global__ __launch_bounds__(256) void mlstm_segment_kernel(MlstmLaunch a) {
     if (rev) {
       const Update<true> up(G, slot, m);
       next = up.next, keep = up.keep;
-      if (tid < kChunk) w_sh[tid] = up.weight(G, slot * kChunk + tid), wz_sh[tid] = w_sh[tid] * G.d[slot * kChunk + tid];
+      if (tid < kChunk) {
+        const float w = up.weight(G, slot * kChunk + tid);
+        w_sh[tid] = w;
+        wz.set(tid, w * G.d[slot * kChunk + tid]);
+      }
     } else {
       const Update<false> up(G, slot, m);
       next = up.next, keep = up.keep;
-      if (tid < kChunk) wz_sh[tid] = w_sh[tid] = up.weight(G, slot * kChunk + tid);
+      if (tid < kChunk) {
+        const float w = up.weight(G, slot * kChunk + tid);
+        w_sh[tid] = w;
+        wz.set(tid, w);
+      }
+      top = held_m(top, G.resets[slot] ? -__builtin_inf() : G.sum[slot], up.added(G, slot));
     }
     sum = G.resets[slot] ? -__builtin_inf() : sum + G.sum[slot];
     __syncthreads();
@@ -366,8 +411,8 @@ __global__ __launch_bounds__(256) void mlstm_segment_kernel(MlstmLaunch a) {
     update_state<D, NT>(S, keep, b_sh, cf, w_sh, g, c);
 #pragma unroll
     for (int j = 0; j < NZ; ++j) {
-      const f32x4 add = weighted_rows<D>(b_sh + (wave * NZ + j) * 16, wz_sh, g, c);
-      z[j] = (keep == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : z[j] * keep) + add;
+      const f32x4 add = weighted_rows<D>(b_sh + (wave * NZ + j) * 16, wz, g, c);
+      z[j] = scaled(z[j], keep) + add;
     }
     m = next;
     __syncthreads();
@@ -388,6 +433,7 @@ __global__ __launch_bounds__(256) void mlstm_segment_kernel(MlstmLaunch a) {
   if (tid == 0) {
     scalars(part, D)->add = m;
     scalars(part, D)->sum = sum;
+    scalars(part, D)->top = top;
     if (seg == (rev ? a.segs - 1 : 0)) scalars(part, D)->from = !rev && a.C ? (double)a.m_in[list] * kLog2e : -__builtin_inf();
   }
 }
@@ -413,7 +459,7 @@ __global__ __launch_bounds__(256) void mlstm_scan_kernel(MlstmLaunch a, int bloc
   constexpr int kAhead = 4;  // parts on their way
   f32x4 next[kAhead];
   auto part = [&](int i) { return parts + (int64_t)(rev ? a.segs - 1 - i : i) * segment_floats(D); };
-  double m = scalars(part(0), D)->from;
+  double m = scalars(part(0), D)->from, defined = m;
 #pragma unroll
   for (int j = 0; j < kAhead; ++j)
     if (j < a.segs) next[j] = *reinterpret_cast<const f32x4*>(part(j) + e);
@@ -433,11 +479,12 @@ __global__ __launch_bounds__(256) void mlstm_scan_kernel(MlstmLaunch a, int bloc
 #pragma unroll
       for (int r = 0; r < 4; ++r) x[r] = (keep == 0.f ? 0.f : x[r] * keep) + add[r] * put;
       m = now;
+      defined = held_m(defined, s->sum, s->top);
     }
   }
   if (held) {
-    *reinterpret_cast<f32x4*>(held) = x;
-    if (e == 0) a.m[list] = (float)(m * kLog2eInv);
+    *reinterpret_cast<f32x4*>(held) = gone(m) ? x : x * pow2(m - defined);
+    if (e == 0) a.m[list] = (float)(defined * kLog2eInv);
   }
 }
 
@@ -451,7 +498,9 @@ struct Shared {
   __align__(16) uint16_t tile[kTiles][kChunk * (D + 8)];
   __align__(16) uint16_t p[kRoles][kChunk * (kChunk + 8)];
   Gates G;
-  __align__(16) float w[kChunk], wz[kChunk];
+  __align__(16) float w[kChunk];
+  __align__(16) Weights wz;
+  __align__(16) uint16_t zrow[MODE == kFwd ? 2 * (D + 8) : 8];  // z's high and low bf16 parts
   __align__(16) float far[kRoles][kChunk], far_z[kRoles][kChunk], out[kChunk];
   __align__(16) float z[kRoles][D];
   float dig[4][kChunk];
@@ -463,7 +512,7 @@ struct Shared {
 // serves as an operand from the registers that accumulate it (its rows are the contraction, in the
 // order of two accumulator tiles' rows) and a lane's outputs are 4 neighbours of a row.
 template <int D, int MODE>
-__global__ __launch_bounds__(MODE == kDkv ? 512 : 256) void mlstm_kernel(MlstmLaunch a) {
+__global__ __launch_bounds__(MODE == kDkv ? 512 : 256, 2) void mlstm_kernel(MlstmLaunch a) {
   constexpr bool REV = MODE == kDkv;
   constexpr int NT = D / 64, LS = D + 8, PS = kChunk + 8, NZ = D / 64, THREADS = REV ? 512 : 256;
   __shared__ Shared<D, MODE> sh;
@@ -510,7 +559,20 @@ __global__ __launch_bounds__(MODE == kDkv ? 512 : 256) void mlstm_kernel(MlstmLa
         const int row = 16 * i + 4 * g + r, col = (wave * NT + t) * 16 + c;
         S[i][t][r] = from_S ? from_S[turned ? col * D + row : row * D + col] : 0.f;
       }
-  if ((tid & 255) < D) sh.z[role][tid & 255] = from_z ? from_z[tid & 255] : 0.f;
+  auto set_zrow = [&](int i, float z) __attribute__((always_inline)) {
+    const float hi = (float)(__bf16)z;
+    sh.zrow[i] = bf16_bits(z);
+    sh.zrow[LS + i] = bf16_bits(z - hi);
+  };
+  if ((tid & 255) < D) {
+    const float z = from_z ? from_z[tid & 255] : 0.f;
+    sh.z[role][tid & 255] = z;
+    if (MODE == kFwd) set_zrow(tid, z);
+  }
+  double defined = m;
+
+  // Where this lane's outputs go, from time 0 on.
+  uint16_t* out_at = out + ((int64_t)list * a.T + c - (REV ? 0 : a.delay)) * D + wave * NT * 16 + 4 * g;
 
   Tile<D, THREADS> t0, t1, t2, t3;
   auto load = [&](int chunk) __attribute__((always_inline)) {
@@ -551,7 +613,7 @@ __global__ __launch_bounds__(MODE == kDkv ? 512 : 256) void mlstm_kernel(MlstmLa
     if (tid < kChunk) {
       const float w = up.weight(G, at + tid);
       sh.w[tid] = w;
-      sh.wz[tid] = REV ? w * G.d[at + tid] : w;
+      sh.wz.set(tid, REV ? w * G.d[at + tid] : w);
     }
     {  // The masked product, transposed: this lane has row j and columns 4 g + r of each 16.
       const int j = 16 * wave + c, rid = G.rid[at + j];
@@ -598,12 +660,10 @@ __global__ __launch_bounds__(MODE == kDkv ? 512 : 256) void mlstm_kernel(MlstmLa
         *reinterpret_cast<bf16x4*>(sh.p[role] + j * PS + 16 * kt + 4 * g) = p;
       }
       if (MODE == kFwd) {
-        float qz = 0.f;
+        f32x4 qz = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int s = 0; s < D / 32; ++s)
-#pragma unroll
-          for (int i = 0; i < 8; ++i) qz += (float)af[s][i] * sh.z[0][32 * s + 8 * g + i];
-        den = sum_groups(den + (far == 0.f ? 0.f : far * qz)) * a.scale;
+        for (int s = 0; s < D / 32; ++s) qz = mfma(row8(sh.zrow + (c & 1) * LS + 32 * s + 8 * g), af[s], qz);
+        den = (sum_groups(den) + (far == 0.f ? 0.f : far * (qz[0] + qz[1]))) * a.scale;
         const double e = G.b[at + j] - rho;  // that of the row's common factor
         float fac, lse;
         if (a.normalize) {
@@ -656,6 +716,7 @@ __global__ __launch_bounds__(MODE == kDkv ? 512 : 256) void mlstm_kernel(MlstmLa
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       const int j = 16 * q + c, time = chunk * kChunk + j;
+      uint16_t* out_row = out_at + (chunk * (int64_t)kChunk + 16 * q) * D;
       const float far = sh.far[role][j], fac = MODE == kFwd ? sh.out[j] : a.scale;
       const float far_z = MODE != kFwd && with_z ? sh.far_z[role][j] : 0.f;
       float dot = 0.f;
@@ -679,9 +740,13 @@ __global__ __launch_bounds__(MODE == kDkv ? 512 : 256) void mlstm_kernel(MlstmLa
         for (int r = 0; r < 4; ++r) {
           const float x = acc[q][t][r] * fac;
           y[r] = (__bf16)x;
-          if (REV) dot += x * bf16_value(sh.tile[0][j * LS + col + r]);
         }
-        if (live) *reinterpret_cast<bf16x4*>(out + (((int64_t)b * a.H + h) * a.T + row) * D + col) = y;
+        if (REV && role) {
+          const bf16x4 kr = *reinterpret_cast<const bf16x4*>(sh.tile[0] + j * LS + col);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) dot += acc[q][t][r] * fac * (float)kr[r];
+        }
+        if (live) *reinterpret_cast<bf16x4*>(out_row + 16 * t) = y;
       }
       if (REV && role) {
         dot = sum_groups(dot);
@@ -693,23 +758,26 @@ __global__ __launch_bounds__(MODE == kDkv ? 512 : 256) void mlstm_kernel(MlstmLa
     if (MODE == kFwd) {
 #pragma unroll
       for (int i = 0; i < NZ; ++i) {
-        const f32x4 add = weighted_rows<D>(b_sh + (wave * NZ + i) * 16, sh.w, g, c);
-        float* z = sh.z[0] + (wave * NZ + i) * 16 + 4 * g;
-        if (c == 0)
+        const int at_z = (wave * NZ + i) * 16 + 4 * g;
+        const f32x4 add = weighted_rows<D>(b_sh + (wave * NZ + i) * 16, sh.wz, g, c);
+        f32x4* z = reinterpret_cast<f32x4*>(sh.z[0] + at_z);
+        if (c == 0) {
+          const f32x4 y = scaled(*z, up.keep) + add;
+          *z = y;
 #pragma unroll
-          for (int r = 0; r < 4; ++r) z[r] = (up.keep == 0.f ? 0.f : z[r] * up.keep) + add[r];
+          for (int r = 0; r < 4; ++r) set_zrow(at_z + r, y[r]);
+        }
       }
+      defined = held_m(defined, G.resets[slot] ? -__builtin_inf() : G.sum[slot], up.added(G, slot));
     } else if (with_z) {  // a vector over this wave's own columns: sum w_t c_t
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
-        float x = 0.f;
+        f32x4 add = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int s = 0; s < 2; ++s)
-#pragma unroll
-          for (int i = 0; i < 8; ++i) x += (float)cf[s][t][i] * sh.wz[32 * s + 8 * g + i];
-        x = sum_groups(x);
-        float* z = sh.z[role] + (wave * NT + t) * 16 + c;
-        if (g == 0) *z = (up.keep == 0.f ? 0.f : *z * up.keep) + x;
+        for (int s = 0; s < 2; ++s) add = mfma(cf[s][t], sh.wz.frag(s, g, c), add);
+        add = both_columns(add);
+        f32x4* z = reinterpret_cast<f32x4*>(sh.z[role] + (wave * NT + t) * 16 + 4 * g);
+        if (c == 0) *z = scaled(*z, up.keep) + add;
       }
     }
     m = up.next;
@@ -735,15 +803,16 @@ __global__ __launch_bounds__(MODE == kDkv ? 512 : 256) void mlstm_kernel(MlstmLa
   }
 
   if (MODE == kFwd && a.segs == 1 && a.C) {
+    const float out_scale = gone(m) ? 1.f : pow2(m - defined);
 #pragma unroll
     for (int i = 0; i < D / 16; ++i)
 #pragma unroll
       for (int t = 0; t < NT; ++t)
 #pragma unroll
         for (int r = 0; r < 4; ++r)
-          a.C[(int64_t)list * D * D + (16 * i + 4 * g + r) * D + (wave * NT + t) * 16 + c] = S[i][t][r];
-    if (tid < D) a.z[(int64_t)list * D + tid] = sh.z[0][tid];
-    if (tid == 0) a.m[list] = (float)(m * kLog2eInv);
+          a.C[(int64_t)list * D * D + (16 * i + 4 * g + r) * D + (wave * NT + t) * 16 + c] = S[i][t][r] * out_scale;
+    if (tid < D) a.z[(int64_t)list * D + tid] = sh.z[0][tid] * out_scale;
+    if (tid == 0) a.m[list] = (float)(defined * kLog2eInv);
   }
 }
 
