@@ -27,6 +27,8 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef double f64x2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
 
 constexpr double kLog2e = 1.4426950408889634074, kLog2eInv = 0.69314718055994530942;
@@ -93,7 +95,7 @@ __device__ __forceinline__ bf16x8 column8(const uint16_t* at, int stride, int g,
 // ---------------------------------------------------------------------------
 
 // Of kBlock chunks, in units of log2, running sums from each chunk's start.
-struct Gates {
+struct __align__(16) Gates {
   double u[kGates];    // ig - b
   double r[kGates];    // kFwd: the largest u since the last reset; else b - lse (-inf: not read)
   double b[kGates];
@@ -182,7 +184,8 @@ __device__ __forceinline__ SegmentScalars* scalars(float* part, int D) {
   return reinterpret_cast<SegmentScalars*>(part + D * D + D);
 }
 
-// One array's chunks of rows, on their way to LDS. Rows at times outside [first, n) are zeros.
+// One array's chunks of rows, on their way to LDS. Rows at times outside [shift, n) are zeros; their
+// loads go to a row that is there, so that no load waits for a comparison.
 template <int D, int THREADS>
 struct Tile {
   static constexpr int kPer = kChunk * D / 8 / THREADS;
@@ -190,17 +193,24 @@ struct Tile {
   u32x4 x[kPer];
   __device__ __forceinline__ void load(const Rows& a, int b, int h, int t0, int shift, int n, int tid) {
     const uint16_t* p = a.ptr + b * a.sb + h * a.sh + 8 * (tid % (D / 8));
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      const int t = t0 + tid / (D / 8) + i * (THREADS * 8 / D);
-      x[i] = u32x4{0, 0, 0, 0};
-      if (t >= shift && t < n) x[i] = *reinterpret_cast<const u32x4*>(p + (int64_t)(t - shift) * a.st);
-    }
-  }
-  __device__ __forceinline__ void store(uint16_t* sh, int tid) const {
+    const int first = t0 - shift + tid / (D / 8);
 #pragma unroll
     for (int i = 0; i < kPer; ++i)
-      *reinterpret_cast<u32x4*>(sh + (tid / (D / 8) + i * (THREADS * 8 / D)) * kStride + 8 * (tid % (D / 8))) = x[i];
+      x[i] = *reinterpret_cast<const u32x4*>(p + min(max(first + i * (THREADS * 8 / D), 0), n - 1) * a.st);
+  }
+  __device__ __forceinline__ void store(uint16_t* sh, int t0, int shift, int n, int tid) const {
+    const int row = tid / (D / 8);
+    uint16_t* to = sh + row * kStride + 8 * (tid % (D / 8));
+    if (t0 >= shift && t0 + kChunk <= n) {
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) *reinterpret_cast<u32x4*>(to + i * (THREADS * 8 / D) * kStride) = x[i];
+    } else {
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        const int t = t0 + row + i * (THREADS * 8 / D);
+        *reinterpret_cast<u32x4*>(to + i * (THREADS * 8 / D) * kStride) = t >= shift && t < n ? x[i] : u32x4{0, 0, 0, 0};
+      }
+    }
   }
 };
 
@@ -369,8 +379,8 @@ __global__ __launch_bounds__(256, 2) void mlstm_segment_kernel(MlstmLaunch a) {
       else
         chunk_gates<kFwd>(a, G, b, h, n, chunk_at(i + wave), wave, lane);
     }
-    tb.store(b_sh, tid);
-    tc.store(c_sh, tid);
+    tb.store(b_sh, chunk_at(i) * kChunk, shift, n, tid);
+    tc.store(c_sh, chunk_at(i) * kChunk, shift, n, tid);
     __syncthreads();
     if (rev ? G.odd_q[slot] : G.odd_k[slot]) {
       clear_rows<D>(b_sh, (rev ? G.r : G.u) + slot * kChunk, tid, 256);
@@ -586,10 +596,10 @@ __global__ __launch_bounds__(MODE == kDkv ? 512 : 256, 2) void mlstm_kernel(Mlst
   for (int it = 0; it < count; ++it) {
     const int chunk = chunk_at(it), slot = it % kBlock, at = slot * kChunk;
     if (slot == 0 && role == 0 && it + wave < count) chunk_gates<MODE>(a, G, b, h, n, chunk_at(it + wave), wave, lane);
-    t0.store(sh.tile[0], tid);
-    t1.store(sh.tile[1], tid);
-    t2.store(sh.tile[2], tid);
-    if (REV) t3.store(sh.tile[REV ? 3 : 0], tid);
+    t0.store(sh.tile[0], chunk * kChunk, late0, n, tid);
+    t1.store(sh.tile[1], chunk * kChunk, 0, n, tid);
+    t2.store(sh.tile[2], chunk * kChunk, late2, n, tid);
+    if (REV) t3.store(sh.tile[REV ? 3 : 0], chunk * kChunk, a.delay, n, tid);
     __syncthreads();
     if (G.odd_k[slot] | (MODE != kFwd ? G.odd_q[slot] : 0)) {
       if (MODE == kFwd) {
@@ -635,29 +645,44 @@ __global__ __launch_bounds__(MODE == kDkv ? 512 : 256, 2) void mlstm_kernel(Mlst
 #pragma unroll
       for (int s = 0; s < D / 32; ++s) af[s] = row8(a_sh + j * LS + 32 * s + 8 * g);
       float den = 0.f;
-      const int k0 = REV ? wave & ~1 : 0, k1 = REV ? 4 : (wave | 1) + 1;
+      const bool plain = G.resets[slot] == 0;
+      // Two tiles of 16 columns at a time: all that the product with C takes, the further ones as zeros.
 #pragma unroll
-      for (int kt = 0; kt < 4; ++kt) {
-        if (kt < k0 || kt >= k1) continue;
-        bf16x4 p = {(__bf16)0.f, (__bf16)0.f, (__bf16)0.f, (__bf16)0.f};
-        if (REV ? kt >= wave : kt <= wave) {
-          f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+      for (int half = 0; half < 2; ++half) {
+        if (REV ? half < wave / 2 : half > wave / 2) continue;
+        f32x4 acc[2];
 #pragma unroll
-          for (int s = 0; s < D / 32; ++s) acc = mfma(row8(b_sh + (16 * kt + c) * LS + 32 * s + 8 * g), af[s], acc);
+        for (int x = 0; x < 2; ++x) {
+          const int kt = 2 * half + x, key = 16 * kt + 4 * g;
+          const f64x2* ex = reinterpret_cast<const f64x2*>((REV ? G.r : G.u) + at + key);
+          const f64x2 e0 = ex[0], e1 = ex[1];
+          acc[x] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int s = 0; s < D / 32; ++s) acc[x] = mfma(row8(b_sh + (16 * kt + c) * LS + 32 * s + 8 * g), af[s], acc[x]);
+          const f32x4 w = {pow2(e0.x + rho), pow2(e0.y + rho), pow2(e1.x + rho), pow2(e1.y + rho)};
+          if (MODE == kDq) acc[x] += alpha;
+          if (REV && role) acc[x] += *reinterpret_cast<const f32x4*>(G.d + at + key);
+          acc[x] *= w;
+#pragma unroll
+          for (int r = 0; r < 4; ++r) acc[x][r] = (REV ? key + r >= j : key + r <= j) ? acc[x][r] : 0.f;
+        }
+        if (!plain)
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            const i32x4 other = *reinterpret_cast<const i32x4*>(G.rid + at + 32 * half + 16 * x + 4 * g);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) acc[x][r] = other[r] == rid ? acc[x][r] : 0.f;
+          }
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          bf16x4 p;
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            const int key = 16 * kt + 4 * g + r;
-            const bool in = (REV ? key >= j : key <= j) && G.rid[at + key] == rid;
-            const double e = (REV ? G.r[at + key] : G.u[at + key]) + rho;
-            float x = acc[r];
-            if (MODE == kDq) x += alpha;
-            if (REV && role) x += G.d[at + key];
-            x = in ? x * pow2(e) : 0.f;
-            den += x;
-            p[r] = (__bf16)x;
+            den += acc[x][r];
+            p[r] = (__bf16)acc[x][r];
           }
+          *reinterpret_cast<bf16x4*>(sh.p[role] + j * PS + 32 * half + 16 * x + 4 * g) = p;
         }
-        *reinterpret_cast<bf16x4*>(sh.p[role] + j * PS + 16 * kt + 4 * g) = p;
       }
       if (MODE == kFwd) {
         f32x4 qz = {0.f, 0.f, 0.f, 0.f};
@@ -713,45 +738,45 @@ __global__ __launch_bounds__(MODE == kDkv ? 512 : 256, 2) void mlstm_kernel(Mlst
         for (int t = 0; t < NT; ++t) acc[q][t] = mfma(sf[t], af, acc[q][t]);
       }
     }
+    bf16x4 y[4][NT];
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      const int j = 16 * q + c, time = chunk * kChunk + j;
-      uint16_t* out_row = out_at + (chunk * (int64_t)kChunk + 16 * q) * D;
+      const int j = 16 * q + c;
       const float far = sh.far[role][j], fac = MODE == kFwd ? sh.out[j] : a.scale;
       const float far_z = MODE != kFwd && with_z ? sh.far_z[role][j] : 0.f;
       float dot = 0.f;
-      const int row = REV ? time : time - a.delay;
-      const bool live = time < n && row >= 0;
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
         const int col = (wave * NT + t) * 16 + 4 * g;
-        acc[q][t] = far == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : acc[q][t] * far;
-        if (MODE != kFwd && with_z) {
-          const f32x4 z = *reinterpret_cast<const f32x4*>(sh.z[role] + col);
-#pragma unroll
-          for (int r = 0; r < 4; ++r) acc[q][t][r] += far_z == 0.f ? 0.f : far_z * z[r];
-        }
+        acc[q][t] = scaled(acc[q][t], far);
+        if (MODE != kFwd && with_z) acc[q][t] += scaled(*reinterpret_cast<const f32x4*>(sh.z[role] + col), far_z);
 #pragma unroll
         for (int s = 0; s < 2; ++s)
           if (REV ? 32 * s + 31 >= 16 * q : 32 * s <= 16 * q)
             acc[q][t] = mfma(cf[s][t], row8(sh.p[role] + j * PS + 32 * s + 8 * g), acc[q][t]);
-        bf16x4 y;
+        acc[q][t] *= fac;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const float x = acc[q][t][r] * fac;
-          y[r] = (__bf16)x;
-        }
-        if (REV && role) {
+        for (int r = 0; r < 4; ++r) y[q][t][r] = (__bf16)acc[q][t][r];
+        if (REV) {
           const bf16x4 kr = *reinterpret_cast<const bf16x4*>(sh.tile[0] + j * LS + col);
 #pragma unroll
-          for (int r = 0; r < 4; ++r) dot += acc[q][t][r] * fac * (float)kr[r];
+          for (int r = 0; r < 4; ++r) dot += acc[q][t][r] * (float)kr[r];
         }
-        if (live) *reinterpret_cast<bf16x4*>(out_row + 16 * t) = y;
       }
-      if (REV && role) {
+      if (REV) {
         dot = sum_groups(dot);
-        if (g == 0) sh.dig[wave][j] = dot;
+        if (g == 0 && role) sh.dig[wave][j] = dot;
       }
+    }
+    {
+      const int late = REV ? 0 : a.delay, t0 = chunk * kChunk;
+      uint16_t* to = out_at + (int64_t)t0 * D;
+      const bool whole = t0 >= late && t0 + kChunk <= n;
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        if (whole || (t0 + 16 * q + c >= late && t0 + 16 * q + c < n))
+#pragma unroll
+          for (int t = 0; t < NT; ++t) *reinterpret_cast<bf16x4*>(to + 16 * q * D + 16 * t) = y[q][t];
     }
 
     update_state<D, NT>(S, up.keep, b_sh, cf, sh.w, g, c);
