@@ -160,6 +160,7 @@ struct MlstmLaunch {
   int32_t segs, seg_chunks; // segments of each head and their chunks of 64 tokens
   float* parts;             // [directions, B, H, segs] parts
   float *dots, *dig32;      // backward: [B, H, T]
+  double* edges;            // backward: [B, H, segs]
 };
 
 int launch_mlstm_fwd(MlstmLaunch L);

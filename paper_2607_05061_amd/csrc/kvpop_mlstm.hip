@@ -59,6 +59,43 @@ __device__ __forceinline__ float sum_groups(float x) {
   return x + __shfl_xor(x, 32);
 }
 
+// A lane's value from lanes before it, without LDS: row_shr within 16 lanes, then the last lane of the row (of the
+// two rows) before. CTRL 0x110 + n: n lanes back; 0x142, 0x143: the broadcasts. Lanes without a source get `none`.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double moved(double x, double none) {
+  union { double d; int i[2]; } a, b;
+  a.d = x, b.d = none;
+  a.i[0] = __builtin_amdgcn_update_dpp(b.i[0], a.i[0], CTRL, ROWS, 0xf, false);
+  a.i[1] = __builtin_amdgcn_update_dpp(b.i[1], a.i[1], CTRL, ROWS, 0xf, false);
+  return a.d;
+}
+// Running sum over the wave.
+__device__ __forceinline__ double wave_sums(double x) {
+  x += moved<0x111, 0xf>(x, 0.0);
+  x += moved<0x112, 0xf>(x, 0.0);
+  x += moved<0x114, 0xf>(x, 0.0);
+  x += moved<0x118, 0xf>(x, 0.0);
+  x += moved<0x142, 0xa>(x, 0.0);
+  return x + moved<0x143, 0xc>(x, 0.0);
+}
+// Running maximum over the wave.
+__device__ __forceinline__ double wave_maxima(double x) {
+  const double none = -__builtin_inf();
+  x = fmax(x, moved<0x111, 0xf>(x, none));
+  x = fmax(x, moved<0x112, 0xf>(x, none));
+  x = fmax(x, moved<0x114, 0xf>(x, none));
+  x = fmax(x, moved<0x118, 0xf>(x, none));
+  x = fmax(x, moved<0x142, 0xa>(x, none));
+  return fmax(x, moved<0x143, 0xc>(x, none));
+}
+__device__ __forceinline__ double last_lane(double x) {
+  union { double d; int i[2]; } a;
+  a.d = x;
+  a.i[0] = __builtin_amdgcn_readlane(a.i[0], 63);
+  a.i[1] = __builtin_amdgcn_readlane(a.i[1], 63);
+  return a.d;
+}
+
 // log2 sigmoid(x); 0 for +inf.
 __device__ __forceinline__ double log2_sigmoid(float x) {
   return -(double)(fmaxf(-x, 0.f) + log1pf(expf(-fabsf(x)))) * kLog2e;
@@ -107,56 +144,61 @@ struct __align__(16) Gates {
   int odd_k[kBlock], odd_q[kBlock];  // tokens whose k, v (q, do) have no weight
 };
 
+// A token's gates on their way (and, backward, what its query's read-out left).
+template <int MODE>
+struct RawGates {
+  uint16_t ig, fg;
+  float lse, dot;
+  // The wave's chunk; any token that is there stands for those outside [0, n).
+  __device__ __forceinline__ void load(const MlstmLaunch& a, int b, int h, int n, int chunk, int lane) {
+    const int t = min(chunk * kChunk + lane, n - 1);
+    ig = a.ig.ptr[b * a.ig.sb + h * a.ig.sh + t * a.ig.st];
+    fg = a.fg.ptr[b * a.fg.sb + h * a.fg.sh + t * a.fg.st];
+    if (MODE != kFwd) {
+      const int64_t row = ((int64_t)b * a.H + h) * a.T + max(t - a.delay, 0);
+      lse = a.lse[row];
+      dot = a.dots[row];
+    }
+  }
+};
+
 // The wave's chunk into place `slot`.
 template <int MODE>
-__device__ __forceinline__ void chunk_gates(const MlstmLaunch& a, Gates& G, int b, int h, int n, int chunk, int slot,
-                                            int lane) {
+__device__ __forceinline__ void chunk_gates(const MlstmLaunch& a, Gates& G, const RawGates<MODE>& raw, int n, int chunk,
+                                            int slot, int lane) {
   const int t = chunk * kChunk + lane, i = slot * kChunk + lane;
-  const bool in = t < n;
-  float ig = neg_inf(), fg = -neg_inf();
-  if (in) {
-    ig = bf16_value(a.ig.ptr[b * a.ig.sb + h * a.ig.sh + t * a.ig.st]);
-    fg = bf16_value(a.fg.ptr[b * a.fg.sb + h * a.fg.sh + t * a.fg.st]);
-  }
-  const bool read = in && t >= a.delay;
-  float lse = neg_inf(), dot = 0.f;
-  if (MODE != kFwd && read) {
-    const int64_t row = ((int64_t)b * a.H + h) * a.T + t - a.delay;
-    lse = a.lse[row];
-    if (a.normalize) dot = -a.dots[row];
-  }
+  const bool in = t < n, read = in && t >= a.delay;
+  const float ig = in ? bf16_value(raw.ig) : neg_inf(), fg = in ? bf16_value(raw.fg) : -neg_inf();
   const bool reset = fg == neg_inf();
   const uint64_t resets = __builtin_amdgcn_ballot_w64(reset), mine = resets & ((2ull << lane) - 1);
   const int rid = __builtin_popcountll(mine), all = __builtin_popcountll(resets);
-  double s = reset ? 0.0 : log2_sigmoid(fg);
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const double y = __shfl_up(s, o);
-    if (lane >= o) s += y;
-  }
+  const double s = wave_sums(reset ? 0.0 : log2_sigmoid(fg));
   const double u = (double)ig * kLog2e - s;
   double r, top;
   if (MODE == kFwd) {
-    const int first = mine ? 63 - __builtin_clzll(mine) : 0;
-    r = u;
+    if (all == 0) {
+      r = wave_maxima(u);
+    } else {  // since the last reset
+      const int first = mine ? 63 - __builtin_clzll(mine) : 0;
+      r = u;
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const double y = __shfl_up(r, o);
-      if (lane - o >= first) r = fmax(r, y);
+      for (int o = 1; o < 64; o <<= 1) {
+        const double y = __shfl_up(r, o);
+        if (lane - o >= first) r = fmax(r, y);
+      }
     }
-    top = r;
+    top = last_lane(r);
   } else {
+    const float lse = read ? raw.lse : neg_inf();
     r = lse == neg_inf() ? -__builtin_inf() : s - (double)lse * kLog2e;
     top = MODE == kDq ? (rid == all ? u : -__builtin_inf()) : (rid == 0 ? r : -__builtin_inf());
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) top = fmax(top, __shfl_xor(top, o));
-    if (gone(r)) dot = 0.f;
+    top = last_lane(wave_maxima(top));
+    G.d[i] = a.normalize && !gone(r) ? -raw.dot : 0.f;
   }
   G.u[i] = u;
   G.r[i] = r;
   G.b[i] = s;
   G.rid[i] = rid;
-  if (MODE != kFwd) G.d[i] = dot;
   const uint64_t odd_k = __builtin_amdgcn_ballot_w64(in && gone(u));
   const uint64_t odd_q = __builtin_amdgcn_ballot_w64(MODE != kFwd && read && gone(r));
   if (lane == 63) {
@@ -366,6 +408,15 @@ __global__ __launch_bounds__(256, 2) void mlstm_segment_kernel(MlstmLaunch a) {
   double m = -__builtin_inf(), sum = 0.0, top = -__builtin_inf();
   auto chunk_at = [&](int i) { return rev ? first + count - 1 - i : first + i; };
 
+  RawGates<kDkv> raw;
+  RawGates<kFwd> forward;
+  auto load_gates = [&](int chunk) __attribute__((always_inline)) {
+    if (rev)
+      raw.load(a, b, h, n, chunk, lane);
+    else
+      forward.load(a, b, h, n, chunk, lane);
+  };
+  if (wave < count) load_gates(chunk_at(wave));
   Tile<D, 256> tb, tc;
   if (count > 0) {
     tb.load(rb, b, h, chunk_at(0) * kChunk, shift, n, tid);
@@ -373,11 +424,14 @@ __global__ __launch_bounds__(256, 2) void mlstm_segment_kernel(MlstmLaunch a) {
   }
   for (int i = 0; i < count; ++i) {
     const int slot = i % kBlock;
-    if (slot == 0 && i + wave < count) {
-      if (rev)
-        chunk_gates<kDkv>(a, G, b, h, n, chunk_at(i + wave), wave, lane);
-      else
-        chunk_gates<kFwd>(a, G, b, h, n, chunk_at(i + wave), wave, lane);
+    if (slot == 0) {
+      if (i + wave < count) {
+        if (rev)
+          chunk_gates<kDkv>(a, G, raw, n, chunk_at(i + wave), wave, lane);
+        else
+          chunk_gates<kFwd>(a, G, forward, n, chunk_at(i + wave), wave, lane);
+      }
+      if (i + kBlock + wave < count) load_gates(chunk_at(i + kBlock + wave));
     }
     tb.store(b_sh, chunk_at(i) * kChunk, shift, n, tid);
     tc.store(c_sh, chunk_at(i) * kChunk, shift, n, tid);
@@ -453,44 +507,67 @@ __global__ __launch_bounds__(256, 2) void mlstm_segment_kernel(MlstmLaunch a) {
 // ---------------------------------------------------------------------------
 
 // One thread per 4 elements of a head's matrix and vector, which it carries over the segments: a part is
-// replaced by what its segment starts from. Forwards, a given state is where it starts and ends.
+// replaced by what its segment starts from. Forwards, a given state is where it starts and ends. The
+// exponents' chain is worked out first, by every workgroup; then kAhead parts are on their way.
+constexpr int kScanSegments = 512;  // exponents at once
 template <int D>
 __global__ __launch_bounds__(256) void mlstm_scan_kernel(MlstmLaunch a, int blocks) {
-  const int list = blockIdx.x / blocks, e = ((blockIdx.x % blocks) * 256 + threadIdx.x) * 4;
-  if (e >= D * D + D) return;
-  const bool rev = blockIdx.y != 0;
+  __shared__ double add_sh[kScanSegments], sum_sh[kScanSegments], top_sh[kScanSegments], from_sh[kScanSegments];
+  __shared__ float keep_sh[kScanSegments], put_sh[kScanSegments];
+  __shared__ double last_sh[2];
+  const int list = blockIdx.x / blocks, e = ((blockIdx.x % blocks) * 256 + threadIdx.x) * 4, tid = threadIdx.x;
+  const bool rev = blockIdx.y != 0, mine = e < D * D + D;
   float* parts = a.parts + ((int64_t)blockIdx.y * a.B * a.H + list) * a.segs * segment_floats(D);
+  auto part = [&](int i) { return parts + (int64_t)(rev ? a.segs - 1 - i : i) * segment_floats(D); };
   float* held = nullptr;
   f32x4 x = {0.f, 0.f, 0.f, 0.f};
-  if (!rev && a.C) {
+  if (!rev && a.C && mine) {
     held = e < D * D ? a.C + (int64_t)list * D * D + e : a.z + (int64_t)list * D + (e - D * D);
     x = *reinterpret_cast<const f32x4*>(held);
   }
-  constexpr int kAhead = 4;  // parts on their way
-  f32x4 next[kAhead];
-  auto part = [&](int i) { return parts + (int64_t)(rev ? a.segs - 1 - i : i) * segment_floats(D); };
   double m = scalars(part(0), D)->from, defined = m;
+  constexpr int kAhead = 8;
+  f32x4 next[kAhead];
 #pragma unroll
   for (int j = 0; j < kAhead; ++j)
-    if (j < a.segs) next[j] = *reinterpret_cast<const f32x4*>(part(j) + e);
-  for (int i0 = 0; i0 < a.segs; i0 += kAhead) {
-#pragma unroll
-    for (int j = 0; j < kAhead; ++j) {
-      const int i = i0 + j;
-      if (i >= a.segs) break;
-      float* p = part(i);
-      SegmentScalars* s = scalars(p, D);
-      const f32x4 add = next[j];
-      if (i + kAhead < a.segs) next[j] = *reinterpret_cast<const f32x4*>(part(i + kAhead) + e);
-      *reinterpret_cast<f32x4*>(p + e) = x;
-      if (e == 0 && i > 0) s->from = m;
-      const double old = m + s->sum, now = fmax(old, s->add);
-      const float keep = gone(old) ? 0.f : pow2(old - now), put = gone(s->add) ? 0.f : pow2(s->add - now);
-#pragma unroll
-      for (int r = 0; r < 4; ++r) x[r] = (keep == 0.f ? 0.f : x[r] * keep) + add[r] * put;
-      m = now;
-      defined = held_m(defined, s->sum, s->top);
+    if (mine && j < a.segs) next[j] = *reinterpret_cast<const f32x4*>(part(j) + e);
+  for (int base = 0; base < a.segs; base += kScanSegments) {
+    const int count = min(kScanSegments, a.segs - base);
+    __syncthreads();
+    for (int i = tid; i < count; i += 256) {
+      const SegmentScalars* s = scalars(part(base + i), D);
+      add_sh[i] = s->add, sum_sh[i] = s->sum, top_sh[i] = s->top;
     }
+    __syncthreads();
+    if (tid == 0) {
+      for (int i = 0; i < count; ++i) {
+        from_sh[i] = m;
+        m = fmax(m + sum_sh[i], add_sh[i]);
+        defined = held_m(defined, sum_sh[i], top_sh[i]);
+      }
+      last_sh[0] = m, last_sh[1] = defined;
+    }
+    __syncthreads();
+    m = last_sh[0], defined = last_sh[1];
+    for (int i = tid; i < count; i += 256) {
+      const double old = from_sh[i] + sum_sh[i], now = i + 1 < count ? from_sh[i + 1] : m;
+      keep_sh[i] = gone(old) ? 0.f : pow2(old - now);
+      put_sh[i] = gone(add_sh[i]) ? 0.f : pow2(add_sh[i] - now);
+      if (blockIdx.x % blocks == 0 && base + i > 0) scalars(part(base + i), D)->from = from_sh[i];
+    }
+    __syncthreads();
+    if (mine)
+      for (int i0 = base; i0 < base + count; i0 += kAhead) {
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+          const int i = i0 + j;
+          if (i >= base + count) break;
+          const f32x4 add = next[j];
+          if (i + kAhead < a.segs) next[j] = *reinterpret_cast<const f32x4*>(part(i + kAhead) + e);
+          *reinterpret_cast<f32x4*>(part(i) + e) = x;
+          x = scaled(x, keep_sh[i - base]) + add * put_sh[i - base];
+        }
+      }
   }
   if (held) {
     *reinterpret_cast<f32x4*>(held) = gone(m) ? x : x * pow2(m - defined);
@@ -581,6 +658,31 @@ __global__ __launch_bounds__(MODE == kDkv ? 512 : 256, 2) void mlstm_kernel(Mlst
   }
   double defined = m;
 
+  if (REV) {
+    // At the end of the segment: what is held there times its gradient.
+    float dot = 0.f;
+    const bool inner = seg + 1 < a.segs;
+    const float* held = a.parts + ((int64_t)list * a.segs + (inner ? seg + 1 : 0)) * segment_floats(D);
+    if (inner && !role) {
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) dot += S[i][t][r] * held[(16 * i + 4 * g + r) * D + (wave * NT + t) * 16 + c];
+      if (tid < D) dot += from_z[tid] * held[D * D + tid];
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) dot += __shfl_xor(dot, o);
+    if (lane == 0 && !role) sh.dig[wave][0] = dot;
+    __syncthreads();
+    if (tid == 0) {
+      const double e = inner ? m + scalars(const_cast<float*>(held), D)->from : -__builtin_inf();
+      const double all = ((double)sh.dig[0][0] + sh.dig[1][0] + sh.dig[2][0] + sh.dig[3][0]) * a.scale;
+      a.edges[(int64_t)list * a.segs + seg] = gone(e) ? 0.0 : all * (double)pow2(e);
+    }
+    __syncthreads();
+  }
   // Where this lane's outputs go, from time 0 on.
   uint16_t* out_at = out + ((int64_t)list * a.T + c - (REV ? 0 : a.delay)) * D + wave * NT * 16 + 4 * g;
 
@@ -591,11 +693,16 @@ __global__ __launch_bounds__(MODE == kDkv ? 512 : 256, 2) void mlstm_kernel(Mlst
     t2.load(r2, b, h, chunk * kChunk, late2, n, tid);
     if (REV) t3.load(a.go, b, h, chunk * kChunk, a.delay, n, tid);
   };
+  RawGates<MODE> raw;
+  if (role == 0 && wave < count) raw.load(a, b, h, n, chunk_at(wave), lane);
   if (count > 0) load(chunk_at(0));
 
   for (int it = 0; it < count; ++it) {
     const int chunk = chunk_at(it), slot = it % kBlock, at = slot * kChunk;
-    if (slot == 0 && role == 0 && it + wave < count) chunk_gates<MODE>(a, G, b, h, n, chunk_at(it + wave), wave, lane);
+    if (slot == 0 && role == 0) {
+      if (it + wave < count) chunk_gates<MODE>(a, G, raw, n, chunk_at(it + wave), wave, lane);
+      if (it + kBlock + wave < count) raw.load(a, b, h, n, chunk_at(it + kBlock + wave), lane);
+    }
     t0.store(sh.tile[0], chunk * kChunk, late0, n, tid);
     t1.store(sh.tile[1], chunk * kChunk, 0, n, tid);
     t2.store(sh.tile[2], chunk * kChunk, late2, n, tid);
@@ -881,7 +988,6 @@ __device__ __forceinline__ double block_sum(double x, double* sh) {
 // read-out does not change with x's length) or do . o. The running sum of k . dk, whose terms were
 // rounded on the way, starts from the one product and is made to end in the next, in proportion: its
 // errors do not pile up along the sequence.
-template <int D>
 __global__ __launch_bounds__(256) void mlstm_forget_kernel(MlstmLaunch a) {
   __shared__ double sum_sh[4], edge_sh[4];
   __shared__ int reset_sh[4];
@@ -889,20 +995,8 @@ __global__ __launch_bounds__(256) void mlstm_forget_kernel(MlstmLaunch a) {
   const int seg = blockIdx.x % a.segs, list = blockIdx.x / a.segs, b = list / a.H, h = list % a.H;
   const int n = a.lens ? clampi(a.lens[b], 0, a.T) : a.T;
   const int t0 = min(seg * a.seg_chunks * kChunk, a.T), t1 = min((seg + 1) * a.seg_chunks * kChunk, a.T), end = min(t1, n);
-  auto edge = [&](int s) {  // at the start of segment s
-    if (s <= 0 || s >= a.segs) return 0.0;
-    float* x = a.parts + ((int64_t)list * a.segs + s) * segment_floats(D);
-    float* y = a.parts + (((int64_t)a.B * a.H + list) * a.segs + s - 1) * segment_floats(D);
-    const double e = scalars(x, D)->from + scalars(y, D)->from;
-    float part = 0.f;
-    for (int i = tid * 4; i < D * D + D; i += 1024) {
-      const f32x4 p = *reinterpret_cast<const f32x4*>(x + i), q = *reinterpret_cast<const f32x4*>(y + i);
-      part += p.x * q.x + p.y * q.y + p.z * q.z + p.w * q.w;
-    }
-    const double all = block_sum((double)part, sum_sh) * a.scale;
-    return gone(e) ? 0.0 : all * (double)pow2(e);
-  };
-  const double start = edge(seg), stop = edge(seg + 1);
+  const double* edges = a.edges + (int64_t)list * a.segs;
+  const double start = seg > 0 ? edges[seg - 1] : 0.0, stop = edges[seg];
   // a token's step: x . dx - k . dk
   auto step = [&](int t) -> double {
     if (t >= end) return 0.0;
@@ -1077,7 +1171,7 @@ int launch_bwd(const MlstmLaunch& L) {
   if ((e = (int)hipGetLastError()) != 0) return e;
   hipLaunchKernelGGL((mlstm_kernel<D, kDkv>), dim3(groups), dim3(512), 0, st, L);
   if ((e = (int)hipGetLastError()) != 0) return e;
-  hipLaunchKernelGGL((mlstm_forget_kernel<D>), dim3(groups), dim3(256), 0, st, L);
+  hipLaunchKernelGGL(mlstm_forget_kernel, dim3(groups), dim3(256), 0, st, L);
   return (int)hipGetLastError();
 }
 
@@ -1085,6 +1179,7 @@ int launch_bwd(const MlstmLaunch& L) {
 int64_t part_floats(const MlstmLaunch& L) {
   return L.segs > 1 ? (int64_t)L.B * L.H * L.segs * segment_floats(L.D) : 0;
 }
+int64_t edge_floats(const MlstmLaunch& L) { return ((int64_t)L.B * L.H * L.segs * 2 + 3) / 4 * 4; }
 int64_t row_floats(const MlstmLaunch& L) { return ((int64_t)L.B * L.H * L.T + 3) / 4 * 4; }
 
 }  // namespace
@@ -1097,7 +1192,7 @@ int64_t mlstm_fwd_workspace_floats(MlstmLaunch L) {
 }
 int64_t mlstm_bwd_workspace_floats(MlstmLaunch L) {
   plan(L);
-  return 2 * part_floats(L) + 2 * row_floats(L);
+  return 2 * part_floats(L) + 2 * row_floats(L) + edge_floats(L);
 }
 
 int launch_mlstm_fwd(MlstmLaunch L) {
@@ -1110,7 +1205,8 @@ int launch_mlstm_bwd(MlstmLaunch L) {
   plan(L);
   L.dots = L.workspace;
   L.dig32 = L.dots + row_floats(L);
-  L.parts = L.dig32 + row_floats(L);
+  L.edges = reinterpret_cast<double*>(L.dig32 + row_floats(L));
+  L.parts = L.dig32 + row_floats(L) + edge_floats(L);
   return L.D == 64 ? launch_bwd<64>(L) : launch_bwd<128>(L);
 }
 
