@@ -159,7 +159,8 @@ struct MlstmLaunch {
   // plan
   int32_t segs, seg_chunks; // segments of each head and their chunks of 64 tokens
   float* parts;             // [directions, B, H, segs] parts
-  float *dots, *dig32;      // backward: [B, H, T]
+  float *dots, *dig32;      // backward: [B, H, T]: do . o and k . dk
+  float* xdx;               // backward: [B, H, T], by time: x . dx
   double* edges;            // backward: [B, H, segs]
 };
 

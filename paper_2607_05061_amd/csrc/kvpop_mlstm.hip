@@ -539,14 +539,23 @@ __global__ __launch_bounds__(256) void mlstm_scan_kernel(MlstmLaunch a, int bloc
       add_sh[i] = s->add, sum_sh[i] = s->sum, top_sh[i] = s->top;
     }
     __syncthreads();
-    if (tid == 0) {
-      for (int i = 0; i < count; ++i) {
-        from_sh[i] = m;
-        m = fmax(m + sum_sh[i], add_sh[i]);
-        defined = held_m(defined, sum_sh[i], top_sh[i]);
+    if (tid < 64)  // m -> max(m + sum, add), a wave's segments at a time: such steps compose to one
+      for (int i0 = 0; i0 < count; i0 += 64) {
+        const int i = min(i0 + tid, count - 1);
+        const double none = -__builtin_inf();
+        const bool in = i0 + tid < count;
+        double sum = in ? sum_sh[i] : 0.0, add = in ? add_sh[i] : none, top = in ? top_sh[i] : none;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+          const double s = __shfl_up(sum, o), x = __shfl_up(add, o), y = __shfl_up(top, o);
+          if (tid >= o) add = fmax(x + sum, add), top = fmax(y + sum, top), sum += s;
+        }
+        const double after = fmax(m + sum, add), end = fmax(defined + sum, top);
+        const double before = __shfl_up(after, 1);
+        if (in) from_sh[i] = tid ? before : m;
+        m = last_lane(after), defined = last_lane(end);
       }
-      last_sh[0] = m, last_sh[1] = defined;
-    }
+    if (tid == 0) last_sh[0] = m, last_sh[1] = defined;
     __syncthreads();
     m = last_sh[0], defined = last_sh[1];
     for (int i = tid; i < count; i += 256) {
@@ -590,7 +599,7 @@ struct Shared {
   __align__(16) uint16_t zrow[MODE == kFwd ? 2 * (D + 8) : 8];  // z's high and low bf16 parts
   __align__(16) float far[kRoles][kChunk], far_z[kRoles][kChunk], out[kChunk];
   __align__(16) float z[kRoles][D];
-  float dig[4][kChunk];
+  float dig[4][kChunk];  // backward: the waves' parts of x . dx, of k . dk
 };
 
 // One workgroup per segment of a head. 4 waves (for dk and dv 4 each, over the same tiles): wave w takes
@@ -845,7 +854,16 @@ __global__ __launch_bounds__(MODE == kDkv ? 512 : 256, 2) void mlstm_kernel(Mlst
         for (int t = 0; t < NT; ++t) acc[q][t] = mfma(sf[t], af, acc[q][t]);
       }
     }
-    bf16x4 y[4][NT];
+    bf16x4 y[4][NT], mate[4][NT];  // mate: dq's rows of q (dk's rows of k are in LDS)
+    if (MODE == kDq) {
+      const uint16_t* from = a.q.ptr + b * a.q.sb + h * a.q.sh + wave * NT * 16 + 4 * g;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int row = min(max(chunk * kChunk + 16 * q + c - a.delay, 0), n - 1);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) mate[q][t] = *reinterpret_cast<const bf16x4*>(from + row * a.q.st + 16 * t);
+      }
+    }
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       const int j = 16 * q + c;
@@ -864,15 +882,15 @@ __global__ __launch_bounds__(MODE == kDkv ? 512 : 256, 2) void mlstm_kernel(Mlst
         acc[q][t] *= fac;
 #pragma unroll
         for (int r = 0; r < 4; ++r) y[q][t][r] = (__bf16)acc[q][t][r];
-        if (REV) {
-          const bf16x4 kr = *reinterpret_cast<const bf16x4*>(sh.tile[0] + j * LS + col);
+        if (MODE != kFwd) {
+          if (REV) mate[q][t] = *reinterpret_cast<const bf16x4*>(sh.tile[0] + j * LS + col);
 #pragma unroll
-          for (int r = 0; r < 4; ++r) dot += acc[q][t][r] * (float)kr[r];
+          for (int r = 0; r < 4; ++r) dot += acc[q][t][r] * (float)mate[q][t][r];
         }
       }
-      if (REV) {
+      if (MODE != kFwd) {
         dot = sum_groups(dot);
-        if (g == 0 && role) sh.dig[wave][j] = dot;
+        if (g == 0 && (MODE == kDq || role)) sh.dig[wave][j] = dot;
       }
     }
     {
@@ -914,12 +932,16 @@ __global__ __launch_bounds__(MODE == kDkv ? 512 : 256, 2) void mlstm_kernel(Mlst
     }
     m = up.next;
     __syncthreads();
-    if (REV && tid < kChunk) {
+    if (MODE != kFwd && tid < kChunk) {
       const int t = chunk * kChunk + tid;
       if (t < n) {
         const float x = sh.dig[0][tid] + sh.dig[1][tid] + sh.dig[2][tid] + sh.dig[3][tid];
-        a.dig32[(int64_t)list * a.T + t] = x;
-        a.dig[(int64_t)list * a.T + t] = bf16_bits(x);
+        if (REV) {
+          a.dig32[(int64_t)list * a.T + t] = x;
+          a.dig[(int64_t)list * a.T + t] = bf16_bits(x);
+        } else {
+          a.xdx[(int64_t)list * a.T + t] = t >= a.delay ? x : 0.f;
+        }
       }
     }
   }
@@ -984,10 +1006,9 @@ __device__ __forceinline__ double block_sum(double x, double* sh) {
 
 // The forget gates' gradients, one workgroup per segment. d log f_t is the sum over the pairs s < t <= u
 // that t lies between. At a segment's start that is the product of what is held there and its gradient,
-// and from token to token it changes by x . dx - k . dk of the token, where x . dx is 0 (a normalised
-// read-out does not change with x's length) or do . o. The running sum of k . dk, whose terms were
-// rounded on the way, starts from the one product and is made to end in the next, in proportion: its
-// errors do not pile up along the sequence.
+// and from token to token it changes by x . dx - k . dk of the token. Both of these hold the pairs of their chunk
+// with the same rounded weights, which cancel in the running sum; it is made to end in the next
+// product, in proportion, so that what rounding is left does not pile up along the sequence.
 __global__ __launch_bounds__(256) void mlstm_forget_kernel(MlstmLaunch a) {
   __shared__ double sum_sh[4], edge_sh[4];
   __shared__ int reset_sh[4];
@@ -1000,9 +1021,7 @@ __global__ __launch_bounds__(256) void mlstm_forget_kernel(MlstmLaunch a) {
   // a token's step: x . dx - k . dk
   auto step = [&](int t) -> double {
     if (t >= end) return 0.0;
-    double x = -(double)a.dig32[(int64_t)list * a.T + t];
-    if (!a.normalize && t >= a.delay) x += a.dots[(int64_t)list * a.T + t - a.delay];
-    return x;
+    return (double)a.xdx[(int64_t)list * a.T + t] - a.dig32[(int64_t)list * a.T + t];
   };
   auto fg = [&](int t) { return bf16_value(a.fg.ptr[b * a.fg.sb + h * a.fg.sh + t * a.fg.st]); };
   double total = 0.0, resets = 0.0;
@@ -1192,7 +1211,7 @@ int64_t mlstm_fwd_workspace_floats(MlstmLaunch L) {
 }
 int64_t mlstm_bwd_workspace_floats(MlstmLaunch L) {
   plan(L);
-  return 2 * part_floats(L) + 2 * row_floats(L) + edge_floats(L);
+  return 2 * part_floats(L) + 3 * row_floats(L) + edge_floats(L);
 }
 
 int launch_mlstm_fwd(MlstmLaunch L) {
@@ -1205,8 +1224,9 @@ int launch_mlstm_bwd(MlstmLaunch L) {
   plan(L);
   L.dots = L.workspace;
   L.dig32 = L.dots + row_floats(L);
-  L.edges = reinterpret_cast<double*>(L.dig32 + row_floats(L));
-  L.parts = L.dig32 + row_floats(L) + edge_floats(L);
+  L.xdx = L.dig32 + row_floats(L);
+  L.edges = reinterpret_cast<double*>(L.xdx + row_floats(L));
+  L.parts = L.xdx + row_floats(L) + edge_floats(L);
   return L.D == 64 ? launch_bwd<64>(L) : launch_bwd<128>(L);
 }
 
