@@ -854,54 +854,59 @@ __global__ __launch_bounds__(MODE == kDkv ? 512 : 256, 2) void mlstm_kernel(Mlst
         for (int t = 0; t < NT; ++t) acc[q][t] = mfma(sf[t], af, acc[q][t]);
       }
     }
-    bf16x4 y[4][NT], mate[4][NT];  // mate: dq's rows of q (dk's rows of k are in LDS)
-    if (MODE == kDq) {
-      const uint16_t* from = a.q.ptr + b * a.q.sb + h * a.q.sh + wave * NT * 16 + 4 * g;
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int row = min(max(chunk * kChunk + 16 * q + c - a.delay, 0), n - 1);
-#pragma unroll
-        for (int t = 0; t < NT; ++t) mate[q][t] = *reinterpret_cast<const bf16x4*>(from + row * a.q.st + 16 * t);
-      }
-    }
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const int j = 16 * q + c;
-      const float far = sh.far[role][j], fac = MODE == kFwd ? sh.out[j] : a.scale;
-      const float far_z = MODE != kFwd && with_z ? sh.far_z[role][j] : 0.f;
-      float dot = 0.f;
-#pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        const int col = (wave * NT + t) * 16 + 4 * g;
-        acc[q][t] = scaled(acc[q][t], far);
-        if (MODE != kFwd && with_z) acc[q][t] += scaled(*reinterpret_cast<const f32x4*>(sh.z[role] + col), far_z);
-#pragma unroll
-        for (int s = 0; s < 2; ++s)
-          if (REV ? 32 * s + 31 >= 16 * q : 32 * s <= 16 * q)
-            acc[q][t] = mfma(cf[s][t], row8(sh.p[role] + j * PS + 32 * s + 8 * g), acc[q][t]);
-        acc[q][t] *= fac;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) y[q][t][r] = (__bf16)acc[q][t][r];
-        if (MODE != kFwd) {
-          if (REV) mate[q][t] = *reinterpret_cast<const bf16x4*>(sh.tile[0] + j * LS + col);
-#pragma unroll
-          for (int r = 0; r < 4; ++r) dot += acc[q][t][r] * (float)mate[q][t][r];
-        }
-      }
-      if (MODE != kFwd) {
-        dot = sum_groups(dot);
-        if (g == 0 && (MODE == kDq || role)) sh.dig[wave][j] = dot;
-      }
-    }
     {
       const int late = REV ? 0 : a.delay, t0 = chunk * kChunk;
       uint16_t* to = out_at + (int64_t)t0 * D;
-      const bool whole = t0 >= late && t0 + kChunk <= n;
+      // dq's rows of q, a block of rows ahead (dk's rows of k are in LDS).
+      const uint16_t* from = a.q.ptr + b * a.q.sb + h * a.q.sh + wave * NT * 16 + 4 * g;
+      bf16x4 mate[NT], ahead[NT];
+      auto fetch = [&](int q) __attribute__((always_inline)) {
+        const uint16_t* p = from + min(max(t0 + 16 * q + c - a.delay, 0), n - 1) * a.q.st;
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
-        if (whole || (t0 + 16 * q + c >= late && t0 + 16 * q + c < n))
+        for (int t = 0; t < NT; ++t) ahead[t] = *reinterpret_cast<const bf16x4*>(p + 16 * t);
+      };
+      if (MODE == kDq) fetch(0);
 #pragma unroll
-          for (int t = 0; t < NT; ++t) *reinterpret_cast<bf16x4*>(to + 16 * q * D + 16 * t) = y[q][t];
+      for (int q = 0; q < 4; ++q) {
+        const int j = 16 * q + c;
+        if (MODE == kDq) {
+#pragma unroll
+          for (int t = 0; t < NT; ++t) mate[t] = ahead[t];
+          if (q < 3) fetch(q + 1);
+        }
+        const float far = sh.far[role][j], fac = MODE == kFwd ? sh.out[j] : a.scale;
+        const float far_z = MODE != kFwd && with_z ? sh.far_z[role][j] : 0.f;
+        float dot = 0.f;
+        bf16x4 y[NT];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          const int col = (wave * NT + t) * 16 + 4 * g;
+          acc[q][t] = scaled(acc[q][t], far);
+          if (MODE != kFwd && with_z) acc[q][t] += scaled(*reinterpret_cast<const f32x4*>(sh.z[role] + col), far_z);
+#pragma unroll
+          for (int s = 0; s < 2; ++s)
+            if (REV ? 32 * s + 31 >= 16 * q : 32 * s <= 16 * q)
+              acc[q][t] = mfma(cf[s][t], row8(sh.p[role] + j * PS + 32 * s + 8 * g), acc[q][t]);
+          acc[q][t] *= fac;
+          if (REV) mate[t] = *reinterpret_cast<const bf16x4*>(sh.tile[0] + j * LS + col);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            y[t][r] = (__bf16)acc[q][t][r];
+            if (MODE != kFwd) dot += acc[q][t][r] * (float)mate[t][r];
+          }
+        }
+        // The values are made before the branch: where the products' results were first read behind one, the
+        // compiler had left out the wait that they need.
+#pragma unroll
+        for (int t = 0; t < NT; ++t) asm volatile("" : "+v"(y[t]), "+v"(dot));
+        if (t0 + j >= late && t0 + j < n)
+#pragma unroll
+          for (int t = 0; t < NT; ++t) *reinterpret_cast<bf16x4*>(to + 16 * q * D + 16 * t) = y[t];
+        if (MODE != kFwd) {
+          dot = sum_groups(dot);
+          if (g == 0 && (MODE == kDq || role)) sh.dig[wave][j] = dot;
+        }
+      }
     }
 
     update_state<D, NT>(S, up.keep, b_sh, cf, sh.w, g, c);
