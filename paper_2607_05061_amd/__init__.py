@@ -988,11 +988,25 @@ def kvpop_mlstm_step(q, k, v, ig, fg, state: KvpopMlstmState, scale: float = 1.0
     active: int32 [B], 0 for idle sequences, which keep what they hold (None: all are active). Returns
     o bf16 [B, H, D], 0 for idle sequences."""
     torch = _torch()
-    _need(isinstance(q, torch.Tensor) and q.dim() == 3, "q must be a tensor [B, H, D]")
-    _need(all(isinstance(x, torch.Tensor) and x.dim() == 3 for x in (k, v)), "k and v must be tensors [B, H, D]")
-    _need(all(isinstance(x, torch.Tensor) and x.dim() == 2 for x in (ig, fg)), "ig and fg must be tensors [B, H]")
-    a, B, H, _, D, dev = _mlstm_parts(torch, q.unsqueeze(2), k.unsqueeze(2), v.unsqueeze(2), ig.unsqueeze(2), fg.unsqueeze(2),
-                                      scale, 0, normalize, active)
+    _need(isinstance(q, torch.Tensor) and len(q.shape) == 3, "q must be a tensor [B, H, D]")
+    if not q.is_cuda:
+        raise ValueError("q must be on a GPU device")
+    B, H, D = q.shape
+    _need(B >= 1 and H >= 1, "q must not be empty")
+    dev, bf16 = q.get_device(), torch.bfloat16
+    rows = []
+    for name, x, shape in (("q", q, (B, H, D)), ("k", k, (B, H, D)), ("v", v, (B, H, D)), ("ig", ig, (B, H)), ("fg", fg, (B, H))):
+        if not isinstance(x, torch.Tensor):
+            raise TypeError("%s must be a torch.Tensor" % name)
+        if x.dtype is not bf16:
+            raise TypeError("%s must be %s, got %s" % (name, bf16, x.dtype))
+        if x.shape != shape or x.get_device() != dev:
+            raise ValueError("%s must be %s on the GPU device of q, got %s" % (name, list(shape), list(x.shape)))
+        sb, sh, *sd = x.stride()
+        if sd and sd[0] != 1:
+            raise ValueError("%s must be contiguous in its last dimension" % name)
+        rows += x.data_ptr(), sb if B > 1 else 0, sh if H > 1 else 0, 0
+    a = _MLSTM_PACK.pack(B, H, 1, D, 0, 1 if normalize else 0, float(scale), *rows, _ptr(active, "active", torch.int32, (B,), dev))
     _need(state is not None, "a step needs a state")
     st = _state_ptrs(torch, state, B, H, D, dev)
     if o is None:

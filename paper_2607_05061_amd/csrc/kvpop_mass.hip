@@ -17,95 +17,175 @@ namespace {
 // is not defined).
 __device__ __forceinline__ uint32_t mass_key(float x) { return x != x ? 0u : desc_key(x); }
 
-constexpr int kTile = 32;   // keys per wave
 constexpr int kWaves = 4;
+constexpr int kQueries = 64;  // (token, head) rows that a workgroup shares at a time
 
-// One wave: 32 keys of a list, which stay in registers, against all queries of the KV head,
-// 16 (token, head) rows at a time (tokens slowest). S = K Q^T puts keys on the accumulator's rows and
-// queries on its columns; a lane adds up its column's probabilities and the 16 lanes of a row join
-// at the end. Nothing is shared between waves, and a mass has one writer.
+// 16 keys of a list, widened to 16 bits, and what is known of them.
 template <int D, int FMT>
-__global__ __launch_bounds__(64 * kWaves) void cache_mass_kernel(CacheMassLaunch a, int blocks) {
-  constexpr int KS = D / 32, KW = D / 16;
-  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
-  const int g = lane >> 4, c = lane & 15;
-  const int list = blockIdx.x / blocks, t = (blockIdx.x % blocks) * kWaves + wave;
-  const int b = list / a.c.H, h = list % a.c.H, G = a.Hq / a.c.H;
-  const int lgP = 31 - __builtin_clz(a.c.P);
-  const int L = clampi(a.held[list], 0, a.c.max_pages * a.c.P);
-  const int key0 = kTile * t;
-  if (key0 >= min(L, a.S)) return;
-  const int nq = a.q_lens ? clampi(a.q_lens[b], 0, a.N) : a.N;
-
-  int id[2];
-  float ke[2];
-  H8 k[2][KS];
+struct Keys {
+  Words<4> w[D / 64];
+  H8 k[D / 32];
+  float e;
+  bool page;
+  // Their page (uniform), -1 for none, then their codes.
+  static __device__ __forceinline__ int page_of(const CacheMassLaunch& a, int list, int key, int L, int lgP) {
+    const int id = key < L ? a.c.table[(int64_t)list * a.c.max_pages + (key >> lgP)] : -1;
+    return (unsigned)id < (unsigned)a.c.n_pages ? id : -1;
+  }
+  __device__ __forceinline__ void load(const CacheMassLaunch& a, int id, int key, int lgP, int g, int c) {
+    page = id >= 0;
+    id = max(id, 0);
+    e = (float)clampi(a.c.ke[id], kExpMin, kExpMax);
+    const uint8_t* p = a.c.k + (((int64_t)id << lgP) + (key & (a.c.P - 1)) + c) * D + (D / 4) * g;
 #pragma unroll
-  for (int s = 0; s < 2; ++s) {
-    const int key = key0 + 16 * s, at = key >> lgP;
-    id[s] = key < L ? a.c.table[(int64_t)list * a.c.max_pages + at] : -1;
-    if ((unsigned)id[s] >= (unsigned)a.c.n_pages) id[s] = -1;
-    const int page = max(id[s], 0);
-    ke[s] = (float)clampi(a.c.ke[page], kExpMin, kExpMax);
-    const uint8_t* kp = a.c.k + (((int64_t)page << lgP) + (key & (a.c.P - 1)) + c) * D + (D / 4) * g;
-    Words<4> w[KW / 4];
+    for (int i = 0; i < D / 64; ++i) w[i] = *reinterpret_cast<const Words<4>*>(p + 16 * i);
+  }
+  __device__ __forceinline__ void widen() {
 #pragma unroll
-    for (int i = 0; i < KW / 4; ++i) w[i] = *reinterpret_cast<const Words<4>*>(kp + 16 * i);
-#pragma unroll
-    for (int m = 0; m < KS; ++m) {
-      widen4<FMT>(w[m / 2].w[2 * (m % 2)], k[s][m].h[0], k[s][m].h[1]);
-      widen4<FMT>(w[m / 2].w[2 * (m % 2) + 1], k[s][m].h[2], k[s][m].h[3]);
+    for (int m = 0; m < D / 32; ++m) {
+      widen4<FMT>(w[m / 2].w[2 * (m % 2)], k[m].h[0], k[m].h[1]);
+      widen4<FMT>(w[m / 2].w[2 * (m % 2) + 1], k[m].h[2], k[m].h[3]);
     }
   }
+};
 
-  float sum[2][4] = {};
-  const int R = G * nq;
-  for (int r0 = 0; r0 < R; r0 += 16) {
-    const int row = r0 + c, qi = row / G, qh = h * G + row % G;
-    const bool some = row < R;
-    const int seen = some ? L - (nq - 1 - qi) : 0;
-    float lse = some ? a.lse[((int64_t)b * a.Hq + qh) * a.N + qi] : 0.f;
-    lse = lse == neg_inf() ? -neg_inf() : lse * kLog2e;
-    float x[KS][8], big = 0.f;
+// N elements of a query from `at` on: their largest magnitude, then f16 with e taken out.
+template <int N>
+struct QueryPart {
+  float x[N];
+  __device__ __forceinline__ float load(const uint16_t* at, bool some) {
+    float big = 0.f;
 #pragma unroll
-    for (int m = 0; m < KS; ++m) {
+    for (int m = 0; m < N / 8; ++m) {
       uint4 w = {0, 0, 0, 0};
-      if (some)
-        w = *reinterpret_cast<const uint4*>(a.q.ptr + b * a.q.sb + qh * a.q.sh + qi * a.q.st + (D / 4) * g + 8 * m);
+      if (some) w = *reinterpret_cast<const uint4*>(at + 8 * m);
       const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        x[m][2 * i] = __uint_as_float(u[i] << 16);
-        x[m][2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
+        x[8 * m + 2 * i] = __uint_as_float(u[i] << 16);
+        x[8 * m + 2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
       }
-#pragma unroll
-      for (int i = 0; i < 8; ++i) big = fmaxf(big, __builtin_fabsf(x[m][i]));
     }
-    big = max_groups(big);
-    // Queries in f16: their largest element in [2^14, 2^15), so that elements down to 2^-28 of it
-    // keep their 8 bits (as in the attention that made lse).
-    const int e = big > 0.f ? __builtin_amdgcn_frexp_expf(big) - 15 : 0;
-    const float cq = __builtin_ldexpf(a.scale * kLog2e, e);
-    H8 q[KS];
 #pragma unroll
-    for (int m = 0; m < KS; ++m)
+    for (int i = 0; i < N; ++i) big = fmaxf(big, __builtin_fabsf(x[i]));
+    return big;
+  }
+  __device__ __forceinline__ void half(H8* to, int e) const {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) q[m].v[i] = (_Float16)__builtin_ldexpf(x[m][i], -e);
+    for (int i = 0; i < N; ++i) to[i / 8].v[i % 8] = (_Float16)__builtin_ldexpf(x[i], -e);
+  }
+};
+// Queries in f16: their largest element in [2^14, 2^15), so that elements down to 2^-28 of it keep their 8
+// bits (as in the attention that made lse).
+__device__ __forceinline__ int query_exponent(float big) {
+  return big > 0.f ? __builtin_amdgcn_frexp_expf(big) - 15 : 0;
+}
+// lse in units of log2; a query that saw nothing gives nothing.
+__device__ __forceinline__ float lse2(float x) { return x == neg_inf() ? -neg_inf() : x * kLog2e; }
+
+// One workgroup: 4 waves of 16 KT keys each, which stay in registers, against all queries of the KV head
+// ((token, head) rows, tokens slowest). S = K Q^T puts keys on the accumulator's rows and queries on its
+// columns; a lane adds up its column's probabilities and the 16 lanes of a row join at the end. Nothing is
+// shared between workgroups, and a mass has one writer.
+// MANY: rows pass through LDS in f16, 64 at a time, widened once for all waves; else (16 rows at most)
+// each wave takes them from memory.
+template <int D, int FMT, int KT, bool MANY>
+__global__ __launch_bounds__(64 * kWaves) void cache_mass_kernel(CacheMassLaunch a, int blocks) {
+  constexpr int KS = D / 32, QS = D + 8;
+  __shared__ __align__(16) uint16_t q_sh[MANY ? kQueries * QS : 8];
+  __shared__ float c_sh[MANY ? kQueries : 1], lse_sh[MANY ? kQueries : 1];
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const int g = lane >> 4, c = lane & 15;
+  const int list = blockIdx.x / blocks, key0 = ((blockIdx.x % blocks) * kWaves + wave) * 16 * KT;
+  const int b = list / a.c.H, h = list % a.c.H, G = a.Hq / a.c.H;
+  const int lgP = 31 - __builtin_clz(a.c.P);
+  const int L = clampi(a.held[list], 0, a.c.max_pages * a.c.P), end = min(L, a.S);
+  if ((blockIdx.x % blocks) * kWaves * 16 * KT >= end) return;
+  if (!MANY && key0 >= end) return;
+  const int nq = a.q_lens ? clampi(a.q_lens[b], 0, a.N) : a.N, R = G * nq;
+
+  Keys<D, FMT> k[KT];
+  int id[KT];
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
+  for (int s = 0; s < KT; ++s) id[s] = k[s].page_of(a, list, key0 + 16 * s, L, lgP);
+#pragma unroll
+  for (int s = 0; s < KT; ++s) k[s].load(a, id[s], key0 + 16 * s, lgP, g, c);
+
+  float sum[KT][4] = {};
+  // 16 rows from r0 on against the wave's keys; `edge`: some row may not see some key, or a page is missing.
+  auto add = [&](const H8 (&q)[KS], float cq, float lse, int row, bool edge) __attribute__((always_inline)) {
+    const int seen = row < R ? L - (nq - 1 - row / G) : 0;
+#pragma unroll
+    for (int s = 0; s < KT; ++s) {
       f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int m = 0; m < KS; ++m) acc = mfma16(k[s][m].v, q[m].v, acc);
-      const float kc = __builtin_ldexpf(cq, (int)ke[s]);
+      for (int m = 0; m < KS; ++m) acc = mfma16(k[s].k[m].v, q[m].v, acc);
+      const float kc = __builtin_ldexpf(cq, (int)k[s].e);
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const bool in = id[s] >= 0 && key0 + 16 * s + 4 * g + r < seen;
-        sum[s][r] += in ? __builtin_amdgcn_exp2f(__builtin_fmaf(acc[r], kc, -lse)) : 0.f;
+        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[r], kc, -lse));
+        sum[s][r] += !edge || (k[s].page && key0 + 16 * s + 4 * g + r < seen) ? p : 0.f;
+      }
+    }
+  };
+  if constexpr (!MANY) {
+    const int qi = c / G, qh = h * G + c % G;
+    const bool some = c < R;
+    QueryPart<D / 4> x;
+    const float big = max_groups(x.load(a.q.ptr + b * a.q.sb + qh * a.q.sh + qi * a.q.st + (D / 4) * g, some));
+    const int e = query_exponent(big);
+    H8 q[KS];
+    x.half(q, e);
+    const float lse = some ? lse2(a.lse[((int64_t)b * a.Hq + qh) * a.N + qi]) : 0.f;
+#pragma unroll
+    for (int s = 0; s < KT; ++s) k[s].widen();
+    add(q, __builtin_ldexpf(a.scale * kLog2e, e), lse, c, true);
+  } else {
+#pragma unroll
+    for (int s = 0; s < KT; ++s) k[s].widen();
+    bool pages = true;
+#pragma unroll
+    for (int s = 0; s < KT; ++s) pages = pages && id[s] >= 0;
+    // Four threads a row.
+    const int mine = tid >> 2, part = (tid & 3) * (D / 4);
+    QueryPart<D / 4> x;
+    float big, lse;
+    auto fetch = [&](int r0) __attribute__((always_inline)) {
+      const int row = r0 + mine, qi = row / G, qh = h * G + row % G;
+      const bool some = row < R;
+      big = x.load(a.q.ptr + b * a.q.sb + qh * a.q.sh + qi * a.q.st + part, some);
+      lse = some ? a.lse[((int64_t)b * a.Hq + qh) * a.N + qi] : 0.f;
+    };
+    if (R > 0) fetch(0);
+    for (int r0 = 0; r0 < R; r0 += kQueries) {
+      big = fmaxf(big, __shfl_xor(big, 1));
+      big = fmaxf(big, __shfl_xor(big, 2));
+      const int e = query_exponent(big);
+      H8 y[D / 32];
+      x.half(y, e);
+      __syncthreads();
+#pragma unroll
+      for (int m = 0; m < D / 32; ++m) *reinterpret_cast<f16x8*>(q_sh + mine * QS + part + 8 * m) = y[m].v;
+      if ((tid & 3) == 0) c_sh[mine] = __builtin_ldexpf(a.scale * kLog2e, e), lse_sh[mine] = lse2(lse);
+      __syncthreads();
+      if (r0 + kQueries < R) fetch(r0 + kQueries);
+      const int rows = min(kQueries, R - r0);
+      // All of these rows see all of the wave's keys (the first sees the fewest).
+      const bool whole = pages && rows == kQueries && key0 + 16 * KT <= L - (nq - 1 - r0 / G);
+#pragma unroll
+      for (int i = 0; i < kQueries; i += 16) {
+        H8 q[KS];
+#pragma unroll
+        for (int m = 0; m < KS; ++m) q[m].v = *reinterpret_cast<const f16x8*>(q_sh + (i + c) * QS + (D / 4) * g + 8 * m);
+        if (whole)
+          add(q, c_sh[i + c], lse_sh[i + c], r0 + i + c, false);
+        else
+          add(q, c_sh[i + c], lse_sh[i + c], r0 + i + c, true);
       }
     }
   }
 #pragma unroll
-  for (int s = 0; s < 2; ++s)
+  for (int s = 0; s < KT; ++s)
 #pragma unroll
     for (int r = 0; r < 4; ++r)
 #pragma unroll
@@ -113,23 +193,29 @@ __global__ __launch_bounds__(64 * kWaves) void cache_mass_kernel(CacheMassLaunch
   // Lane c < 4 of a group has its key 4 g + c.
   float* mass = a.mass + (int64_t)list * a.S;
 #pragma unroll
-  for (int s = 0; s < 2; ++s) {
-    const float add = c == 0 ? sum[s][0] : c == 1 ? sum[s][1] : c == 2 ? sum[s][2] : sum[s][3];
+  for (int s = 0; s < KT; ++s) {
+    const float more = c == 0 ? sum[s][0] : c == 1 ? sum[s][1] : c == 2 ? sum[s][2] : sum[s][3];
     const int key = key0 + 16 * s + 4 * g + c;
-    if (c < 4 && key < min(L, a.S)) mass[key] = a.decay > 0.f ? __builtin_fmaf(a.decay, mass[key], add) : add;
+    if (c < 4 && key < end) mass[key] = a.decay > 0.f ? __builtin_fmaf(a.decay, mass[key], more) : more;
   }
 }
 
+// 64 keys a wave for few rows; 32 where rows are many and keys few enough that all CUs get some.
+bool many_rows(const CacheMassLaunch& L) { return (int64_t)L.Hq / L.c.H * L.N > 16; }
+int mass_keys(const CacheMassLaunch& L) { return kWaves * (many_rows(L) ? 32 : 64); }
 int mass_blocks(const CacheMassLaunch& L) {
   const int64_t slots = (int64_t)L.c.max_pages * L.c.P < L.S ? (int64_t)L.c.max_pages * L.c.P : L.S;
-  return (int)((slots + kTile * kWaves - 1) / (kTile * kWaves));
+  return (int)((slots + mass_keys(L) - 1) / mass_keys(L));
 }
 
 template <int D, int FMT>
 int launch_mass(const CacheMassLaunch& L) {
   const int blocks = mass_blocks(L);
-  hipLaunchKernelGGL((cache_mass_kernel<D, FMT>), dim3((unsigned)(L.c.B * L.c.H * blocks)), dim3(64 * kWaves), 0,
-                     (hipStream_t)L.stream, L, blocks);
+  const dim3 grid((unsigned)(L.c.B * L.c.H * blocks)), block(64 * kWaves);
+  if (many_rows(L))
+    hipLaunchKernelGGL((cache_mass_kernel<D, FMT, 2, true>), grid, block, 0, (hipStream_t)L.stream, L, blocks);
+  else
+    hipLaunchKernelGGL((cache_mass_kernel<D, FMT, 4, false>), grid, block, 0, (hipStream_t)L.stream, L, blocks);
   return (int)hipGetLastError();
 }
 
@@ -152,17 +238,69 @@ __global__ __launch_bounds__(kSumThreads) void mass_sum_kernel(MassPromptLaunch 
 }
 
 constexpr int kPickThreads = 1024, kPickWaves = kPickThreads / 64;
+constexpr int kBins = 2048;  // 11 bits of a key: the first of them spread masses over some tens of bins
+constexpr int kMostEach = 32;  // tokens per thread that stay in registers
 
-// One workgroup per list: the topk-th key (in the order of mass_key) digit by digit, 8 bits at a time, from counts
-// in LDS, then a stable compaction of what is at or before it; each wave has a run of the tokens.
+// A list's masses: EACH tokens of a thread in registers, read and summed once, or (EACH = 0) from memory
+// in every pass. Token `it` of a thread is t0 + 64 it + lane; each wave has a run of the tokens.
+template <int EACH>
+struct ListMasses {
+  float x[EACH > 0 ? EACH : 1];
+  const float* at;
+  int t0, n, steps;
+  __device__ __forceinline__ ListMasses(const MassPromptLaunch& a, int list, int n_, int wave, int lane) : n(n_) {
+    if constexpr (EACH > 0) {
+      steps = EACH;
+      t0 = wave * EACH * 64 + lane;
+      const int b = list / a.H, h = list % a.H, G = a.Hq / a.H;
+      const float* p = a.mass + ((int64_t)b * a.Hq + h * G) * a.T;
+      if (G == 1) {
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) x[i] = t0 + 64 * i < n ? p[t0 + 64 * i] : 0.f;
+        return;
+      }
+#pragma unroll
+      for (int i0 = 0; i0 < EACH; i0 += 4) {  // 4 tokens' loads of all heads at a time
+        double s[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[i] = p[min(t0 + 64 * (i0 + i), a.T - 1)];
+        for (int g = 1; g < G; ++g)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s[i] += p[(int64_t)g * a.T + min(t0 + 64 * (i0 + i), a.T - 1)];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i0 + i] = (float)s[i];
+      }
+    } else {
+      at = a.sums + (int64_t)list * a.T;
+      steps = (n + kPickThreads - 1) / kPickThreads;
+      t0 = wave * steps * 64 + lane;
+    }
+  }
+  template <class F>
+  __device__ __forceinline__ void each(F&& f) const {
+    if constexpr (EACH > 0) {
+#pragma unroll
+      for (int i = 0; i < EACH; ++i) f(t0 + 64 * i, x[i]);
+    } else {
+      for (int i = 0; i < steps; ++i) {
+        const int t = t0 + 64 * i;
+        f(t, t < n ? at[t] : 0.f);
+      }
+    }
+  }
+};
+
+// One workgroup per list: the topk-th key (in the order of mass_key) 11, 11 and 10 bits at a time, from counts in
+// LDS, then a stable compaction of what is at or before it.
+template <int EACH>
 __global__ __launch_bounds__(kPickThreads) void mass_pick_kernel(MassPromptLaunch a) {
-  __shared__ __align__(16) int hist[256];
-  __shared__ int keep_sh[kPickWaves], equal_sh[kPickWaves];
+  __shared__ __align__(16) int hist[kBins];
+  __shared__ int total_sh[kPickWaves], keep_sh[kPickWaves], equal_sh[kPickWaves];
   __shared__ uint32_t prefix_sh;
   __shared__ int need_sh;
   const int list = blockIdx.x, b = list / a.H, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const int n = a.lens ? clampi(a.lens[b], 0, a.T) : a.T;
-  const float* x = a.sums + (int64_t)list * a.T;
+  const ListMasses<EACH> x(a, list, n, wave, lane);
   int32_t* pos = a.pos + (int64_t)list * a.S;
   float* prio = a.prio + (int64_t)list * a.S;
   const int lo = min(a.sinks, n), hi = max(lo, (int)max((int64_t)n - a.window, (int64_t)lo));
@@ -170,48 +308,47 @@ __global__ __launch_bounds__(kPickThreads) void mass_pick_kernel(MassPromptLaunc
   uint32_t prefix = 0;
   int need = min(a.topk, hi - lo);  // how many of those that begin with `prefix` are kept
   if (!all)
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      if (tid < 256) hist[tid] = 0;
+#pragma unroll
+    for (int pass = 0; pass < 3; ++pass) {
+      const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, above = pass == 0 ? 32 : pass == 1 ? 21 : 10;
+      const uint32_t bins = pass == 2 ? 1023u : 2047u;
+      reinterpret_cast<int2*>(hist)[tid] = int2{0, 0};
       __syncthreads();
-      for (int t = lo + tid; t < hi; t += kPickThreads) {
-        const uint32_t k = mass_key(x[t]);
-        if (shift == 24 || (k >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&hist[(k >> shift) & 255], 1);
+      x.each([&](int t, float v) __attribute__((always_inline)) {
+        const uint32_t k = mass_key(v);
+        if (t >= lo && t < hi && (pass == 0 || (k >> above) == (prefix >> above))) atomicAdd(&hist[(k >> shift) & bins], 1);
+      });
+      __syncthreads();
+      // Two bins a thread: the one where the counts reach `need`.
+      const int2 c = reinterpret_cast<const int2*>(hist)[tid];
+      const int mine = c.x + c.y;
+      int upto = mine;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const int y = __shfl_up(upto, o);
+        if (lane >= o) upto += y;
       }
+      if (lane == 63) total_sh[wave] = upto;
       __syncthreads();
-      if (wave == 0) {  // four bins a lane: the one where the counts reach `need`
-        const int4 c = *reinterpret_cast<const int4*>(hist + 4 * lane);
-        const int mine = c.x + c.y + c.z + c.w;
-        int upto = mine;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-          const int y = __shfl_up(upto, o);
-          if (lane >= o) upto += y;
-        }
-        const int before = upto - mine;
-        if (before < need && need <= upto) {
-          int rest = need - before, d = 0;
-          const int each[3] = {c.x, c.y, c.z};
-#pragma unroll
-          for (int i = 0; i < 3; ++i)
-            if (d == i && rest > each[i]) rest -= each[i], ++d;
-          prefix_sh = prefix | ((uint32_t)(4 * lane + d) << shift);
-          need_sh = rest;
-        }
+      for (int w = 0; w < wave; ++w) upto += total_sh[w];
+      const int before = upto - mine;
+      if (before < need && need <= upto) {
+        const bool second = need > before + c.x;
+        prefix_sh = prefix | ((uint32_t)(2 * tid + (second ? 1 : 0)) << shift);
+        need_sh = need - before - (second ? c.x : 0);
       }
       __syncthreads();
       prefix = prefix_sh, need = need_sh;
     }
 
   // Tokens before the cutoff key are kept, and of those that have it the first `need`.
-  const int span = ((n + kPickThreads - 1) / kPickThreads) * 64;
-  const int t0 = min(n, wave * span), t1 = min(n, t0 + span);
   int kept = 0, equal = 0;
-  for (int t = t0 + lane; t < t1; t += 64) {
-    const bool mid = t >= lo && t < hi && !all;
-    const uint32_t k = mid ? mass_key(x[t]) : 0u;
-    kept += !mid || k < prefix;
+  x.each([&](int t, float v) __attribute__((always_inline)) {
+    const bool in = t < n, mid = t >= lo && t < hi && !all;
+    const uint32_t k = mass_key(v);
+    kept += in && (!mid || k < prefix);
     equal += mid && k == prefix;
-  }
+  });
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) {
     kept += __shfl_xor(kept, o);
@@ -227,11 +364,9 @@ __global__ __launch_bounds__(kPickThreads) void mass_pick_kernel(MassPromptLaunc
   auto below = [&](uint64_t m) __attribute__((always_inline)) {
     return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0u));
   };
-  for (int first = t0; first < t1; first += 64) {
-    const int t = first + lane;
-    const bool in = t < t1, mid = in && t >= lo && t < hi && !all;
-    const float v = in ? x[t] : 0.f;
-    const uint32_t k = mid ? mass_key(v) : 0u;
+  x.each([&](int t, float v) __attribute__((always_inline)) {
+    const bool in = t < n, mid = t >= lo && t < hi && !all;
+    const uint32_t k = mass_key(v);
     const uint64_t ties = __builtin_amdgcn_ballot_w64(mid && k == prefix);
     const bool keep = in && (!mid || k < prefix || (k == prefix && eq + below(ties) < need));
     const uint64_t m = __builtin_amdgcn_ballot_w64(keep);
@@ -241,7 +376,7 @@ __global__ __launch_bounds__(kPickThreads) void mass_pick_kernel(MassPromptLaunc
     }
     at += __builtin_popcountll(m);
     eq += __builtin_popcountll(ties);
-  }
+  });
   const int held = lo + (n - hi) + min(a.topk, hi - lo);
   for (int i = held + tid; i < a.S; i += kPickThreads) {
     pos[i] = -1;
@@ -323,25 +458,41 @@ int launch_cache_mass(const CacheMassLaunch& L) {
   return i8 ? launch_mass<128, KVPOP_CACHE_INT8>(L) : launch_mass<128, KVPOP_CACHE_E4M3>(L);
 }
 
-int64_t mass_prompt_workspace_floats(int64_t B, int64_t H, int64_t Hq, int64_t T) { return Hq == H ? 0 : B * H * T; }
+// Longer prompts are summed first, into the workspace.
+constexpr int64_t kLongPrompt = (int64_t)kPickThreads * kMostEach;
+
+int64_t mass_prompt_workspace_floats(int64_t B, int64_t H, int64_t Hq, int64_t T) {
+  return Hq == H || T <= kLongPrompt ? 0 : B * H * T;
+}
 
 int64_t mass_prompt_threads(const MassPromptLaunch& L) {
   const int64_t lists = (int64_t)L.B * L.H;
-  return L.Hq == L.H ? lists * kPickThreads : lists * sum_parts(L.T) * kSumThreads;
+  return L.Hq == L.H || L.T <= kLongPrompt ? lists * kPickThreads : lists * sum_parts(L.T) * kSumThreads;
 }
 
 int launch_mass_prompt(const MassPromptLaunch& in) {
   MassPromptLaunch L = in;
   const hipStream_t st = (hipStream_t)L.stream;
-  L.sums = L.mass;
-  if (L.Hq != L.H) {
-    const int parts = sum_parts(L.T);
-    hipLaunchKernelGGL(mass_sum_kernel, dim3((unsigned)(L.B * L.H * parts)), dim3(kSumThreads), 0, st, L, parts);
-    const int e = (int)hipGetLastError();
-    if (e != 0) return e;
-    L.sums = L.workspace;
+  const dim3 lists((unsigned)(L.B * L.H)), block(kPickThreads);
+  if (L.T <= kPickThreads * 4) {
+    hipLaunchKernelGGL((mass_pick_kernel<4>), lists, block, 0, st, L);
+  } else if (L.T <= kPickThreads * 8) {
+    hipLaunchKernelGGL((mass_pick_kernel<8>), lists, block, 0, st, L);
+  } else if (L.T <= kPickThreads * 16) {
+    hipLaunchKernelGGL((mass_pick_kernel<16>), lists, block, 0, st, L);
+  } else if (L.T <= kLongPrompt) {
+    hipLaunchKernelGGL((mass_pick_kernel<kMostEach>), lists, block, 0, st, L);
+  } else {
+    L.sums = L.mass;
+    if (L.Hq != L.H) {
+      const int parts = sum_parts(L.T);
+      hipLaunchKernelGGL(mass_sum_kernel, dim3((unsigned)(L.B * L.H * parts)), dim3(kSumThreads), 0, st, L, parts);
+      const int e = (int)hipGetLastError();
+      if (e != 0) return e;
+      L.sums = L.workspace;
+    }
+    hipLaunchKernelGGL((mass_pick_kernel<0>), lists, block, 0, st, L);
   }
-  hipLaunchKernelGGL(mass_pick_kernel, dim3((unsigned)(L.B * L.H)), dim3(kPickThreads), 0, st, L);
   return (int)hipGetLastError();
 }
 

@@ -528,9 +528,11 @@ __global__ __launch_bounds__(256) void mlstm_scan_kernel(MlstmLaunch a, int bloc
   double m = scalars(part(0), D)->from, defined = m;
   constexpr int kAhead = 8;
   f32x4 next[kAhead];
+  auto fetch = [&](int i0) __attribute__((always_inline)) {
 #pragma unroll
-  for (int j = 0; j < kAhead; ++j)
-    if (mine && j < a.segs) next[j] = *reinterpret_cast<const f32x4*>(part(j) + e);
+    for (int j = 0; j < kAhead; ++j) next[j] = *reinterpret_cast<const f32x4*>(part(min(i0 + j, a.segs - 1)) + (mine ? e : 0));
+  };
+  fetch(0);
   for (int base = 0; base < a.segs; base += kScanSegments) {
     const int count = min(kScanSegments, a.segs - base);
     __syncthreads();
@@ -565,18 +567,18 @@ __global__ __launch_bounds__(256) void mlstm_scan_kernel(MlstmLaunch a, int bloc
       if (blockIdx.x % blocks == 0 && base + i > 0) scalars(part(base + i), D)->from = from_sh[i];
     }
     __syncthreads();
-    if (mine)
-      for (int i0 = base; i0 < base + count; i0 += kAhead) {
+    for (int i0 = base; i0 < base + count; i0 += kAhead) {
+      f32x4 now[kAhead];
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
-          const int i = i0 + j;
-          if (i >= base + count) break;
-          const f32x4 add = next[j];
-          if (i + kAhead < a.segs) next[j] = *reinterpret_cast<const f32x4*>(part(i + kAhead) + e);
-          *reinterpret_cast<f32x4*>(part(i) + e) = x;
-          x = scaled(x, keep_sh[i - base]) + add * put_sh[i - base];
+      for (int j = 0; j < kAhead; ++j) now[j] = next[j];
+      if (i0 + kAhead < a.segs) fetch(i0 + kAhead);
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j)
+        if (i0 + j < base + count) {
+          if (mine) *reinterpret_cast<f32x4*>(part(i0 + j) + e) = x;
+          x = scaled(x, keep_sh[i0 + j - base]) + now[j] * put_sh[i0 + j - base];
         }
-      }
+    }
   }
   if (held) {
     *reinterpret_cast<f32x4*>(held) = gone(m) ? x : x * pow2(m - defined);

@@ -36,7 +36,7 @@ def retained(B=2, H=2, S=20, pos=1 * GB, prio=2 * GB, held=3 * GB):
     return kv.KvpopRetainC(B, H, S, pos, prio, held)
 
 
-def prompt(s=None, T=50, Hq=4, mass=4 * GB, lens=None, sinks=2, w=3, k=15, ws=5 * GB, size=None):
+def prompt(s=None, T=40000, Hq=4, mass=4 * GB, lens=None, sinks=2, w=3, k=15, ws=5 * GB, size=None):
     s = s or retained()
     size = kv.kvpop_mass_prompt_workspace_size(s.batch, s.n_heads, Hq, T) if size is None else size
     return kv.lib().kvpop_mass_prompt(ctypes.byref(s), T, Hq, mass, lens, sinks, w, k, ws, size, None)
@@ -89,9 +89,9 @@ def test_prompt_and_step_checks():
         assert prompt(**kw) == EINVAL, kw
     for kw in (dict(T=(1 << 24) + 1), dict(mass=4 * GB + 2), dict(lens=8 * GB + 1), dict(ws=5 * GB + 8)):
         assert prompt(**kw) == EUNS, kw
-    assert kv.kvpop_mass_prompt_workspace_size(2, 2, 4, 50) == 2 * 2 * 50 * 4
-    assert kv.kvpop_mass_prompt_workspace_size(2, 2, 2, 50) == 0
-    assert kv.kvpop_mass_prompt_workspace_size(0, 2, 4, 50) == kv.kvpop_mass_prompt_workspace_size(2, 2, 3, 50) == 0
+    assert kv.kvpop_mass_prompt_workspace_size(2, 2, 4, 40000) == 2 * 2 * 40000 * 4
+    assert kv.kvpop_mass_prompt_workspace_size(2, 2, 2, 40000) == kv.kvpop_mass_prompt_workspace_size(2, 2, 4, 32768) == 0
+    assert kv.kvpop_mass_prompt_workspace_size(0, 2, 4, 40000) == kv.kvpop_mass_prompt_workspace_size(2, 2, 3, 40000) == 0
     for kw in (dict(q=None), dict(slot=None), dict(slot=4 * GB), dict(slot=3 * GB), dict(q=1 * GB)):
         assert step(**kw) == EINVAL, kw
     for kw in (dict(q=4 * GB + 2), dict(slot=5 * GB + 2)):
