@@ -18,7 +18,7 @@ namespace {
 __device__ __forceinline__ uint32_t mass_key(float x) { return x != x ? 0u : desc_key(x); }
 
 constexpr int kWaves = 4;
-constexpr int kQueries = 64;  // (token, head) rows that a workgroup shares at a time
+constexpr int kQueries = 128;  // (token, head) rows that a workgroup shares at a time
 
 // 16 keys of a list, widened to 16 bits, and what is known of them.
 template <int D, int FMT>
@@ -87,14 +87,16 @@ __device__ __forceinline__ float lse2(float x) { return x == neg_inf() ? -neg_in
 // ((token, head) rows, tokens slowest). S = K Q^T puts keys on the accumulator's rows and queries on its
 // columns; a lane adds up its column's probabilities and the 16 lanes of a row join at the end. Nothing is
 // shared between workgroups, and a mass has one writer.
-// MANY: rows pass through LDS in f16, 64 at a time, widened once for all waves; else (16 rows at most)
-// each wave takes them from memory.
+// MANY: rows pass through LDS in f16, 128 at a time, widened once, and 8 waves take them: two for
+// each 16 KT keys, with half of the rows each (a lane's chain of sums is the time; twice the waves hide it).
+// Else (16 rows at most) each wave takes them from memory.
 template <int D, int FMT, int KT, bool MANY>
-__global__ __launch_bounds__(64 * kWaves) void cache_mass_kernel(CacheMassLaunch a, int blocks) {
+__global__ __launch_bounds__(64 * kWaves * (MANY ? 2 : 1)) void cache_mass_kernel(CacheMassLaunch a, int blocks) {
   constexpr int KS = D / 32, QS = D + 8;
   __shared__ __align__(16) uint16_t q_sh[MANY ? kQueries * QS : 8];
-  __shared__ float c_sh[MANY ? kQueries : 1], lse_sh[MANY ? kQueries : 1];
-  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  __shared__ float c_sh[MANY ? kQueries : 1], lse_sh[MANY ? kQueries : 1], half_sh[MANY ? kWaves * 16 * KT : 1];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane((tid >> 6) % kWaves), half = __builtin_amdgcn_readfirstlane(tid / (64 * kWaves));
   const int g = lane >> 4, c = lane & 15;
   const int list = blockIdx.x / blocks, key0 = ((blockIdx.x % blocks) * kWaves + wave) * 16 * KT;
   const int b = list / a.c.H, h = list % a.c.H, G = a.Hq / a.c.H;
@@ -111,12 +113,19 @@ __global__ __launch_bounds__(64 * kWaves) void cache_mass_kernel(CacheMassLaunch
 #pragma unroll
   for (int s = 0; s < KT; ++s) k[s].load(a, id[s], key0 + 16 * s, lgP, g, c);
 
+  // The old masses are on their way meanwhile. Lane c < 4 of a group has its key 4 g + c.
+  float* mass = a.mass + (int64_t)list * a.S;
+  float old[KT];
+#pragma unroll
+  for (int s = 0; s < KT; ++s) old[s] = a.decay > 0.f ? mass[min(key0 + 16 * s + 4 * g + (c & 3), end - 1)] : 0.f;
+
   float sum[KT][4] = {};
   // 16 rows from r0 on against the wave's keys; `edge`: some row may not see some key, or a page is missing.
   auto add = [&](const H8 (&q)[KS], float cq, float lse, int row, bool edge) __attribute__((always_inline)) {
     const int seen = row < R ? L - (nq - 1 - row / G) : 0;
 #pragma unroll
     for (int s = 0; s < KT; ++s) {
+      if (!MANY) k[s].widen();
       f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int m = 0; m < KS; ++m) acc = mfma16(k[s].k[m].v, q[m].v, acc);
@@ -137,8 +146,6 @@ __global__ __launch_bounds__(64 * kWaves) void cache_mass_kernel(CacheMassLaunch
     H8 q[KS];
     x.half(q, e);
     const float lse = some ? lse2(a.lse[((int64_t)b * a.Hq + qh) * a.N + qi]) : 0.f;
-#pragma unroll
-    for (int s = 0; s < KT; ++s) k[s].widen();
     add(q, __builtin_ldexpf(a.scale * kLog2e, e), lse, c, true);
   } else {
 #pragma unroll
@@ -169,11 +176,11 @@ __global__ __launch_bounds__(64 * kWaves) void cache_mass_kernel(CacheMassLaunch
       if ((tid & 3) == 0) c_sh[mine] = __builtin_ldexpf(a.scale * kLog2e, e), lse_sh[mine] = lse2(lse);
       __syncthreads();
       if (r0 + kQueries < R) fetch(r0 + kQueries);
-      const int rows = min(kQueries, R - r0);
       // All of these rows see all of the wave's keys (the first sees the fewest).
-      const bool whole = pages && rows == kQueries && key0 + 16 * KT <= L - (nq - 1 - r0 / G);
+      const bool whole = pages && r0 + kQueries <= R && key0 + 16 * KT <= L - (nq - 1 - r0 / G);
 #pragma unroll
-      for (int i = 0; i < kQueries; i += 16) {
+      for (int x = 0; x < kQueries / 2; x += 16) {
+        const int i = half * (kQueries / 2) + x;
         H8 q[KS];
 #pragma unroll
         for (int m = 0; m < KS; ++m) q[m].v = *reinterpret_cast<const f16x8*>(q_sh + (i + c) * QS + (D / 4) * g + 8 * m);
@@ -184,19 +191,29 @@ __global__ __launch_bounds__(64 * kWaves) void cache_mass_kernel(CacheMassLaunch
       }
     }
   }
-#pragma unroll
-  for (int s = 0; s < KT; ++s)
-#pragma unroll
-    for (int r = 0; r < 4; ++r)
-#pragma unroll
-      for (int o = 1; o < 16; o <<= 1) sum[s][r] += __shfl_xor(sum[s][r], o);
-  // Lane c < 4 of a group has its key 4 g + c.
-  float* mass = a.mass + (int64_t)list * a.S;
+  // The sum over a row's 16 lanes: pairs exchange what the other keeps, so that lane c ends with its key 4 g + (c & 3).
+  float mine[KT];
 #pragma unroll
   for (int s = 0; s < KT; ++s) {
-    const float more = c == 0 ? sum[s][0] : c == 1 ? sum[s][1] : c == 2 ? sum[s][2] : sum[s][3];
+    const bool odd = c & 1, high = c & 2;
+    const float x = (odd ? sum[s][1] : sum[s][0]) + __shfl_xor(odd ? sum[s][0] : sum[s][1], 1);
+    const float y = (odd ? sum[s][3] : sum[s][2]) + __shfl_xor(odd ? sum[s][2] : sum[s][3], 1);
+    float z = (high ? y : x) + __shfl_xor(high ? x : y, 2);
+    z += __shfl_xor(z, 4);
+    mine[s] = z + __shfl_xor(z, 8);
+  }
+  if constexpr (MANY) {
+#pragma unroll
+    for (int s = 0; s < KT; ++s)
+      if (half && c < 4) half_sh[(wave * KT + s) * 16 + 4 * g + c] = mine[s];
+    __syncthreads();
+    if (half) return;
+  }
+#pragma unroll
+  for (int s = 0; s < KT; ++s) {
+    const float more = mine[s] + (MANY ? half_sh[MANY ? (wave * KT + s) * 16 + 4 * g + (c & 3) : 0] : 0.f);
     const int key = key0 + 16 * s + 4 * g + c;
-    if (c < 4 && key < end) mass[key] = a.decay > 0.f ? __builtin_fmaf(a.decay, mass[key], more) : more;
+    if (c < 4 && key < end) mass[key] = a.decay > 0.f ? __builtin_fmaf(a.decay, old[s], more) : more;
   }
 }
 
@@ -213,7 +230,7 @@ int launch_mass(const CacheMassLaunch& L) {
   const int blocks = mass_blocks(L);
   const dim3 grid((unsigned)(L.c.B * L.c.H * blocks)), block(64 * kWaves);
   if (many_rows(L))
-    hipLaunchKernelGGL((cache_mass_kernel<D, FMT, 2, true>), grid, block, 0, (hipStream_t)L.stream, L, blocks);
+    hipLaunchKernelGGL((cache_mass_kernel<D, FMT, 2, true>), grid, dim3(128 * kWaves), 0, (hipStream_t)L.stream, L, blocks);
   else
     hipLaunchKernelGGL((cache_mass_kernel<D, FMT, 4, false>), grid, block, 0, (hipStream_t)L.stream, L, blocks);
   return (int)hipGetLastError();
@@ -241,57 +258,75 @@ constexpr int kPickThreads = 1024, kPickWaves = kPickThreads / 64;
 constexpr int kBins = 2048;  // 11 bits of a key: the first of them spread masses over some tens of bins
 constexpr int kMostEach = 32;  // tokens per thread that stay in registers
 
-// A list's masses: EACH tokens of a thread in registers, read and summed once, or (EACH = 0) from memory
-// in every pass. Token `it` of a thread is t0 + 64 it + lane; each wave has a run of the tokens.
+// A list's keys (mass_key; kNoKey outside [lo, hi), which is behind every key): EACH tokens of a thread in registers, whose
+// masses are read and summed once, or (EACH = 0) from memory in every pass. Token `i` of a thread is
+// t0 + 64 i; each wave has a run of the tokens.
+constexpr uint32_t kNoKey = 0xFFFFFFFFu;
+__device__ __forceinline__ float key_mass(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k : ~k & 0x7FFFFFFFu); }
+
 template <int EACH>
-struct ListMasses {
-  float x[EACH > 0 ? EACH : 1];
+struct ListKeys {
+  uint32_t k[EACH > 0 ? EACH : 1];
   const float* at;
-  int t0, n, steps;
-  __device__ __forceinline__ ListMasses(const MassPromptLaunch& a, int list, int n_, int wave, int lane) : n(n_) {
+  int t0, lo, hi, steps;
+  // `edge` gets the tokens of [0, lo) and [hi, n) with their masses.
+  template <class F>
+  __device__ __forceinline__ ListKeys(const MassPromptLaunch& a, int list, int n, int lo_, int hi_, int wave, int lane, F&& edge)
+      : lo(lo_), hi(hi_) {
     if constexpr (EACH > 0) {
       steps = EACH;
       t0 = wave * EACH * 64 + lane;
       const int b = list / a.H, h = list % a.H, G = a.Hq / a.H;
       const float* p = a.mass + ((int64_t)b * a.Hq + h * G) * a.T;
-      if (G == 1) {
+      constexpr int W = EACH < 8 ? EACH : 8;  // tokens of 4 heads whose loads are on their way at once
 #pragma unroll
-        for (int i = 0; i < EACH; ++i) x[i] = t0 + 64 * i < n ? p[t0 + 64 * i] : 0.f;
-        return;
-      }
+      for (int i0 = 0; i0 < EACH; i0 += W) {
+        double s[W] = {};
+        for (int g0 = 0; g0 < G; g0 += 4) {
+          float y[4][W];
 #pragma unroll
-      for (int i0 = 0; i0 < EACH; i0 += 4) {  // 4 tokens' loads of all heads at a time
-        double s[4];
+          for (int g = 0; g < 4; ++g)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s[i] = p[min(t0 + 64 * (i0 + i), a.T - 1)];
-        for (int g = 1; g < G; ++g)
+            for (int i = 0; i < W; ++i) y[g][i] = p[(int64_t)min(g0 + g, G - 1) * a.T + min(t0 + 64 * (i0 + i), a.T - 1)];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) s[i] += p[(int64_t)g * a.T + min(t0 + 64 * (i0 + i), a.T - 1)];
+          for (int g = 0; g < 4; ++g)
+            if (g0 + g < G)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[i0 + i] = (float)s[i];
+              for (int i = 0; i < W; ++i) s[i] = g0 + g == 0 ? (double)y[g][i] : s[i] + y[g][i];
+        }
+#pragma unroll
+        for (int i = 0; i < W; ++i) k[i0 + i] = key(t0 + 64 * (i0 + i), (float)s[i], n, edge);
       }
     } else {
       at = a.sums + (int64_t)list * a.T;
       steps = (n + kPickThreads - 1) / kPickThreads;
       t0 = wave * steps * 64 + lane;
+      for (int i = 0; i < steps; ++i)
+        if (t0 + 64 * i < n) key(t0 + 64 * i, at[t0 + 64 * i], n, edge);
     }
+  }
+  template <class F>
+  __device__ __forceinline__ uint32_t key(int t, float x, int n, F&& edge) const {
+    if (t >= lo && t < hi) return mass_key(x);
+    if (t < n) edge(t, x);
+    return kNoKey;
   }
   template <class F>
   __device__ __forceinline__ void each(F&& f) const {
     if constexpr (EACH > 0) {
 #pragma unroll
-      for (int i = 0; i < EACH; ++i) f(t0 + 64 * i, x[i]);
+      for (int i = 0; i < EACH; ++i) f(t0 + 64 * i, k[i]);
     } else {
       for (int i = 0; i < steps; ++i) {
         const int t = t0 + 64 * i;
-        f(t, t < n ? at[t] : 0.f);
+        f(t, t >= lo && t < hi ? mass_key(at[t]) : kNoKey);
       }
     }
   }
 };
 
-// One workgroup per list: the topk-th key (in the order of mass_key) 11, 11 and 10 bits at a time, from counts in
-// LDS, then a stable compaction of what is at or before it.
+// One workgroup per list: the topk-th key 11, 11 and 10 bits at a time, from counts in LDS, then a stable compaction
+// of what is at or before it. The sinks' and the window's slots are known before.
 template <int EACH>
 __global__ __launch_bounds__(kPickThreads) void mass_pick_kernel(MassPromptLaunch a) {
   __shared__ __align__(16) int hist[kBins];
@@ -300,23 +335,28 @@ __global__ __launch_bounds__(kPickThreads) void mass_pick_kernel(MassPromptLaunc
   __shared__ int need_sh;
   const int list = blockIdx.x, b = list / a.H, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const int n = a.lens ? clampi(a.lens[b], 0, a.T) : a.T;
-  const ListMasses<EACH> x(a, list, n, wave, lane);
   int32_t* pos = a.pos + (int64_t)list * a.S;
   float* prio = a.prio + (int64_t)list * a.S;
   const int lo = min(a.sinks, n), hi = max(lo, (int)max((int64_t)n - a.window, (int64_t)lo));
-  const bool all = hi - lo <= a.topk;
-  uint32_t prefix = 0;
-  int need = min(a.topk, hi - lo);  // how many of those that begin with `prefix` are kept
-  if (!all)
+  const int middle = min(a.topk, hi - lo), held = lo + middle + (n - hi);
+  const ListKeys<EACH> x(a, list, n, lo, hi, wave, lane, [&](int t, float v) {
+    const int slot = t < lo ? t : lo + middle + (t - hi);
+    pos[slot] = t;
+    prio[slot] = v;
+  });
+  // Keys before `cut` are kept, and of those that are it the first `need`.
+  uint32_t cut = kNoKey;
+  int need = 0;
+  if (hi - lo > a.topk) {
+    cut = 0, need = a.topk;
 #pragma unroll
     for (int pass = 0; pass < 3; ++pass) {
-      const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, above = pass == 0 ? 32 : pass == 1 ? 21 : 10;
+      const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, above = pass == 1 ? 21 : 10;
       const uint32_t bins = pass == 2 ? 1023u : 2047u;
       reinterpret_cast<int2*>(hist)[tid] = int2{0, 0};
       __syncthreads();
-      x.each([&](int t, float v) __attribute__((always_inline)) {
-        const uint32_t k = mass_key(v);
-        if (t >= lo && t < hi && (pass == 0 || (k >> above) == (prefix >> above))) atomicAdd(&hist[(k >> shift) & bins], 1);
+      x.each([&](int, uint32_t k) __attribute__((always_inline)) {
+        if (pass == 0 ? k != kNoKey : (k >> above) == (cut >> above)) atomicAdd(&hist[(k >> shift) & bins], 1);
       });
       __syncthreads();
       // Two bins a thread: the one where the counts reach `need`.
@@ -334,29 +374,22 @@ __global__ __launch_bounds__(kPickThreads) void mass_pick_kernel(MassPromptLaunc
       const int before = upto - mine;
       if (before < need && need <= upto) {
         const bool second = need > before + c.x;
-        prefix_sh = prefix | ((uint32_t)(2 * tid + (second ? 1 : 0)) << shift);
+        prefix_sh = cut | ((uint32_t)(2 * tid + (second ? 1 : 0)) << shift);
         need_sh = need - before - (second ? c.x : 0);
       }
       __syncthreads();
-      prefix = prefix_sh, need = need_sh;
+      cut = prefix_sh, need = need_sh;
     }
-
-  // Tokens before the cutoff key are kept, and of those that have it the first `need`.
-  int kept = 0, equal = 0;
-  x.each([&](int t, float v) __attribute__((always_inline)) {
-    const bool in = t < n, mid = t >= lo && t < hi && !all;
-    const uint32_t k = mass_key(v);
-    kept += in && (!mid || k < prefix);
-    equal += mid && k == prefix;
-  });
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    kept += __shfl_xor(kept, o);
-    equal += __shfl_xor(equal, o);
   }
+  int kept = 0, equal = 0;
+  x.each([&](int, uint32_t k) __attribute__((always_inline)) {
+    kept += __builtin_popcountll(__builtin_amdgcn_ballot_w64(k < cut));
+    equal += __builtin_popcountll(__builtin_amdgcn_ballot_w64(k == cut));
+  });
+  if (need == 0) equal = 0;
   if (lane == 0) keep_sh[wave] = kept, equal_sh[wave] = equal;
   __syncthreads();
-  int at = 0, eq = 0;
+  int at = lo, eq = 0;
   for (int w = 0; w < wave; ++w) {
     at += keep_sh[w] + max(0, min(need - eq, equal_sh[w]));
     eq += equal_sh[w];
@@ -364,20 +397,20 @@ __global__ __launch_bounds__(kPickThreads) void mass_pick_kernel(MassPromptLaunc
   auto below = [&](uint64_t m) __attribute__((always_inline)) {
     return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0u));
   };
-  x.each([&](int t, float v) __attribute__((always_inline)) {
-    const bool in = t < n, mid = t >= lo && t < hi && !all;
-    const uint32_t k = mass_key(v);
-    const uint64_t ties = __builtin_amdgcn_ballot_w64(mid && k == prefix);
-    const bool keep = in && (!mid || k < prefix || (k == prefix && eq + below(ties) < need));
+  x.each([&](int t, uint32_t k) __attribute__((always_inline)) {
+    bool keep = k < cut;
+    const uint64_t ties = __builtin_amdgcn_ballot_w64(k == cut);
+    if (ties != 0 && need > 0) {
+      keep = keep || (k == cut && eq + below(ties) < need);
+      eq += __builtin_popcountll(ties);
+    }
     const uint64_t m = __builtin_amdgcn_ballot_w64(keep);
     if (keep) {
       pos[at + below(m)] = t;
-      prio[at + below(m)] = v;
+      prio[at + below(m)] = key_mass(k);
     }
     at += __builtin_popcountll(m);
-    eq += __builtin_popcountll(ties);
   });
-  const int held = lo + (n - hi) + min(a.topk, hi - lo);
   for (int i = held + tid; i < a.S; i += kPickThreads) {
     pos[i] = -1;
     prio[i] = 0.f;
@@ -450,7 +483,7 @@ __global__ __launch_bounds__(kStepThreads) void mass_step_kernel(RetainLaunch a)
 
 }  // namespace
 
-int64_t cache_mass_threads(const CacheMassLaunch& L) { return (int64_t)L.c.B * L.c.H * mass_blocks(L) * 64 * kWaves; }
+int64_t cache_mass_threads(const CacheMassLaunch& L) { return (int64_t)L.c.B * L.c.H * mass_blocks(L) * 128 * kWaves; }
 
 int launch_cache_mass(const CacheMassLaunch& L) {
   const bool i8 = L.c.format == KVPOP_CACHE_INT8;
