@@ -617,7 +617,10 @@ __global__ __launch_bounds__(MODE == kDkv ? 512 : 256, 2) void mlstm_kernel(Mlst
   Gates& G = sh.G;
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, c = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane((tid >> 6) & 3), role = REV ? __builtin_amdgcn_readfirstlane(tid >> 8) : 0;
-  const int seg = blockIdx.x % a.segs, list = blockIdx.x / a.segs, b = list / a.H, h = list % a.H;
+  // The first sweep went over the heads in order: the read-outs and dq begin with its last ones, whose rows the
+  // memory-side cache still has, and dk and dv where dq ended.
+  const int block = REV ? blockIdx.x : gridDim.x - 1 - blockIdx.x;
+  const int seg = block % a.segs, list = block / a.segs, b = list / a.H, h = list % a.H;
   const int n = a.lens ? clampi(a.lens[b], 0, a.T) : a.T, chunks = (n + kChunk - 1) / kChunk;
   const int first = min(seg * a.seg_chunks, chunks), count = min((seg + 1) * a.seg_chunks, chunks) - first;
   auto chunk_at = [&](int i) { return REV ? first + count - 1 - i : first + i; };
