@@ -55,8 +55,11 @@ __device__ __forceinline__ f32x4 mfma(const bf16x8& a, const bf16x8& b, const f3
 }
 // The sum over the lanes l % 16 + 16 k, on all of them.
 __device__ __forceinline__ float sum_groups(float x) {
-  x += __shfl_xor(x, 16);
-  return x + __shfl_xor(x, 32);
+  // Swapped with itself, x becomes its two halves (its even and odd rows of 16) on all lanes.
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
 // A lane's value from lanes before it, without LDS: row_shr within 16 lanes, then the last lane of the row (of the
@@ -236,9 +239,15 @@ struct Tile {
   __device__ __forceinline__ void load(const Rows& a, int b, int h, int t0, int shift, int n, int tid) {
     const uint16_t* p = a.ptr + b * a.sb + h * a.sh + 8 * (tid % (D / 8));
     const int first = t0 - shift + tid / (D / 8);
+    if (t0 >= shift && t0 + kChunk <= n) {
+      p += first * a.st;
 #pragma unroll
-    for (int i = 0; i < kPer; ++i)
-      x[i] = *reinterpret_cast<const u32x4*>(p + min(max(first + i * (THREADS * 8 / D), 0), n - 1) * a.st);
+      for (int i = 0; i < kPer; ++i) x[i] = *reinterpret_cast<const u32x4*>(p + i * (THREADS * 8 / D) * a.st);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kPer; ++i)
+        x[i] = *reinterpret_cast<const u32x4*>(p + min(max(first + i * (THREADS * 8 / D), 0), n - 1) * a.st);
+    }
   }
   __device__ __forceinline__ void store(uint16_t* sh, int t0, int shift, int n, int tid) const {
     const int row = tid / (D / 8);
@@ -358,7 +367,8 @@ struct Weights {
 // The two columns' sum, in lanes of even c.
 __device__ __forceinline__ f32x4 both_columns(f32x4 z) {
 #pragma unroll
-  for (int r = 0; r < 4; ++r) z[r] += __shfl_xor(z[r], 1);
+  for (int r = 0; r < 4; ++r)  // lanes 1, 0, 3, 2 of each four
+    z[r] += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(z[r]), 0xB1, 0xf, 0xf, true));
   return z;
 }
 
@@ -740,12 +750,6 @@ __global__ __launch_bounds__(MODE == kDkv ? 512 : 256, 2) void mlstm_kernel(Mlst
     }
     if (it + 1 < count) load(chunk_at(it + 1));
 
-    const Update<REV> up(G, slot, m);
-    if (tid < kChunk) {
-      const float w = up.weight(G, at + tid);
-      sh.w[tid] = w;
-      sh.wz.set(tid, REV ? w * G.d[at + tid] : w);
-    }
     {  // The masked product, transposed: this lane has row j and columns 4 g + r of each 16.
       const int j = 16 * wave + c, rid = G.rid[at + j];
       double rho;   // the row's exponent within the chunk
@@ -832,7 +836,15 @@ __global__ __launch_bounds__(MODE == kDkv ? 512 : 256, 2) void mlstm_kernel(Mlst
         if (MODE != kFwd) sh.far_z[role][j] = MODE == kDq ? far * alpha : far;
       }
     }
+    if (role == 0 && wave == (REV ? 3 : 0)) {  // the wave that has the least of it
+      const Update<REV> up(G, slot, m);
+      const float w = up.weight(G, at + lane);
+      sh.w[lane] = w;
+      sh.wz.set(lane, REV ? w * G.d[at + lane] : w);
+    }
     __syncthreads();
+    const Update<REV> up(G, slot, m);
+    const double added = up.added(G, slot), gates_sum = G.resets[slot] ? -__builtin_inf() : G.sum[slot];
 
     bf16x8 cf[2][NT];
 #pragma unroll
@@ -862,82 +874,95 @@ __global__ __launch_bounds__(MODE == kDkv ? 512 : 256, 2) void mlstm_kernel(Mlst
     {
       const int late = REV ? 0 : a.delay, t0 = chunk * kChunk;
       uint16_t* to = out_at + (int64_t)t0 * D;
-      // dq's rows of q, a block of rows ahead (dk's rows of k are in LDS).
+      // dq's rows of q (dk's rows of k are in LDS), two blocks of rows at a time.
       const uint16_t* from = a.q.ptr + b * a.q.sb + h * a.q.sh + wave * NT * 16 + 4 * g;
-      bf16x4 mate[NT], ahead[NT];
-      auto fetch = [&](int q) __attribute__((always_inline)) {
-        const uint16_t* p = from + min(max(t0 + 16 * q + c - a.delay, 0), n - 1) * a.q.st;
+      bf16x4 ahead[2][NT];
+      auto fetch = [&](int q0) __attribute__((always_inline)) {
 #pragma unroll
-        for (int t = 0; t < NT; ++t) ahead[t] = *reinterpret_cast<const bf16x4*>(p + 16 * t);
-      };
-      if (MODE == kDq) fetch(0);
+        for (int x = 0; x < 2; ++x) {
+          const uint16_t* p = from + min(max(t0 + 16 * (q0 + x) + c - a.delay, 0), n - 1) * a.q.st;
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int j = 16 * q + c;
-        if (MODE == kDq) {
-#pragma unroll
-          for (int t = 0; t < NT; ++t) mate[t] = ahead[t];
-          if (q < 3) fetch(q + 1);
+          for (int t = 0; t < NT; ++t) ahead[x][t] = *reinterpret_cast<const bf16x4*>(p + 16 * t);
         }
-        const float far = sh.far[role][j], fac = MODE == kFwd ? sh.out[j] : a.scale;
-        const float far_z = MODE != kFwd && with_z ? sh.far_z[role][j] : 0.f;
-        float dot = 0.f;
-        bf16x4 y[NT];
+      };
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-          const int col = (wave * NT + t) * 16 + 4 * g;
-          acc[q][t] = scaled(acc[q][t], far);
-          if (MODE != kFwd && with_z) acc[q][t] += scaled(*reinterpret_cast<const f32x4*>(sh.z[role] + col), far_z);
+      for (int q0 = 0; q0 < 4; q0 += 2) {
+        if (MODE == kDq) fetch(q0);
+        bf16x4 y[2][NT];
+        float dot[2] = {0.f, 0.f};
 #pragma unroll
-          for (int s = 0; s < 2; ++s)
-            if (REV ? 32 * s + 31 >= 16 * q : 32 * s <= 16 * q)
-              acc[q][t] = mfma(cf[s][t], row8(sh.p[role] + j * PS + 32 * s + 8 * g), acc[q][t]);
-          acc[q][t] *= fac;
-          if (REV) mate[t] = *reinterpret_cast<const bf16x4*>(sh.tile[0] + j * LS + col);
+        for (int x = 0; x < 2; ++x) {
+          const int q = q0 + x, j = 16 * q + c;
+          const float far = sh.far[role][j], fac = MODE == kFwd ? sh.out[j] : a.scale;
+          const float far_z = MODE != kFwd && with_z ? sh.far_z[role][j] : 0.f;
 #pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            y[t][r] = (__bf16)acc[q][t][r];
-            if (MODE != kFwd) dot += acc[q][t][r] * (float)mate[t][r];
+          for (int t = 0; t < NT; ++t) {
+            const int col = (wave * NT + t) * 16 + 4 * g;
+            acc[q][t] = scaled(acc[q][t], far);
+            if (MODE != kFwd && with_z) acc[q][t] += scaled(*reinterpret_cast<const f32x4*>(sh.z[role] + col), far_z);
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+              if (REV ? 32 * s + 31 >= 16 * q : 32 * s <= 16 * q)
+                acc[q][t] = mfma(cf[s][t], row8(sh.p[role] + j * PS + 32 * s + 8 * g), acc[q][t]);
+            acc[q][t] *= fac;
+            if (REV) ahead[x][t] = *reinterpret_cast<const bf16x4*>(sh.tile[0] + j * LS + col);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              y[x][t][r] = (__bf16)acc[q][t][r];
+              if (MODE != kFwd) dot[x] += acc[q][t][r] * (float)ahead[x][t][r];
+            }
           }
+          if (MODE != kFwd) dot[x] = sum_groups(dot[x]);
         }
         // The values are made before the branch: where the products' results were first read behind one, the
         // compiler had left out the wait that they need.
 #pragma unroll
-        for (int t = 0; t < NT; ++t) asm volatile("" : "+v"(y[t]), "+v"(dot));
-        if (t0 + j >= late && t0 + j < n)
+        for (int x = 0; x < 2; ++x)
 #pragma unroll
-          for (int t = 0; t < NT; ++t) *reinterpret_cast<bf16x4*>(to + 16 * q * D + 16 * t) = y[t];
-        if (MODE != kFwd) {
-          dot = sum_groups(dot);
-          if (g == 0 && (MODE == kDq || role)) sh.dig[wave][j] = dot;
+          for (int t = 0; t < NT; ++t) asm volatile("" : "+v"(y[x][t]), "+v"(dot[x]));
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const int j = 16 * (q0 + x) + c;
+          if (t0 + j >= late && t0 + j < n)
+#pragma unroll
+            for (int t = 0; t < NT; ++t) *reinterpret_cast<bf16x4*>(to + 16 * (q0 + x) * D + 16 * t) = y[x][t];
+          if (MODE != kFwd && g == 0 && (MODE == kDq || role)) sh.dig[wave][j] = dot[x];
         }
       }
     }
 
+    f32x4 add[NT];
+    if (MODE == kFwd) {
+#pragma unroll
+      for (int i = 0; i < NZ; ++i) add[i] = weighted_rows<D>(b_sh + (wave * NZ + i) * 16, sh.wz, g, c);
+    } else if (with_z) {  // a vector over this wave's own columns: sum w_t c_t
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        add[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int s = 0; s < 2; ++s) add[t] = mfma(cf[s][t], sh.wz.frag(s, g, c), add[t]);
+        add[t] = both_columns(add[t]);
+      }
+    }
     update_state<D, NT>(S, up.keep, b_sh, cf, sh.w, g, c);
     if (MODE == kFwd) {
 #pragma unroll
       for (int i = 0; i < NZ; ++i) {
         const int at_z = (wave * NZ + i) * 16 + 4 * g;
-        const f32x4 add = weighted_rows<D>(b_sh + (wave * NZ + i) * 16, sh.wz, g, c);
         f32x4* z = reinterpret_cast<f32x4*>(sh.z[0] + at_z);
         if (c == 0) {
-          const f32x4 y = scaled(*z, up.keep) + add;
+          const f32x4 y = scaled(*z, up.keep) + add[i];
           *z = y;
 #pragma unroll
           for (int r = 0; r < 4; ++r) set_zrow(at_z + r, y[r]);
         }
       }
-      defined = held_m(defined, G.resets[slot] ? -__builtin_inf() : G.sum[slot], up.added(G, slot));
-    } else if (with_z) {  // a vector over this wave's own columns: sum w_t c_t
+      defined = held_m(defined, gates_sum, added);
+    } else if (with_z) {
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
-        f32x4 add = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int s = 0; s < 2; ++s) add = mfma(cf[s][t], sh.wz.frag(s, g, c), add);
-        add = both_columns(add);
         f32x4* z = reinterpret_cast<f32x4*>(sh.z[role] + (wave * NT + t) * 16 + 4 * g);
-        if (c == 0) *z = scaled(*z, up.keep) + add;
+        if (c == 0) *z = scaled(*z, up.keep) + add[t];
       }
     }
     m = up.next;
