@@ -305,7 +305,8 @@ struct Update {
 __device__ __forceinline__ double held_m(double m, double sum, double top) { return fmax(m + sum, top); }
 
 // S <- keep S + B^T (w o C) on this wave's NT * 16 columns of C. w o C is taken as the sum of two bf16
-// (16 bits), so that what is held keeps fp32's meaning; rounded once, it would be off by 2^-9.
+// (16 bits), so that what is held is good for more than the read-outs that are made from it; rounded once, it
+// would be off by as much as they are.
 template <int D, int NT>
 __device__ __forceinline__ void update_state(f32x4 (&S)[D / 16][NT], float keep, const uint16_t* b_sh,
                                              const bf16x8 (&cf)[2][NT], const float* w_sh, int g, int c) {
@@ -856,19 +857,27 @@ __global__ __launch_bounds__(MODE == kDkv ? 512 : 256, 2) void mlstm_kernel(Mlst
     for (int q = 0; q < 4; ++q)
 #pragma unroll
       for (int t = 0; t < NT; ++t) acc[q][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-    // What is held, rounded to bf16 for the product (its terms' errors are independent; out is rounded too).
+    // What is held, rounded to bf16 for the product (its terms' errors are independent; out is rounded too). For dq it
+    // is two bf16: there o's rounding, by way of d, is a third error of that size.
 #pragma unroll
     for (int s = 0; s < D / 32; ++s) {
-      bf16x8 sf[NT];
+      bf16x8 sf[NT], low[NT];
 #pragma unroll
       for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sf[t][i] = (__bf16)S[2 * s + i / 4][t][i % 4];
+        for (int i = 0; i < 8; ++i) {
+          const float x = S[2 * s + i / 4][t][i % 4];
+          sf[t][i] = (__bf16)x;
+          if (MODE == kDq) low[t][i] = (__bf16)(x - (float)sf[t][i]);
+        }
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         const bf16x8 af = row4x2(a_sh + (16 * q + c) * LS + 32 * s + 4 * g);
 #pragma unroll
-        for (int t = 0; t < NT; ++t) acc[q][t] = mfma(sf[t], af, acc[q][t]);
+        for (int t = 0; t < NT; ++t) {
+          acc[q][t] = mfma(sf[t], af, acc[q][t]);
+          if (MODE == kDq) acc[q][t] = mfma(low[t], af, acc[q][t]);
+        }
       }
     }
     {
