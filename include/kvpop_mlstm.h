@@ -58,8 +58,9 @@ typedef struct kvpop_mlstm_state {
  * o: bf16 [B, H, T, D] contiguous; rows that are not read (t + delay >= lens[b]) are 0.
  * lse: fp32 [B, H, T] or NULL: log of x . z (normalize = 1; -inf where that is not > 0) or 0
  * (normalize = 0); -inf for rows that are not read. kvpop_mlstm_bwd takes it.
- * Products are of bf16 operands with fp32 sums: an intermediate weight, a read state's element and
- * o are each rounded to bf16 once; what is held, and x . z, are not.
+ * Products are of bf16 operands with fp32 sums: within a chunk of 64 tokens a weight times its <x, k>, a
+ * read state's element and o are each rounded to bf16 once. What is held adds a token's weight times v to
+ * 16 bits, in fp32 sums; x . z is not rounded to bf16.
  * workspace: kvpop_mlstm_fwd_workspace_size bytes of device memory, 16-byte aligned (may be NULL
  * if that is 0); its contents on entry do not matter. Calls that may run at the same time, and
  * graphs, need workspaces of their own.
@@ -81,6 +82,8 @@ size_t kvpop_mlstm_fwd_workspace_size(const kvpop_mlstm* a);
  * Rows with lse = -inf give nothing. All are bf16 and contiguous: dq (scale dx), dk, dv [B, H, T, D];
  * dig, dfg [B, H, T]; 0 for tokens and queries that take no part. do_: bf16 [B, H, T, D] (strided),
  * o: bf16 [B, H, T, D] contiguous, lse: fp32 [B, H, T].
+ * Roundings are those of kvpop_mlstm_fwd; for dq the read state's elements keep 16 bits. dfg is a running
+ * sum of differences: its error is relative to the largest of a sequence's partial sums, not to each element.
  * Nothing depends on the order of workgroups. workspace as above (kvpop_mlstm_bwd_workspace_size).
  * Errors as kvpop_mlstm_fwd. */
 typedef struct kvpop_mlstm_grads {
@@ -97,6 +100,7 @@ size_t kvpop_mlstm_bwd_workspace_size(const kvpop_mlstm* a);
 /* One token of each sequence: k, v and the gates go into what is held, then q reads it (q is that
  * of the token `delay` before; seq_len is 1, delay 0, and the rows' stride_t means nothing).
  * lens: NULL, or 0 for idle sequences, which keep what they hold and get o = 0.
+ * m is rounded to fp32 after every token: decays below half of its last place (2^-25 |m|) are lost.
  * o: bf16 [B, H, D] contiguous. Errors as kvpop_mlstm_fwd, and seq_len != 1 or delay != 0. */
 int kvpop_mlstm_step(const kvpop_mlstm* a, const kvpop_mlstm_state* state, void* o, void* stream);
 

@@ -1046,5 +1046,7 @@ def _mlstm_function():
 
 def kvpop_mlstm(q, k, v, ig, fg, scale: float = 1.0, delay: int = 0, normalize: bool = True, lens=None):
     """kvpop_mlstm_fwd as a differentiable torch function (of q, k, v, ig and fg, once): returns o. Runs on
-    the current stream."""
+    the current stream. To capture a training step, drop eager results of the same leaves first: torch keeps a
+    leaf's accumulation on the stream of the graph that lives, outside the capture; or capture
+    ``torch.autograd.grad``, which accumulates nothing."""
     return _mlstm_function().apply(q, k, v, ig, fg, float(scale), int(delay), bool(normalize), lens)
