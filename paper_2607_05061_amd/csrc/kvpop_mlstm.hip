@@ -779,7 +779,7 @@ __global__ __launch_bounds__(MODE == kDkv ? 512 : 256, 2) void mlstm_kernel(Mlst
       bf16x8 af[D / 32];
 #pragma unroll
       for (int s = 0; s < D / 32; ++s) af[s] = row8(a_sh + j * LS + 32 * s + 8 * g);
-      float den = 0.f;
+      float den = 0.f, rounded = 0.f;
       const bool plain = G.resets[slot] == 0;
       // Two tiles of 16 columns at a time: all that the product with C takes, the further ones as zeros.
 #pragma unroll
@@ -813,8 +813,8 @@ __global__ __launch_bounds__(MODE == kDkv ? 512 : 256, 2) void mlstm_kernel(Mlst
           bf16x4 p;
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            den += acc[x][r];
             p[r] = (__bf16)acc[x][r];
+            if (MODE == kFwd) den += acc[x][r], rounded += (float)p[r];
           }
           *reinterpret_cast<bf16x4*>(sh.p[role] + j * PS + 32 * half + 16 * x + 4 * g) = p;
         }
@@ -823,12 +823,16 @@ __global__ __launch_bounds__(MODE == kDkv ? 512 : 256, 2) void mlstm_kernel(Mlst
         f32x4 qz = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int s = 0; s < D / 32; ++s) qz = mfma(row8(sh.zrow + (c & 1) * LS + 32 * s + 8 * g), af[s], qz);
-        den = (sum_groups(den) + (far == 0.f ? 0.f : far * (qz[0] + qz[1]))) * a.scale;
+        const float held = far == 0.f ? 0.f : far * (qz[0] + qz[1]);
+        den = (sum_groups(den) + held) * a.scale;
+        // o is divided by the sum of the rounded weights that it is made with: what rounding leaves weighs v - o then, not
+        // v, and is nothing where a query sees one token. do . (v - o) of few tokens needs that.
+        rounded = (sum_groups(rounded) + held) * a.scale;
         const double e = G.b[at + j] - rho;  // that of the row's common factor
         float fac, lse;
         if (a.normalize) {
           const bool some = den > 0.f;
-          fac = some ? a.scale / den : 0.f;
+          fac = some ? a.scale / (rounded > 0.f ? rounded : den) : 0.f;
           lse = some ? logf(den) + (float)(e * kLog2eInv) : neg_inf();
           if (den != den) fac = lse = den;
         } else {
