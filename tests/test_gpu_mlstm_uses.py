@@ -3,6 +3,8 @@ that idle and masked tokens pass, sequences behind large gates."""
 import numpy as np
 import pytest
 
+from oracle import mlstm as om
+
 torch = pytest.importorskip("torch")
 import paper_2607_05061_amd as kv  # noqa: E402
 from cache_cases import i32  # noqa: E402
@@ -133,3 +135,33 @@ def test_a_state_outlives_masked_tokens(T):
     want = torch.matmul(q, C.double()) / torch.matmul(q, z.double().unsqueeze(-1))
     spread = torch.matmul(q.abs(), C.double().abs()) / torch.matmul(q, z.double().unsqueeze(-1)).abs()
     assert ((o.double() - want).abs() <= 3 * 2.0 ** -8 * spread).all()
+
+
+@pytest.mark.parametrize("T,D,delay", [(1, 64, 0), (2, 128, 0), (5, 64, 0), (17, 128, 1), (42, 64, 0), (300, 64, 7),
+                                       (512, 128, 0)])
+def test_queries_that_see_few_tokens(T, D, delay):
+    """A normalised read-out of one token is v itself, bit for bit, and has no gradient but v's. With few tokens do . (v - o)
+    is a small difference; dq and dk still have the error of independent roundings of their own terms: o rounded
+    (its part in do . o taken out by x . dx = 0, to a rounding of each term), the weights of a row, the result: 3 of at most
+    2^-8 / sqrt(3) in the 2-norm."""
+    rng = np.random.default_rng(40 + T)
+    B, H = 3, 4
+    x, ref = on_gpu(inputs(rng, B, H, T, D))
+    a = [x[n] for n in ARGS]
+    o, lse = kv.kvpop_mlstm_fwd(*a, delay=delay)
+    grads = kv.kvpop_mlstm_bwd(x["do"], *a, o, lse, delay=delay)
+    if delay == 0:
+        assert torch.equal(o[:, :, 0], x["v"][:, :, 0])
+    want = [np.zeros((B, H, T, D)), np.zeros((B, H, T, D))]
+    for b in range(B):
+        for h in range(H):
+            y = [ref[n][b, h] for n in ARGS]
+            exact, lse64, *_ = om.read(*y, 1.0, delay, True)
+            g = om.grads(ref["do"][b, h], *y, exact, lse64, 1.0, delay, True)[0]
+            want[0][b, h], want[1][b, h] = g[0], g[1]
+    for name, got, w, unit in (("dq", grads[0], want[0], ref["do"]), ("dk", grads[1], want[1], ref["do"])):
+        err = np.linalg.norm(got.double().cpu().numpy() - w)
+        if T == 1:  # nothing but what fp32 leaves of do . v - do . o
+            assert err <= 2.0 ** -20 * np.linalg.norm(unit) * np.linalg.norm(ref["v"]), name
+        else:
+            assert err <= 3 * 2.0 ** -8 / 3 ** 0.5 * np.linalg.norm(w), name
