@@ -17,7 +17,8 @@
  *   m_t = max(m_{t-1} + log f_t, ig_t),  C = C_t e^-m_t,  z = z_t e^-m_t;  empty: C = z = 0, m = -inf.
  *
  * Gates: ig = -inf masks a token (its k and v do not matter then, NaN included), fg = -inf forgets
- * everything exactly (where a packed sequence begins), fg = +inf nothing. NaN, ig = +inf and
+ * everything exactly (where a packed sequence begins), and so does any fg below -2^24, where an fp32 m or lse
+ * has no bits left for another token's gate; fg = +inf forgets nothing. NaN, ig = +inf and
  * elements of the other inputs that are not finite reach the results of their sequence and head only.
  */
 #ifndef KVPOP_MLSTM_H

@@ -8,7 +8,8 @@
 // one product with what is held (S, D x D, in registers), a masked product within the chunk, and the
 // update. All four sweeps are this: the read-outs (A, B, C = q, k, v), dq (do, v, k) forwards,
 // dv (k, q, do) and dk (v, do, q) backwards in time, where what is held is the gradient of C_t.
-// Exponents are sums of 64-bit running sums in units of log2: no weight loses bits to a large |b|.
+// Exponents are sums of 64-bit running sums in units of log2, which no gate makes larger than 2^31 (kForget): no
+// weight loses bits to a large |b|.
 //
 // Sequences are cut into segments for parallelism: a first sweep finds what each segment adds to
 // what is held, a scan over the segments what each one starts from, then every segment runs alone.
@@ -99,6 +100,12 @@ __device__ __forceinline__ double last_lane(double x) {
   return a.d;
 }
 
+// A gate below this forgets everything, as -inf does. Its logarithm has no bits of other gates in fp32, in which m and
+// lse are held; and a running sum that holds it keeps fewer of them the larger it is (64 bits have none beside 2^53),
+// where 64 sums of at most 2^24 keep 22 below the point.
+constexpr float kForget = -16777216.f;
+__device__ __forceinline__ bool forgets(float fg) { return fg < kForget; }
+
 // log2 sigmoid(x); 0 for +inf.
 __device__ __forceinline__ double log2_sigmoid(float x) {
   return -(double)(fmaxf(-x, 0.f) + log1pf(expf(-fabsf(x)))) * kLog2e;
@@ -139,7 +146,7 @@ struct __align__(16) Gates {
   double u[kGates];    // ig - b
   double r[kGates];    // kFwd: the largest u since the last reset; else b - lse (-inf: not read)
   double b[kGates];
-  int rid[kGates];     // resets (fg = -inf) up to here
+  int rid[kGates];     // resets (gates that forget everything) up to here
   float d[kGates];     // backward: d_u, of the query that reads here
   double sum[kBlock];  // b at the chunk's end
   double top[kBlock];  // the largest exponent that the chunk adds to what is held
@@ -172,7 +179,7 @@ __device__ __forceinline__ void chunk_gates(const MlstmLaunch& a, Gates& G, cons
   const int t = chunk * kChunk + lane, i = slot * kChunk + lane;
   const bool in = t < n, read = in && t >= a.delay;
   const float ig = in ? bf16_value(raw.ig) : neg_inf(), fg = in ? bf16_value(raw.fg) : -neg_inf();
-  const bool reset = fg == neg_inf();
+  const bool reset = forgets(fg);
   const uint64_t resets = __builtin_amdgcn_ballot_w64(reset), mine = resets & ((2ull << lane) - 1);
   const int rid = __builtin_popcountll(mine), all = __builtin_popcountll(resets);
   const double s = wave_sums(reset ? 0.0 : log2_sigmoid(fg));
@@ -1086,7 +1093,7 @@ __global__ __launch_bounds__(256) void mlstm_forget_kernel(MlstmLaunch a) {
   double total = 0.0, resets = 0.0;
   for (int t = t0 + tid; t < end; t += 256) {
     total += step(t);
-    resets += fg(t) == neg_inf();
+    resets += forgets(fg(t));
   }
   total = block_sum(total, sum_sh);
   resets = block_sum(resets, sum_sh);
@@ -1096,7 +1103,7 @@ __global__ __launch_bounds__(256) void mlstm_forget_kernel(MlstmLaunch a) {
     const int t = base + tid;
     const bool in = t < end;
     const float f = in ? fg(t) : 0.f;
-    const bool reset = in && f == neg_inf();
+    const bool reset = in && forgets(f);
     const double mine = step(t);
     // the running sum of steps before t, since the last reset at or before t
     double s = mine;
@@ -1149,7 +1156,7 @@ __global__ __launch_bounds__(kStepThreads) void mlstm_step_kernel(MlstmLaunch a)
   const uint16_t* k = a.k.ptr + b * a.k.sb + h * a.k.sh;
   const uint16_t* v = a.v.ptr + b * a.v.sb + h * a.v.sh;
   const float m = a.m_in[list];
-  const double old = fg == neg_inf() ? -__builtin_inf() : (double)m * kLog2e + log2_sigmoid(fg), put = (double)ig * kLog2e;
+  const double old = forgets(fg) ? -__builtin_inf() : (double)m * kLog2e + log2_sigmoid(fg), put = (double)ig * kLog2e;
   const double now = fmax(old, put);
   const bool masked = ig == neg_inf();
   const float keep = gone(old) ? 0.f : pow2(old - now), in = masked ? 0.f : pow2(put - now);
