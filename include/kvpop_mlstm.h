@@ -61,7 +61,8 @@ typedef struct kvpop_mlstm_state {
  * (normalize = 0); -inf for rows that are not read. kvpop_mlstm_bwd takes it.
  * Products are of bf16 operands with fp32 sums: within a chunk of 64 tokens a weight times its <x, k>, a
  * read state's element and o are each rounded to bf16 once. What is held adds a token's weight times v to
- * 16 bits, in fp32 sums; x . z is not rounded to bf16.
+ * 16 bits, in fp32 sums. lse is of an x . z that is not rounded to bf16; o is divided by the sum of the weights that it is made
+ * with, rounded, unless one of them is negative (features of either sign: x . z may cancel), then by x . z.
  * workspace: kvpop_mlstm_fwd_workspace_size bytes of device memory, 16-byte aligned (may be NULL
  * if that is 0); its contents on entry do not matter. Calls that may run at the same time, and
  * graphs, need workspaces of their own.

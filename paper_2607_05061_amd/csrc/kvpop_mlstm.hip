@@ -787,6 +787,7 @@ __global__ __launch_bounds__(MODE == kDkv ? 512 : 256, 2) void mlstm_kernel(Mlst
 #pragma unroll
       for (int s = 0; s < D / 32; ++s) af[s] = row8(a_sh + j * LS + 32 * s + 8 * g);
       float den = 0.f, rounded = 0.f;
+      uint32_t signs = 0;
       const bool plain = G.resets[slot] == 0;
       // Two tiles of 16 columns at a time: all that the product with C takes, the further ones as zeros.
 #pragma unroll
@@ -821,7 +822,7 @@ __global__ __launch_bounds__(MODE == kDkv ? 512 : 256, 2) void mlstm_kernel(Mlst
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
             p[r] = (__bf16)acc[x][r];
-            if (MODE == kFwd) den += acc[x][r], rounded += (float)p[r];
+            if (MODE == kFwd) den += acc[x][r], rounded += (float)p[r], signs |= __float_as_uint(acc[x][r]);
           }
           *reinterpret_cast<bf16x4*>(sh.p[role] + j * PS + 32 * half + 16 * x + 4 * g) = p;
         }
@@ -833,7 +834,10 @@ __global__ __launch_bounds__(MODE == kDkv ? 512 : 256, 2) void mlstm_kernel(Mlst
         const float held = far == 0.f ? 0.f : far * (qz[0] + qz[1]);
         den = (sum_groups(den) + held) * a.scale;
         // o is divided by the sum of the rounded weights that it is made with: what rounding leaves weighs v - o then, not
-        // v, and is nothing where a query sees one token. do . (v - o) of few tokens needs that.
+        // v, and is nothing where a query sees one token. do . (v - o) of few tokens needs that. Not where a weight or
+        // the held part is negative: such sums cancel, and their roundings are no longer small beside them. (NaN then,
+        // which is not > 0.) 2-norm error of o of signed features, 64 tokens: 2.1e-1 with the rounded sum, 2.5e-3 so.
+        rounded = (int32_t)signs < 0 || held < 0.f ? __builtin_nanf("") : rounded;
         rounded = (sum_groups(rounded) + held) * a.scale;
         const double e = G.b[at + j] - rho;  // that of the row's common factor
         float fac, lse;
