@@ -26,6 +26,7 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
@@ -116,6 +117,17 @@ union Frag {
   bf16x4 h[2];
   u32x2 d[2];
   u32x4 u;
+};
+
+// Whether some bf16 of many is negative (-0 is not): the largest of their bits, two at a time.
+struct Signs {
+  u16x2 most = {0, 0};
+  __device__ __forceinline__ void add(uint32_t w) {
+    union { uint32_t u; u16x2 h; } x;
+    x.u = w;
+    most = __builtin_elementwise_max(most, x.h);
+  }
+  __device__ __forceinline__ bool negative() const { return most.x > 0x8000u || most.y > 0x8000u; }
 };
 
 // 8 elements of a row, 16 bytes.
@@ -230,8 +242,10 @@ struct SegmentScalars {
   double sum;   // log f over the segment, -inf with a reset
   double from;  // the exponent of what it starts from
   double top;   // forwards: what m is after the segment alone
+  int32_t negative;  // forwards: some key has a negative element
+  int32_t pad[3];
 };
-__host__ __device__ constexpr int segment_floats(int D) { return D * D + D + 8; }
+__host__ __device__ constexpr int segment_floats(int D) { return D * D + D + 12; }
 __device__ __forceinline__ SegmentScalars* scalars(float* part, int D) {
   return reinterpret_cast<SegmentScalars*>(part + D * D + D);
 }
@@ -271,6 +285,20 @@ struct Tile {
     }
   }
 };
+
+// The signs of a chunk's rows that have a weight: from the registers, or, where some were cleared, from LDS.
+template <int D, int THREADS>
+__device__ __forceinline__ void add_signs(Signs& signs, const Tile<D, THREADS>& tile, const uint16_t* sh, bool cleared, int tid) {
+  constexpr int kPer = Tile<D, THREADS>::kPer;
+  const uint16_t* at = sh + tid / (D / 8) * Tile<D, THREADS>::kStride + 8 * (tid % (D / 8));
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    u32x4 x = tile.x[i];
+    if (cleared) x = *reinterpret_cast<const u32x4*>(at + i * (THREADS * 8 / D) * Tile<D, THREADS>::kStride);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) signs.add(x[j]);
+  }
+}
 
 // Rows of a chunk that have no weight become zeros, so that nothing in them (NaN) matters.
 template <int D>
@@ -426,6 +454,7 @@ __global__ __launch_bounds__(256, 2) void mlstm_segment_kernel(MlstmLaunch a) {
 #pragma unroll
   for (int j = 0; j < NZ; ++j) z[j] = f32x4{0.f, 0.f, 0.f, 0.f};
   double m = -__builtin_inf(), sum = 0.0, top = -__builtin_inf();
+  Signs signs;
   auto chunk_at = [&](int i) { return rev ? first + count - 1 - i : first + i; };
 
   RawGates<kDkv> raw;
@@ -456,11 +485,13 @@ __global__ __launch_bounds__(256, 2) void mlstm_segment_kernel(MlstmLaunch a) {
     tb.store(b_sh, chunk_at(i) * kChunk, shift, n, tid);
     tc.store(c_sh, chunk_at(i) * kChunk, shift, n, tid);
     __syncthreads();
-    if (rev ? G.odd_q[slot] : G.odd_k[slot]) {
+    const bool odd = rev ? G.odd_q[slot] : G.odd_k[slot];
+    if (odd) {
       clear_rows<D>(b_sh, (rev ? G.r : G.u) + slot * kChunk, tid, 256);
       clear_rows<D>(c_sh, (rev ? G.r : G.u) + slot * kChunk, tid, 256);
       __syncthreads();
     }
+    add_signs(signs, tb, b_sh, odd, tid);
     if (i + 1 < count) {
       tb.load(rb, b, h, chunk_at(i + 1) * kChunk, shift, n, tid);
       tc.load(rc, b, h, chunk_at(i + 1) * kChunk, shift, n, tid);
@@ -514,7 +545,9 @@ __global__ __launch_bounds__(256, 2) void mlstm_segment_kernel(MlstmLaunch a) {
 #pragma unroll
     for (int r = 0; r < 4; ++r)
       if (c == 0) part[D * D + (wave * NZ + j) * 16 + 4 * g + r] = z[j][r];
+  const int negative = __syncthreads_or(signs.negative());
   if (tid == 0) {
+    scalars(part, D)->negative = negative;
     scalars(part, D)->add = m;
     scalars(part, D)->sum = sum;
     scalars(part, D)->top = top;
@@ -623,6 +656,7 @@ struct Shared {
   __align__(16) float far[kRoles][kChunk], far_z[kRoles][kChunk], out[kChunk];
   __align__(16) float z[kRoles][D];
   float dig[4][kChunk];  // backward: the waves' parts of x . dx, of k . dk
+  int negative[4];       // kDq: the waves' keys up to here have negative elements
 };
 
 // One workgroup per segment of a head. 4 waves (for dk and dv 4 each, over the same tiles): wave w takes
@@ -698,6 +732,10 @@ __global__ __launch_bounds__(MODE == kDkv ? 512 : 256, 2) void mlstm_kernel(Mlst
     if (MODE == kFwd) set_zrow(tid, z);
   }
   double defined = m;
+  Signs signs;
+  if (MODE == kDq)
+    for (int i = tid; i < seg; i += THREADS)
+      if (scalars(a.parts + ((int64_t)list * a.segs + i) * segment_floats(D), D)->negative) signs.add(0xFFFFFFFFu);
 
   if (REV) {
     // At the end of the segment: what is held there times its gradient.
@@ -749,7 +787,8 @@ __global__ __launch_bounds__(MODE == kDkv ? 512 : 256, 2) void mlstm_kernel(Mlst
     t2.store(sh.tile[2], chunk * kChunk, late2, n, tid);
     if (REV) t3.store(sh.tile[REV ? 3 : 0], chunk * kChunk, a.delay, n, tid);
     __syncthreads();
-    if (G.odd_k[slot] | (MODE != kFwd ? G.odd_q[slot] : 0)) {
+    const bool odd = G.odd_k[slot] | (MODE != kFwd ? G.odd_q[slot] : 0);
+    if (odd) {
       if (MODE == kFwd) {
         clear_rows<D>(sh.tile[1], G.u + at, tid, THREADS);
         clear_rows<D>(sh.tile[2], G.u + at, tid, THREADS);
@@ -764,6 +803,11 @@ __global__ __launch_bounds__(MODE == kDkv ? 512 : 256, 2) void mlstm_kernel(Mlst
         clear_rows<D>(sh.tile[REV ? 3 : 0], G.r + at, tid, THREADS);
       }
       __syncthreads();
+    }
+    if (MODE == kDq) {
+      add_signs(signs, t2, sh.tile[2], odd, tid);
+      const bool negative = __builtin_amdgcn_ballot_w64(signs.negative()) != 0;
+      if (lane == 0) sh.negative[wave] = negative;
     }
     if (it + 1 < count) load(chunk_at(it + 1));
 
@@ -945,6 +989,16 @@ __global__ __launch_bounds__(MODE == kDkv ? 512 : 256, 2) void mlstm_kernel(Mlst
               if (MODE != kFwd) dot[x] += acc[q][t][r] * (float)ahead[x][t][r];
             }
           }
+          if (MODE == kDq && a.refine) {  // NaN tells of a query with negative elements
+            Signs row;
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+              union { bf16x4 h; u32x2 u; } w;
+              w.h = ahead[x][t];
+              row.add(w.u[0]), row.add(w.u[1]);
+            }
+            if (row.negative()) dot[x] = __builtin_nanf("");
+          }
           if (MODE != kFwd) dot[x] = sum_groups(dot[x]);
         }
         // The values are made before the branch: where the products' results were first read behind one, the
@@ -1009,7 +1063,8 @@ __global__ __launch_bounds__(MODE == kDkv ? 512 : 256, 2) void mlstm_kernel(Mlst
           a.dig[(int64_t)list * a.T + t] = bf16_bits(x);
         } else {
           a.xdx[(int64_t)list * a.T + t] = t >= a.delay ? x : 0.f;
-          if (a.refine && t >= a.delay) a.dots[(int64_t)list * a.T + t - a.delay] += x;
+          const bool positive = !(sh.negative[0] | sh.negative[1] | sh.negative[2] | sh.negative[3]);
+          if (a.refine && t >= a.delay && positive && x == x) a.dots[(int64_t)list * a.T + t - a.delay] += x;
         }
       }
     }
@@ -1256,6 +1311,9 @@ int launch_fwd(const MlstmLaunch& L) {
 // sweep runs once before, for that alone. 2-norm errors of dq at up to 8 tokens 3.7e-3 -> 2.8e-3, at most 6.2e-3 -> 3.8e-3;
 // of dfg at up to 64 tokens 4.9e-3 -> 3.5e-3. A training step takes 53 us with it and 49 without (2 x 8 x 64), 122 and 90 (x 300),
 // 140 and 106 (4 x 8 x 512). Longer sequences are below 3.7e-3 without it.
+// Only where neither the query nor a key up to there has a negative element: else a row's terms can cancel in x . dx, and what
+// their roundings leave there may be far larger than the error of do . o (2-norm error of dq of signed features with it and
+// without: 256 tokens 4.6 and 9.0e-2, 64 1.5e-1 and 2.5e-3; but 4 tokens 2.4e-3 and 2.8e-2).
 constexpr int kRefineChunks = 8;
 
 template <int D>

@@ -5,7 +5,7 @@ import pytest
 
 torch = pytest.importorskip("torch")
 import paper_2607_05061_amd as kv  # noqa: E402
-from mlstm_cases import check_read, inputs, norm_error, on_gpu  # noqa: E402
+from mlstm_cases import check_grads, check_read, inputs, norm_error, on_gpu  # noqa: E402
 from oracle import mlstm as om  # noqa: E402
 
 pytestmark = pytest.mark.gpu
@@ -63,3 +63,37 @@ def test_the_divisor_is_the_sum_and_not_the_sum_of_rounded_weights():
                 bound = 2.0 ** -8 / 3 ** 0.5 * (np.linalg.norm(rss[use]) + np.linalg.norm(ro[use]))
                 got = o[b, h].double().cpu().numpy()[use]
                 assert np.linalg.norm(got - ro[use]) <= bound, (norm_error(got, ro[use]), bound / np.linalg.norm(ro[use]))
+
+
+@pytest.mark.parametrize("T,D,delay", [(3, 64, 0), (64, 64, 0), (64, 128, 1), (300, 64, 3), (300, 128, 0), (512, 64, 0), (700, 64, 20)])
+def test_gradients(T, D, delay):
+    x, ref = on_gpu(inputs(np.random.default_rng(60 + T), 2, 2, T, D, signed=True))
+    a = [x[n] for n in ARGS]
+    o, lse = kv.kvpop_mlstm_fwd(*a, 0.3, delay, True)
+    check_grads(ref, None, 0.3, delay, True, o, lse, kv.kvpop_mlstm_bwd(x["do"], *a, o, lse, 0.3, delay, True))
+
+
+@pytest.mark.parametrize("where", ["first key", "a late key", "a masked key", "a query", "all queries"])
+def test_gradients_of_features_that_are_mostly_positive(where):
+    """Negative elements here and there, large enough that some rows cancel."""
+    rng = np.random.default_rng(63)
+    x = inputs(rng, 2, 2, 400, 64)
+    if where == "all queries":
+        x["q"][..., ::2] *= -0.7
+    elif where == "a query":
+        x["q"][:, :, 200, :40] *= -0.7
+    else:
+        t = {"first key": 0, "a late key": 301, "a masked key": 7}[where]
+        x["k"][:, :, t] *= -6.0
+        if where == "a masked key":
+            x["ig"][:, :, t] = -np.inf
+    g, ref = on_gpu(x)
+    a = [g[n] for n in ARGS]
+    o, lse = kv.kvpop_mlstm_fwd(*a)
+    check_read(ref, None, 1.0, 0, True, o, lse)
+    grads = kv.kvpop_mlstm_bwd(g["do"], *a, o, lse)
+    check_grads(ref, None, 1.0, 0, True, o, lse, grads)
+    if where == "a masked key":  # what it holds does not matter
+        a[1][:, :, 7] = float("nan")
+        for p, r in zip(grads, kv.kvpop_mlstm_bwd(g["do"], *a, o, lse)):
+            assert torch.equal(p, r)
