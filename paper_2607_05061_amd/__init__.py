@@ -1037,7 +1037,8 @@ def _mlstm_function():
             def backward(ctx, do):
                 q, k, v, ig, fg, o, lse, lens = ctx.saved_tensors
                 if do.stride(-1) != 1 or any(s % 8 for s in do.stride()[:-1]) or do.data_ptr() % 16:
-                    do = do.contiguous()
+                    # Not contiguous(), which leaves a contiguous view at an odd offset where it is.
+                    do = do.clone(memory_format=torch.contiguous_format)
                 return (*kvpop_mlstm_bwd(do, q, k, v, ig, fg, o, lse, *ctx.args, lens), None, None, None, None)
 
         _MLSTM_FUNCTION = Mlstm
