@@ -15,6 +15,8 @@
  *
  * What is held keeps a common factor apart, so that no gate overflows it:
  *   m_t = max(m_{t-1} + log f_t, ig_t),  C = C_t e^-m_t,  z = z_t e^-m_t;  empty: C = z = 0, m = -inf.
+ * m is fp32: kvpop_mlstm_fwd rounds it once, at its end (2^-25 |m| at most); kvpop_mlstm_step, which would lose a
+ * slow decay with every token, makes C and z those of the rounded m.
  *
  * Gates: ig = -inf masks a token (its k and v do not matter then, NaN included), fg = -inf forgets
  * everything exactly (where a packed sequence begins), and so does any fg below -2^24, where an fp32 m or lse
@@ -104,7 +106,6 @@ size_t kvpop_mlstm_bwd_workspace_size(const kvpop_mlstm* a);
 /* One token of each sequence: k, v and the gates go into what is held, then q reads it (q is that
  * of the token `delay` before; seq_len is 1, delay 0, and the rows' stride_t means nothing).
  * lens: NULL, or 0 for idle sequences, which keep what they hold and get o = 0.
- * m is rounded to fp32 after every token: decays below half of its last place (2^-25 |m|) are lost.
  * o: bf16 [B, H, D] contiguous. Errors as kvpop_mlstm_fwd, and seq_len != 1 or delay != 0. */
 int kvpop_mlstm_step(const kvpop_mlstm* a, const kvpop_mlstm_state* state, void* o, void* stream);
 

@@ -1216,9 +1216,12 @@ __global__ __launch_bounds__(kStepThreads) void mlstm_step_kernel(MlstmLaunch a)
   const uint16_t* v = a.v.ptr + b * a.v.sb + h * a.v.sh;
   const float m = a.m_in[list];
   const double old = forgets(fg) ? -__builtin_inf() : (double)m * kLog2e + log2_sigmoid(fg), put = (double)ig * kLog2e;
-  const double now = fmax(old, put);
+  // C and z go with m as it is stored, so that what its rounding loses (up to 2^-25 |m| a token, all of a slow decay beside a
+  // large m) is theirs. Below fp32's range nothing is held.
+  const float m_out = (float)(fmax(old, put) * kLog2eInv);
+  const double now = (double)m_out * kLog2e;
   const bool masked = ig == neg_inf();
-  const float keep = gone(old) ? 0.f : pow2(old - now), in = masked ? 0.f : pow2(put - now);
+  const float keep = gone(old) || gone(now) ? 0.f : pow2(old - now), in = masked || gone(now) ? 0.f : pow2(put - now);
   float vi[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j) vi[j] = masked ? 0.f : in * bf16_value(v[col + j]);
@@ -1250,7 +1253,7 @@ __global__ __launch_bounds__(kStepThreads) void mlstm_step_kernel(MlstmLaunch a)
   if ((tid & 63) < COLS) *reinterpret_cast<f32x4*>(&num_sh[wave][col]) = num;
   if ((tid & 63) == 0) den_sh[wave] = den;
   __syncthreads();
-  if (tid == 0) a.m[list] = (float)(now * kLog2eInv);
+  if (tid == 0) a.m[list] = m_out;
   if (tid >= D) return;
   float y = 0.f;
 #pragma unroll
