@@ -86,9 +86,9 @@ size_t kvpop_mlstm_fwd_workspace_size(const kvpop_mlstm* a);
  * Rows with lse = -inf give nothing. All are bf16 and contiguous: dq (scale dx), dk, dv [B, H, T, D];
  * dig, dfg [B, H, T]; 0 for tokens and queries that take no part. do_: bf16 [B, H, T, D] (strided),
  * o: bf16 [B, H, T, D] contiguous, lse: fp32 [B, H, T].
- * Roundings are those of kvpop_mlstm_fwd; for dq the read state's elements keep 16 bits. Up to 512 tokens with
- * normalize = 1, the rounding of o is taken out of d_u (x . dx = 0 tells it) where neither q nor a key of
- * the sequence up to there has a negative element. dfg is a running
+ * Roundings are those of kvpop_mlstm_fwd; for dq the read state's elements keep 16 bits. With normalize = 1, the
+ * rounding of o is taken out of d_u (x . dx = 0 tells it) where neither q nor a key of the sequence up to there
+ * has a negative element. dfg is a running
  * sum of differences: its error is relative to the largest of a sequence's partial sums, not to each element.
  * Nothing depends on the order of workgroups. workspace as above (kvpop_mlstm_bwd_workspace_size).
  * Errors as kvpop_mlstm_fwd. */

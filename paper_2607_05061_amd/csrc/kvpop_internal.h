@@ -160,7 +160,7 @@ struct MlstmLaunch {
   int32_t segs, seg_chunks; // segments of each head and their chunks of 64 tokens
   float* parts;             // [directions, B, H, segs] parts
   float *dots, *dig32;      // backward: [B, H, T]: do . o and k . dk
-  int refine;               // dq's sweep adds x . dx to dots
+  int direction;            // the first of a launch over segments: 0 forwards, 1 backwards
   float* xdx;               // backward: [B, H, T], by time: x . dx
   double* edges;            // backward: [B, H, segs]
 };

@@ -425,8 +425,8 @@ __device__ __forceinline__ f32x4 scaled(f32x4 x, float keep) {
 // First sweep: what each segment adds to what is held
 // ---------------------------------------------------------------------------
 
-// One workgroup per segment of a head and direction (blockIdx.y: 0 forwards, k and v; 1 backwards, q
-// and do). Wave w holds columns [w D / 4, (w + 1) D / 4) of the matrix. Each row is read once and HBM bounds it:
+// One workgroup per segment of a head and direction (blockIdx.y, from a.direction on: 0 forwards, k and v; 1
+// backwards, q and do). Wave w holds columns [w D / 4, (w + 1) D / 4) of the matrix. Each row is read once and HBM bounds it:
 // k and v of 4 x 8 x 32768 tokens of 128 (537 MB) 125 us, 4.3 TB/s. 256 threads, so that two workgroups a CU
 // fill each other's waits.
 template <int D>
@@ -439,7 +439,7 @@ __global__ __launch_bounds__(256, 2) void mlstm_segment_kernel(MlstmLaunch a) {
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, c = lane & 15;
   const int seg = blockIdx.x % a.segs, list = blockIdx.x / a.segs, b = list / a.H, h = list % a.H;
   const int n = a.lens ? clampi(a.lens[b], 0, a.T) : a.T, chunks = (n + kChunk - 1) / kChunk;
-  const bool rev = blockIdx.y != 0;
+  const bool rev = a.direction + blockIdx.y != 0;
   const int first = min(seg * a.seg_chunks, chunks), count = min((seg + 1) * a.seg_chunks, chunks) - first;
   const Rows& rb = rev ? a.q : a.k;
   const Rows& rc = rev ? a.go : a.v;
@@ -533,7 +533,7 @@ __global__ __launch_bounds__(256, 2) void mlstm_segment_kernel(MlstmLaunch a) {
     __syncthreads();
   }
 
-  float* part = a.parts + ((int64_t)blockIdx.y * a.B * a.H * a.segs + blockIdx.x) * segment_floats(D);
+  float* part = a.parts + ((int64_t)(rev ? 1 : 0) * a.B * a.H * a.segs + blockIdx.x) * segment_floats(D);
 #pragma unroll
   for (int i = 0; i < D / 16; ++i)
 #pragma unroll
@@ -570,8 +570,8 @@ __global__ __launch_bounds__(256) void mlstm_scan_kernel(MlstmLaunch a, int bloc
   __shared__ float keep_sh[kScanSegments], put_sh[kScanSegments];
   __shared__ double last_sh[2];
   const int list = blockIdx.x / blocks, e = ((blockIdx.x % blocks) * 256 + threadIdx.x) * 4, tid = threadIdx.x;
-  const bool rev = blockIdx.y != 0, mine = e < D * D + D;
-  float* parts = a.parts + ((int64_t)blockIdx.y * a.B * a.H + list) * a.segs * segment_floats(D);
+  const bool rev = a.direction + blockIdx.y != 0, mine = e < D * D + D;
+  float* parts = a.parts + ((int64_t)(rev ? 1 : 0) * a.B * a.H + list) * a.segs * segment_floats(D);
   auto part = [&](int i) { return parts + (int64_t)(rev ? a.segs - 1 - i : i) * segment_floats(D); };
   float* held = nullptr;
   f32x4 x = {0.f, 0.f, 0.f, 0.f};
@@ -668,7 +668,7 @@ struct Shared {
 // Chunks follow each other, and the phases of one wait for each other: two waves a SIMD (256 registers a lane; two
 // workgroups a CU, of dk and dv one) fill part of the waits, and neither the products nor HBM are busy
 // all the time. D = 128: read-outs of 4 x 8 x 32768 tokens 266 us (1.07 GB: 4.0 TB/s), of 2 x 8 x 16384 76 us; dq there
-// 108 us, dk and dv 161 us. Twice the waves with 16 columns each needed more registers than they have: read-outs
+// 120 us, dk and dv 161 us. Twice the waves with 16 columns each needed more registers than they have: read-outs
 // 493 us where 4 waves took 277.
 template <int D, int MODE>
 __global__ __launch_bounds__(MODE == kDkv ? 512 : 256, 2) void mlstm_kernel(MlstmLaunch a) {
@@ -762,11 +762,8 @@ __global__ __launch_bounds__(MODE == kDkv ? 512 : 256, 2) void mlstm_kernel(Mlst
     }
     __syncthreads();
   }
-  // Where this lane's outputs go, from time 0 on.
-  uint16_t* out_at = out + ((int64_t)list * a.T + c - (REV ? 0 : a.delay)) * D + wave * NT * 16 + 4 * g;
-
   Tile<D, THREADS> t0, t1, t2, t3;
-  auto load = [&](int chunk) __attribute__((always_inline)) {
+  auto load = [&](int chunk, int tid) __attribute__((always_inline)) {
     t0.load(r0, b, h, chunk * kChunk, late0, n, tid);
     t1.load(r1, b, h, chunk * kChunk, 0, n, tid);
     t2.load(r2, b, h, chunk * kChunk, late2, n, tid);
@@ -774,9 +771,15 @@ __global__ __launch_bounds__(MODE == kDkv ? 512 : 256, 2) void mlstm_kernel(Mlst
   };
   RawGates<MODE> raw;
   if (role == 0 && wave < count) raw.load(a, b, h, n, chunk_at(wave), lane);
-  if (count > 0) load(chunk_at(0));
+  if (count > 0) load(chunk_at(0), tid);
 
   for (int it = 0; it < count; ++it) {
+    // Addresses are made anew in every chunk (kDq, and D = 64): held over them all, they took so many registers that
+    // others went to memory, whose waits are those of the tiles on their way (dq of 2 x 8 x 16384 of 128 187 us, 120 so; a training
+    // step of 4 x 8 x 4096 of 64 170 us, 159 so).
+    int tid_now = tid;
+    if (MODE == kDq || D == 64) asm volatile("" : "+v"(tid_now));
+    const int tid = tid_now, lane = tid & 63, g = lane >> 4, c = lane & 15;
     const int chunk = chunk_at(it), slot = it % kBlock, at = slot * kChunk;
     if (slot == 0 && role == 0) {
       if (it + wave < count) chunk_gates<MODE>(a, G, raw, n, chunk_at(it + wave), wave, lane);
@@ -809,8 +812,10 @@ __global__ __launch_bounds__(MODE == kDkv ? 512 : 256, 2) void mlstm_kernel(Mlst
       const bool negative = __builtin_amdgcn_ballot_w64(signs.negative()) != 0;
       if (lane == 0) sh.negative[wave] = negative;
     }
-    if (it + 1 < count) load(chunk_at(it + 1));
+    if (it + 1 < count) load(chunk_at(it + 1), tid);
 
+    f32x4 weighted[4];  // kDq: the masked product in 32 bits, and its weights
+    bf16x4 weight[4];
     {  // The masked product, transposed: this lane has row j and columns 4 g + r of each 16.
       const int j = 16 * wave + c, rid = G.rid[at + j];
       double rho;   // the row's exponent within the chunk
@@ -831,13 +836,13 @@ __global__ __launch_bounds__(MODE == kDkv ? 512 : 256, 2) void mlstm_kernel(Mlst
 #pragma unroll
       for (int s = 0; s < D / 32; ++s) af[s] = row8(a_sh + j * LS + 32 * s + 8 * g);
       float den = 0.f, rounded = 0.f;
-      uint32_t signs = 0;
+      uint32_t bits = 0;
       const bool plain = G.resets[slot] == 0;
       // Two tiles of 16 columns at a time: all that the product with C takes, the further ones as zeros.
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
         if (REV ? half < wave / 2 : half > wave / 2) continue;
-        f32x4 acc[2];
+        f32x4 acc[2], w[2];
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
           const int kt = 2 * half + x, key = 16 * kt + 4 * g;
@@ -846,19 +851,26 @@ __global__ __launch_bounds__(MODE == kDkv ? 512 : 256, 2) void mlstm_kernel(Mlst
           acc[x] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int s = 0; s < D / 32; ++s) acc[x] = mfma(row8(b_sh + (16 * kt + c) * LS + 32 * s + 8 * g), af[s], acc[x]);
-          const f32x4 w = {pow2(e0.x + rho), pow2(e0.y + rho), pow2(e1.x + rho), pow2(e1.y + rho)};
+          w[x] = f32x4{pow2(e0.x + rho), pow2(e0.y + rho), pow2(e1.x + rho), pow2(e1.y + rho)};
           if (MODE == kDq) acc[x] += alpha;
           if (REV && role) acc[x] += *reinterpret_cast<const f32x4*>(G.d + at + key);
-          acc[x] *= w;
+          acc[x] *= w[x];
 #pragma unroll
-          for (int r = 0; r < 4; ++r) acc[x][r] = (REV ? key + r >= j : key + r <= j) ? acc[x][r] : 0.f;
+          for (int r = 0; r < 4; ++r) {
+            const bool in = REV ? key + r >= j : key + r <= j;
+            acc[x][r] = in ? acc[x][r] : 0.f;
+            if (MODE == kDq) w[x][r] = in ? w[x][r] : 0.f;
+          }
         }
         if (!plain)
 #pragma unroll
           for (int x = 0; x < 2; ++x) {
             const i32x4 other = *reinterpret_cast<const i32x4*>(G.rid + at + 32 * half + 16 * x + 4 * g);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) acc[x][r] = other[r] == rid ? acc[x][r] : 0.f;
+            for (int r = 0; r < 4; ++r) {
+              acc[x][r] = other[r] == rid ? acc[x][r] : 0.f;
+              if (MODE == kDq) w[x][r] = other[r] == rid ? w[x][r] : 0.f;
+            }
           }
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
@@ -866,9 +878,14 @@ __global__ __launch_bounds__(MODE == kDkv ? 512 : 256, 2) void mlstm_kernel(Mlst
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
             p[r] = (__bf16)acc[x][r];
-            if (MODE == kFwd) den += acc[x][r], rounded += (float)p[r], signs |= __float_as_uint(acc[x][r]);
+            if (MODE == kFwd) den += acc[x][r], rounded += (float)p[r], bits |= __float_as_uint(acc[x][r]);
           }
           *reinterpret_cast<bf16x4*>(sh.p[role] + j * PS + 32 * half + 16 * x + 4 * g) = p;
+          if (MODE == kDq) {
+            weighted[2 * half + x] = acc[x];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) weight[2 * half + x][r] = (__bf16)w[x][r];
+          }
         }
       }
       if (MODE == kFwd) {
@@ -881,7 +898,7 @@ __global__ __launch_bounds__(MODE == kDkv ? 512 : 256, 2) void mlstm_kernel(Mlst
         // v, and is nothing where a query sees one token. do . (v - o) of few tokens needs that. Not where a weight or
         // the held part is negative: such sums cancel, and their roundings are no longer small beside them. (NaN then,
         // which is not > 0.) 2-norm error of o of signed features, 64 tokens: 2.1e-1 with the rounded sum, 2.5e-3 so.
-        rounded = (int32_t)signs < 0 || held < 0.f ? __builtin_nanf("") : rounded;
+        rounded = (int32_t)bits < 0 || held < 0.f ? __builtin_nanf("") : rounded;
         rounded = (sum_groups(rounded) + held) * a.scale;
         const double e = G.b[at + j] - rho;  // that of the row's common factor
         float fac, lse;
@@ -915,11 +932,17 @@ __global__ __launch_bounds__(MODE == kDkv ? 512 : 256, 2) void mlstm_kernel(Mlst
     const Update<REV> up(G, slot, m);
     const double added = up.added(G, slot), gates_sum = G.resets[slot] ? -__builtin_inf() : G.sum[slot];
 
-    bf16x8 cf[2][NT];
+    const int t_0 = chunk * kChunk;
+    bf16x4 rows_q[MODE == kDq ? 4 : 1][NT];  // dq's rows of q (dk's rows of k are in LDS), on their way
+    if (MODE == kDq) {
+      const uint16_t* from = a.q.ptr + b * a.q.sb + h * a.q.sh + wave * NT * 16 + 4 * g;
 #pragma unroll
-    for (int s = 0; s < 2; ++s)
+      for (int q = 0; q < 4; ++q) {
+        const uint16_t* p = from + min(max(t_0 + 16 * q + c - a.delay, 0), n - 1) * a.q.st;
 #pragma unroll
-      for (int t = 0; t < NT; ++t) cf[s][t] = column8(c_sh + 32 * s * LS + (wave * NT + t) * 16, LS, g, c);
+        for (int t = 0; t < NT; ++t) rows_q[MODE == kDq ? q : 0][t] = *reinterpret_cast<const bf16x4*>(p + 16 * t);
+      }
+    }
     f32x4 acc[4][NT];
 #pragma unroll
     for (int q = 0; q < 4; ++q)
@@ -948,23 +971,75 @@ __global__ __launch_bounds__(MODE == kDkv ? 512 : 256, 2) void mlstm_kernel(Mlst
         }
       }
     }
-    {
-      const int late = REV ? 0 : a.delay, t0 = chunk * kChunk;
-      uint16_t* to = out_at + (int64_t)t0 * D;
-      // dq's rows of q (dk's rows of k are in LDS), two blocks of rows at a time.
-      const uint16_t* from = a.q.ptr + b * a.q.sb + h * a.q.sh + wave * NT * 16 + 4 * g;
-      bf16x4 ahead[2][NT];
-      auto fetch = [&](int q0) __attribute__((always_inline)) {
+    bf16x8 cf[2][NT];
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          const uint16_t* p = from + min(max(t0 + 16 * (q0 + x) + c - a.delay, 0), n - 1) * a.q.st;
+    for (int s = 0; s < 2; ++s)
 #pragma unroll
-          for (int t = 0; t < NT; ++t) ahead[x][t] = *reinterpret_cast<const bf16x4*>(p + 16 * t);
-        }
-      };
+      for (int t = 0; t < NT; ++t) cf[s][t] = column8(c_sh + 32 * s * LS + (wave * NT + t) * 16, LS, g, c);
+    // Columns 16 t + 4 g + 0 .. 3 of the wave's of row 16 q + c.
+    auto result = [&](int q, int t, float far, float far_z, float fac) __attribute__((always_inline)) {
+      f32x4 y = scaled(acc[q][t], far);
+      if (MODE != kFwd && with_z) y += scaled(*reinterpret_cast<const f32x4*>(sh.z[role] + (wave * NT + t) * 16 + 4 * g), far_z);
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+        if (REV ? 32 * s + 31 >= 16 * q : 32 * s <= 16 * q)
+          y = mfma(cf[s][t], row8(sh.p[role] + (16 * q + c) * PS + 32 * s + 8 * g), y);
+      return y * fac;
+    };
+    // A normalised read-out does not change with the size of x, so x . dx = 0, and what comes out for it is the error of
+    // do . o: of the rounding of o, which is not small beside do . (v - o) where a query sees few tokens, by whatever gates and
+    // features. So the rows' x . dx is taken first, and the masked product's do . v - do . o corrected with it. Not where
+    // q (NaN tells) or a key up to here has a negative element: then a row's terms can cancel in x . dx, and what their
+    // roundings leave may be far larger than the error of do . o.
+    if (MODE == kDq && a.normalize && !(sh.negative[0] | sh.negative[1] | sh.negative[2] | sh.negative[3])) {
 #pragma unroll
       for (int q0 = 0; q0 < 4; q0 += 2) {
-        if (MODE == kDq) fetch(q0);
+        float dot[2] = {0.f, 0.f};
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const int q = q0 + x, j = 16 * q + c;
+          const float far = sh.far[role][j], far_z = sh.far_z[role][j];
+          Signs row;
+#pragma unroll
+          for (int t = 0; t < NT; ++t) {
+            const f32x4 y = result(q, t, far, far_z, a.scale);
+            union { bf16x4 h; u32x2 u; } w;
+            w.h = rows_q[MODE == kDq ? q : 0][t];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) dot[x] += y[r] * (float)w.h[r];
+            row.add(w.u[0]), row.add(w.u[1]);
+          }
+          dot[x] = sum_groups(row.negative() ? __builtin_nanf("") : dot[x]);
+          asm volatile("" : "+v"(dot[x]));
+        }
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+          if (g == 0) sh.dig[wave][16 * (q0 + x) + c] = dot[x];
+      }
+      __syncthreads();
+      const int j = 16 * wave + c, t = t_0 + j;
+      float x = sh.dig[0][j] + sh.dig[1][j] + sh.dig[2][j] + sh.dig[3][j];
+      if (x != x || gone(G.r[at + j])) x = 0.f;
+#pragma unroll
+      for (int kt = 0; kt < 4; ++kt) {
+        if (kt / 2 > wave / 2) continue;
+        bf16x4 p;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) p[r] = (__bf16)(weighted[kt][r] - x * (float)weight[kt][r]);
+        *reinterpret_cast<bf16x4*>(sh.p[role] + j * PS + 16 * kt + 4 * g) = p;
+      }
+      if (g == 0) {
+        const float d = G.d[at + j] - x;
+        sh.far_z[role][j] = sh.far[role][j] * d;
+        if (t >= a.delay && t < n) a.dots[(int64_t)list * a.T + t - a.delay] = -d;
+      }
+      __syncthreads();
+    }
+    {
+      const int late = REV ? 0 : a.delay;
+      uint16_t* to = out + ((int64_t)list * a.T + c - late + t_0) * D + wave * NT * 16 + 4 * g;
+#pragma unroll
+      for (int q0 = 0; q0 < 4; q0 += 2) {
         bf16x4 y[2][NT];
         float dot[2] = {0.f, 0.f};
 #pragma unroll
@@ -974,30 +1049,15 @@ __global__ __launch_bounds__(MODE == kDkv ? 512 : 256, 2) void mlstm_kernel(Mlst
           const float far_z = MODE != kFwd && with_z ? sh.far_z[role][j] : 0.f;
 #pragma unroll
           for (int t = 0; t < NT; ++t) {
-            const int col = (wave * NT + t) * 16 + 4 * g;
-            acc[q][t] = scaled(acc[q][t], far);
-            if (MODE != kFwd && with_z) acc[q][t] += scaled(*reinterpret_cast<const f32x4*>(sh.z[role] + col), far_z);
-#pragma unroll
-            for (int s = 0; s < 2; ++s)
-              if (REV ? 32 * s + 31 >= 16 * q : 32 * s <= 16 * q)
-                acc[q][t] = mfma(cf[s][t], row8(sh.p[role] + j * PS + 32 * s + 8 * g), acc[q][t]);
-            acc[q][t] *= fac;
-            if (REV) ahead[x][t] = *reinterpret_cast<const bf16x4*>(sh.tile[0] + j * LS + col);
+            acc[q][t] = result(q, t, far, far_z, fac);
+            bf16x4 with;
+            if (MODE == kDq) with = rows_q[MODE == kDq ? q : 0][t];
+            if (REV) with = *reinterpret_cast<const bf16x4*>(sh.tile[0] + j * LS + (wave * NT + t) * 16 + 4 * g);
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
               y[x][t][r] = (__bf16)acc[q][t][r];
-              if (MODE != kFwd) dot[x] += acc[q][t][r] * (float)ahead[x][t][r];
+              if (MODE != kFwd) dot[x] += acc[q][t][r] * (float)with[r];
             }
-          }
-          if (MODE == kDq && a.refine) {  // NaN tells of a query with negative elements
-            Signs row;
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
-              union { bf16x4 h; u32x2 u; } w;
-              w.h = ahead[x][t];
-              row.add(w.u[0]), row.add(w.u[1]);
-            }
-            if (row.negative()) dot[x] = __builtin_nanf("");
           }
           if (MODE != kFwd) dot[x] = sum_groups(dot[x]);
         }
@@ -1010,7 +1070,7 @@ __global__ __launch_bounds__(MODE == kDkv ? 512 : 256, 2) void mlstm_kernel(Mlst
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
           const int j = 16 * (q0 + x) + c;
-          if (t0 + j >= late && t0 + j < n)
+          if (t_0 + j >= late && t_0 + j < n)
 #pragma unroll
             for (int t = 0; t < NT; ++t) *reinterpret_cast<bf16x4*>(to + 16 * (q0 + x) * D + 16 * t) = y[x][t];
           if (MODE != kFwd && g == 0 && (MODE == kDq || role)) sh.dig[wave][j] = dot[x];
@@ -1063,8 +1123,6 @@ __global__ __launch_bounds__(MODE == kDkv ? 512 : 256, 2) void mlstm_kernel(Mlst
           a.dig[(int64_t)list * a.T + t] = bf16_bits(x);
         } else {
           a.xdx[(int64_t)list * a.T + t] = t >= a.delay ? x : 0.f;
-          const bool positive = !(sh.negative[0] | sh.negative[1] | sh.negative[2] | sh.negative[3]);
-          if (a.refine && t >= a.delay && positive && x == x) a.dots[(int64_t)list * a.T + t - a.delay] += x;
         }
       }
     }
@@ -1288,7 +1346,8 @@ void plan(MlstmLaunch& L) {
 }
 
 template <int D>
-int launch_states(const MlstmLaunch& L, int directions) {
+int launch_states(MlstmLaunch L, int first, int directions) {
+  L.direction = first;
   const hipStream_t st = (hipStream_t)L.stream;
   const unsigned lists = (unsigned)L.B * L.H;
   hipLaunchKernelGGL((mlstm_segment_kernel<D>), dim3(lists * L.segs, directions), dim3(256), 0, st, L);
@@ -1302,22 +1361,12 @@ int launch_states(const MlstmLaunch& L, int directions) {
 template <int D>
 int launch_fwd(const MlstmLaunch& L) {
   if (L.segs > 1) {
-    const int e = launch_states<D>(L, 1);
+    const int e = launch_states<D>(L, 0, 1);
     if (e != 0) return e;
   }
   hipLaunchKernelGGL((mlstm_kernel<D, kFwd>), dim3((unsigned)(L.B * L.H * L.segs)), dim3(256), 0, (hipStream_t)L.stream, L);
   return (int)hipGetLastError();
 }
-
-// Where queries see few tokens, the rounding of o in do . o is not small beside do . (v - o). A normalised read-out does not
-// change with the size of x, so x . dx = 0, and what dq's sweep has for it is the error of do . o: on short sequences the
-// sweep runs once before, for that alone. 2-norm errors of dq at up to 8 tokens 3.7e-3 -> 2.8e-3, at most 6.2e-3 -> 3.8e-3;
-// of dfg at up to 64 tokens 4.9e-3 -> 3.5e-3. A training step takes 53 us with it and 49 without (2 x 8 x 64), 122 and 90 (x 300),
-// 140 and 106 (4 x 8 x 512). Longer sequences are below 3.7e-3 without it.
-// Only where neither the query nor a key up to there has a negative element: else a row's terms can cancel in x . dx, and what
-// their roundings leave there may be far larger than the error of do . o (2-norm error of dq of signed features with it and
-// without: 256 tokens 4.6 and 9.0e-2, 64 1.5e-1 and 2.5e-3; but 4 tokens 2.4e-3 and 2.8e-2).
-constexpr int kRefineChunks = 8;
 
 template <int D>
 int launch_bwd(const MlstmLaunch& L) {
@@ -1327,16 +1376,11 @@ int launch_bwd(const MlstmLaunch& L) {
   int e;
   hipLaunchKernelGGL((mlstm_dots_kernel<D>), dim3((unsigned)((rows + per - 1) / per)), dim3(256), 0, st, L, rows);
   if ((e = (int)hipGetLastError()) != 0) return e;
-  if (L.normalize && chunk_count(L) <= kRefineChunks) {
-    MlstmLaunch R = L;
-    R.refine = 1;
-    if (L.segs > 1 && (e = launch_states<D>(L, 1)) != 0) return e;
-    hipLaunchKernelGGL((mlstm_kernel<D, kDq>), dim3(groups), dim3(256), 0, st, R);
-    if ((e = (int)hipGetLastError()) != 0) return e;
-  }
-  if (L.segs > 1 && (e = launch_states<D>(L, 2)) != 0) return e;
+  // The backward direction sums do . o, which dq's sweep corrects where it is normalised.
+  if (L.segs > 1 && (e = launch_states<D>(L, 0, L.normalize ? 1 : 2)) != 0) return e;
   hipLaunchKernelGGL((mlstm_kernel<D, kDq>), dim3(groups), dim3(256), 0, st, L);
   if ((e = (int)hipGetLastError()) != 0) return e;
+  if (L.segs > 1 && L.normalize && (e = launch_states<D>(L, 1, 1)) != 0) return e;
   hipLaunchKernelGGL((mlstm_kernel<D, kDkv>), dim3(groups), dim3(512), 0, st, L);
   if ((e = (int)hipGetLastError()) != 0) return e;
   hipLaunchKernelGGL(mlstm_forget_kernel, dim3(groups), dim3(256), 0, st, L);

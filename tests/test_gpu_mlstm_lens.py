@@ -1,0 +1,97 @@
+"""What a sequence's gradients are does not depend on what else is in the call: not on the length that others are padded
+to, nor on sequences packed before it. Queries that see few tokens are the ones that show it."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+import paper_2607_05061_amd as kv  # noqa: E402
+from cache_cases import i32  # noqa: E402
+from mlstm_cases import inputs, on_gpu  # noqa: E402
+from oracle import mlstm as om  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+ARGS = ("q", "k", "v", "ig", "fg")
+FEW = 3 * 2.0 ** -8 / 3 ** 0.5
+
+
+def both(a, do, **kw):
+    o, lse = kv.kvpop_mlstm_fwd(*a, **kw)
+    return (o, lse) + kv.kvpop_mlstm_bwd(do, *a, o, lse, **kw)
+
+
+def exact(ref, b, h, i, j, delay):
+    """dq, dk of tokens [i, j) as a sequence of their own."""
+    y = [ref[n][b, h, i:j] for n in ARGS]
+    o, lse, *_ = om.read(*y, 1.0, delay, True)
+    return om.grads(ref["do"][b, h, i:j], *y, o, lse, 1.0, delay, True)[0][:2]
+
+
+@pytest.mark.parametrize("n", [1, 2, 5, 17, 64, 130])
+def test_padding_does_not_matter(n):
+    """512 heads are one segment each, whatever T: bit for bit the same."""
+    B, H, D = 4, 128, 64
+    x, _ = on_gpu(inputs(np.random.default_rng(80 + n), B, H, n, D))
+    want = both([x[y] for y in ARGS], x["do"], delay=min(1, n - 1))
+    for T in (n + 30, 513, 700):
+        pad = {y: torch.full((B, H, T, *t.shape[3:]), float("nan"), dtype=t.dtype, device="cuda") for y, t in x.items()}
+        for y, t in x.items():
+            pad[y][:, :, :n] = t
+        got = both([pad[y] for y in ARGS], pad["do"], delay=min(1, n - 1), lens=i32([n] * B))
+        for g, w in zip(got, want):
+            assert torch.equal(g[:, :, :n], w), T
+
+
+@pytest.mark.parametrize("n", [1, 2, 5, 17, 64])
+def test_what_is_packed_before_does_not_matter(n):
+    """The same tokens at the start of a call and behind fg = -inf at a chunk's start, one segment a head."""
+    B, H, D, at = 4, 128, 64, 576
+    x, _ = on_gpu(inputs(np.random.default_rng(90 + n), B, H, n, D))
+    x["fg"][:, :, 0] = float("-inf")
+    y, _ = on_gpu(inputs(np.random.default_rng(91), B, H, at, D))
+    want = both([x[t] for t in ARGS], x["do"])
+    whole = {t: torch.cat([y[t], x[t]], 2) for t in x}
+    got = both([whole[t] for t in ARGS], whole["do"])
+    for g, w in zip(got[:-1], want[:-1]):  # dfg is a running sum over both
+        assert torch.equal(g[:, :, at:], w)
+
+
+@pytest.mark.parametrize("T", [64, 513, 700, 2000])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n", [2, 4, 8, 40])
+def test_short_sequences_in_a_long_call(T, D, n):
+    """Sequences of n tokens, by lens or packed: the 2-norm error of dq and dk over a call's is that of independent
+    roundings of their own terms, as where they are alone: o rounded (its part in do . o taken out by x . dx = 0, to a
+    rounding of each term), the weights of a row, the result: 3 of at most 2^-8 / sqrt(3)."""
+    rng = np.random.default_rng(T + D + n)
+    B, H = 8, 8
+    x = inputs(rng, B, H, T, D)
+    x["fg"][:, :, ::n] = -np.inf
+    g, ref = on_gpu(x)
+    a = [g[y] for y in ARGS]
+    count = min(T // n, 10)
+    for lens in (i32([n] * B), None):
+        grads = both(a, g["do"], lens=lens)[2:4]
+        err, size = np.zeros(2), np.zeros(2)
+        for b in range(B):
+            for h in range(H):
+                for s in range(count if lens is None else 1):
+                    s = (T // n - 1) * s // max(1, count - 1) * n  # spread over the call
+                    for i, w in enumerate(exact(ref, b, h, s, s + n, 0)):
+                        err[i] += ((grads[i][b, h, s:s + n].double().cpu().numpy() - w) ** 2).sum()
+                        size[i] += (w ** 2).sum()
+        assert (np.sqrt(err) <= FEW * np.sqrt(size)).all(), (lens is None, np.sqrt(err / size))
+
+
+@pytest.mark.parametrize("T", [300, 513, 1500])
+def test_gates_that_forget_at_once(T):
+    """f about 1/20: every query sees a token or two, anywhere in the sequence."""
+    rng = np.random.default_rng(T)
+    B, H, D = 1, 4, 64
+    g, ref = on_gpu(inputs(rng, B, H, T, D, fg=(-3.0, 0.5)))
+    grads = both([g[y] for y in ARGS], g["do"])[2:4]
+    want = [exact(ref, 0, h, 0, T, 0) for h in range(H)]
+    for i, got in enumerate(grads):
+        w = np.stack([y[i] for y in want])
+        err = np.linalg.norm(got[0].double().cpu().numpy() - w) / np.linalg.norm(w)
+        assert err <= FEW, (i, err)
