@@ -1073,7 +1073,8 @@ __global__ __launch_bounds__(MODE == kDkv ? 512 : 256, 2) void mlstm_kernel(Mlst
           if (t_0 + j >= late && t_0 + j < n)
 #pragma unroll
             for (int t = 0; t < NT; ++t) *reinterpret_cast<bf16x4*>(to + 16 * (q0 + x) * D + 16 * t) = y[x][t];
-          if (MODE != kFwd && g == 0 && (MODE == kDq || role)) sh.dig[wave][j] = dot[x];
+          // A row that is not read has dx = 0, whatever q holds.
+          if (MODE != kFwd && g == 0 && (MODE == kDq || role)) sh.dig[wave][j] = MODE == kDq && gone(G.r[at + j]) ? 0.f : dot[x];
         }
       }
     }

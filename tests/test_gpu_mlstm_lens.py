@@ -6,7 +6,7 @@ import pytest
 torch = pytest.importorskip("torch")
 import paper_2607_05061_amd as kv  # noqa: E402
 from cache_cases import i32  # noqa: E402
-from mlstm_cases import inputs, on_gpu  # noqa: E402
+from mlstm_cases import check_grads, inputs, on_gpu  # noqa: E402
 from oracle import mlstm as om  # noqa: E402
 
 pytestmark = pytest.mark.gpu
@@ -95,3 +95,23 @@ def test_gates_that_forget_at_once(T):
         w = np.stack([y[i] for y in want])
         err = np.linalg.norm(got[0].double().cpu().numpy() - w) / np.linalg.norm(w)
         assert err <= FEW, (i, err)
+
+
+@pytest.mark.parametrize("T,D,delay", [(5, 64, 0), (200, 64, 3), (700, 128, 0)])
+@pytest.mark.parametrize("normalize", [True, False])
+def test_rows_that_the_caller_takes_out_give_nothing(T, D, delay, normalize):
+    """lse = -inf, whatever q, do and o hold there."""
+    rng = np.random.default_rng(T + D)
+    g, ref = on_gpu(inputs(rng, 2, 2, T, D))
+    a = [g[y] for y in ARGS]
+    o, lse = kv.kvpop_mlstm_fwd(*a, 0.3, delay, normalize)
+    off = torch.from_numpy(rng.random((2, 2, T)) < 0.3).cuda()
+    off[0, 0, 0] = True
+    lse[off] = float("-inf")
+    for x in (a[0], g["do"], o):
+        x[off] = float("nan")
+    grads = kv.kvpop_mlstm_bwd(g["do"], *a, o, lse, 0.3, delay, normalize)
+    for n in ("q", "do"):
+        ref[n][off.cpu().numpy()] = np.nan
+    check_grads(ref, None, 0.3, delay, normalize, o, lse, grads)
+    assert all(x.isfinite().all() for x in grads)
