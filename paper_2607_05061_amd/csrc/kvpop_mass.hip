@@ -446,6 +446,7 @@ __global__ __launch_bounds__(kStepThreads) void mass_step_kernel(RetainLaunch a)
     if (tid == 0) a.slot[list] = -1;
     return;
   }
+  __syncthreads();  // all have read held before one writes it
   int32_t* pos = a.pos + (int64_t)list * a.S;
   float* mass = a.prio + (int64_t)list * a.S;
   if (held < a.sinks + a.window + a.topk) {
