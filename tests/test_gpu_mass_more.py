@@ -28,3 +28,59 @@ def test_many_lists_fill_up_at_once():
     can = np.where((np.arange(S) >= s) & (np.arange(S) <= S - w), m, np.inf)
     np.testing.assert_array_equal(kv.kvpop_mass_step(i32([S] * B), pos, mass, held, s, w, k).cpu().numpy(), can.argmin(-1))
     assert (held == S).all()
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("D,P", [(64, 64), (128, 16), (128, 128)])
+@pytest.mark.parametrize("G,N,lens", [(1, 300, [300, 130]), (4, 100, None), (7, 41, [41, 37])])
+def test_chunks_over_long_lists(fmt, D, P, G, N, lens):
+    """Lists long enough that most workgroups' keys are seen by all rows of 128, and others end inside a workgroup's keys, a
+    page, and the chunk itself."""
+    rng = np.random.default_rng(D + P + G)
+    B, H, per = 2, 2, 1100 // P + 1
+    host = HostCache(rng, B, H, per, P, D, fmt)
+    q, q64 = bf16(rng.standard_normal((B, H * G, N, D)))
+    held, scale = [[per * P, 700], [N + 1, N // 2]], D ** -0.5
+    dev = None if lens is None else i32(lens)
+    cache = host.gpu()
+    _, lse = kv.kvpop_cache_attn(q, cache, i32(held), scale, q_lens=dev)
+    before = rng.random((B, H, per * P)).astype(np.float32)
+    for decay in (1.0, 0.5):
+        mass = torch.from_numpy(before.copy()).cuda()
+        kv.kvpop_cache_mass(q, cache, i32(held), lse, scale, mass, q_lens=dev, decay=decay)
+        check_mass(q64, host, held, scale, lse.double().cpu().numpy(), before, mass.cpu().numpy(), decay, lens)
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("D", [64, 128])
+def test_chunks_over_lists_that_lack_pages(fmt, D):
+    rng = np.random.default_rng(D)
+    B, H, G, N, P, per = 1, 2, 3, 60, 16, 40
+    host = HostCache(rng, B, H, per, P, D, fmt)
+    host.table[0, 0, 5], host.table[0, 0, 20:23], host.table[0, 1, 0] = -1, 10 ** 7, -3
+    q, q64 = bf16(rng.standard_normal((B, H * G, N, D)))
+    held, scale = [[per * P, 500]], D ** -0.5
+    cache = host.gpu()
+    _, lse = kv.kvpop_cache_attn(q, cache, i32(held), scale)
+    before = rng.random((B, H, per * P)).astype(np.float32)
+    mass = torch.from_numpy(before.copy()).cuda()
+    kv.kvpop_cache_mass(q, cache, i32(held), lse, scale, mass, decay=0.75)
+    check_mass(q64, host, held, scale, lse.double().cpu().numpy(), before, mass.cpu().numpy(), 0.75)
+
+
+@pytest.mark.parametrize("T", [32768, 32769, 131072, 300001])
+@pytest.mark.parametrize("G", [1, 4])
+def test_long_prompts(T, G):
+    """On both sides of what stays in registers, to lengths that one workgroup reads many times."""
+    H, s, w, k = 2, 4, 256, 2016
+    rng = np.random.default_rng(T + G)
+    m = np.round(np.exp(rng.standard_normal((1, H * G, T))), 2).astype(np.float32)  # with ties
+    for n in (T, T - 1000):
+        pos, kept, held = kv.kvpop_mass_prompt(torch.from_numpy(m).cuda(), H, s + w + k, s, w, k, lens=i32([n]))
+        assert held.tolist() == [[s + w + k] * H]
+        for h in range(H):
+            a = om.group_mass(m[0, h * G:(h + 1) * G, :n])
+            order = np.lexsort((np.arange(s, n - w), -a[s:n - w].astype(np.float64)))[:k] + s
+            want = np.concatenate([np.arange(s), np.sort(order), np.arange(n - w, n)])
+            np.testing.assert_array_equal(pos[0, h].cpu().numpy(), want)
+            np.testing.assert_array_equal(kept[0, h].cpu().numpy(), a[want])
