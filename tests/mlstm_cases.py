@@ -102,3 +102,53 @@ def check_grads(ref, lens, scale, delay, normalize, o, lse, grads):
 def norm_error(got, want):
     got = got.double().cpu().numpy() if isinstance(got, torch.Tensor) else got
     return float(np.linalg.norm(got - want) / max(np.linalg.norm(want), 1e-300))
+
+
+def partial_sums(x, o, lse, scale, delay, normalize):
+    """Of one head, by token t: G, the sum over the pairs of a token s < t and a read-out at u >= t of
+    W(u, s) (x_u . k_s) (do_u . v_s + d_u), which sigmoid(-fg_t) makes dfg_t; and R, the root of the sum of the squares of
+    W |x . k| times the root of the sum of the squares of what do . v + d adds up. own: that of a token's pair with itself, which
+    is in neither but in both of the terms that a running sum subtracts."""
+    q, k, v, ig, fg, do = (x[n] for n in ("q", "k", "v", "ig", "fg", "do"))
+    T, D = q.shape
+    off = np.isneginf(ig)
+    k, v = om.clean(k, off), om.clean(v, off)
+    n = max(0, T - delay)
+    got = np.zeros(T, bool)
+    got[:n] = ~np.isneginf(lse[:n])
+    L = om.log_weights(ig, fg)
+    P, Q = np.zeros((T, T)), np.zeros((T, T))
+    u = np.flatnonzero(got)
+    if len(u):
+        W = np.exp(L[u + delay] - lse[u][:, None])
+        s = scale * q[u] @ k.T
+        d = -(do[u] * o[u]).sum(1) if normalize else np.zeros(len(u))
+        P[u + delay] = W * s * (do[u] @ v.T + d[:, None])
+        squares = (do[u] ** 2) @ (v.T ** 2) + (((do[u] * o[u]) ** 2).sum(1) if normalize else np.zeros(len(u)))[:, None]
+        Q[u + delay] = (W * s) ** 2 * squares
+    G, R = np.zeros(T), np.zeros(T)
+    forgets = np.asarray(fg) < -2.0 ** 24
+    for y, sums in ((P, G), (Q, R)):  # a token's pairs as a key begin behind it, those as a query end there
+        step = y.sum(0) - y.sum(1)
+        for t in range(1, T):
+            sums[t] = 0.0 if forgets[t] else sums[t - 1] + step[t - 1]
+    return G, np.sqrt(np.maximum(R, 0)), np.sqrt(np.diag(Q))
+
+
+def check_forget(name, got, fg, G, R, own, D):
+    """The forget gates' gradients of one head. Their error is that of sums, relative to the largest of the partial sums since
+    the last gate that forgets everything (or to R where those cancel): in the 2-norm over these tokens, four of at most
+    2^-8 / sqrt(3): the pairs' rounded weights, the read state's elements in dk, o in do . o, the result. Beside it what fp32 leaves
+    where a token's own pair cancels in x . dx - k . dk, sums of D products that are sums of up to 64 terms: (D + 64) 2^-24 of it
+    on each side, independent from token to token. (With f = e^-20 that is more than all other pairs are.)"""
+    sig = np.exp(om.log_sigmoid(-np.asarray(fg, np.float64)))
+    group = np.cumsum(np.asarray(fg) < -2.0 ** 24)
+    for i in range(group[-1] + 1 if len(group) else 0):
+        t = np.flatnonzero(group == i)
+        if not len(t):
+            continue
+        most = max(np.abs(G[t]).max(), R[t].max())
+        most = 4 * U / 3 ** 0.5 * most + 2 * (D + 64) * 2.0 ** -24 * np.linalg.norm(own[t])
+        err, bound = np.linalg.norm(got[t] - sig[t] * G[t]), most * np.linalg.norm(sig[t])
+        assert err <= bound + 1e-30, "%s: tokens %d to %d: error %.3g, bound %.3g, size %.3g" % (
+            name, t[0], t[-1], err, bound, np.linalg.norm(sig[t] * G[t]))
