@@ -563,7 +563,7 @@ __global__ __launch_bounds__(256, 2) void mlstm_segment_kernel(MlstmLaunch a) {
 // replaced by what its segment starts from. Forwards, a given state is where it starts and ends. The
 // exponents' chain is worked out first, by every workgroup; then kAhead parts are on their way. Memory
 // bounds it, with the start of a launch: 32 heads of 16 parts (34 MB, read and written) 12 us.
-constexpr int kScanSegments = 512;  // exponents at once
+constexpr int kScanSegments = 512;  // the most that plan() makes
 template <int D>
 __global__ __launch_bounds__(256) void mlstm_scan_kernel(MlstmLaunch a, int blocks) {
   __shared__ double add_sh[kScanSegments], sum_sh[kScanSegments], top_sh[kScanSegments], from_sh[kScanSegments];
@@ -587,52 +587,49 @@ __global__ __launch_bounds__(256) void mlstm_scan_kernel(MlstmLaunch a, int bloc
     for (int j = 0; j < kAhead; ++j) next[j] = *reinterpret_cast<const f32x4*>(part(min(i0 + j, a.segs - 1)) + (mine ? e : 0));
   };
   fetch(0);
-  for (int base = 0; base < a.segs; base += kScanSegments) {
-    const int count = min(kScanSegments, a.segs - base);
-    __syncthreads();
-    for (int i = tid; i < count; i += 256) {
-      const SegmentScalars* s = scalars(part(base + i), D);
-      add_sh[i] = s->add, sum_sh[i] = s->sum, top_sh[i] = s->top;
-    }
-    __syncthreads();
-    if (tid < 64)  // m -> max(m + sum, add), a wave's segments at a time: such steps compose to one
-      for (int i0 = 0; i0 < count; i0 += 64) {
-        const int i = min(i0 + tid, count - 1);
-        const double none = -__builtin_inf();
-        const bool in = i0 + tid < count;
-        double sum = in ? sum_sh[i] : 0.0, add = in ? add_sh[i] : none, top = in ? top_sh[i] : none;
+  const int count = a.segs;
+  for (int i = tid; i < count; i += 256) {
+    const SegmentScalars* s = scalars(part(i), D);
+    add_sh[i] = s->add, sum_sh[i] = s->sum, top_sh[i] = s->top;
+  }
+  __syncthreads();
+  if (tid < 64)  // m -> max(m + sum, add), a wave's segments at a time: such steps compose to one
+    for (int i0 = 0; i0 < count; i0 += 64) {
+      const int i = min(i0 + tid, count - 1);
+      const double none = -__builtin_inf();
+      const bool in = i0 + tid < count;
+      double sum = in ? sum_sh[i] : 0.0, add = in ? add_sh[i] : none, top = in ? top_sh[i] : none;
 #pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-          const double s = __shfl_up(sum, o), x = __shfl_up(add, o), y = __shfl_up(top, o);
-          if (tid >= o) add = fmax(x + sum, add), top = fmax(y + sum, top), sum += s;
-        }
-        const double after = fmax(m + sum, add), end = fmax(defined + sum, top);
-        const double before = __shfl_up(after, 1);
-        if (in) from_sh[i] = tid ? before : m;
-        m = last_lane(after), defined = last_lane(end);
+      for (int o = 1; o < 64; o <<= 1) {
+        const double s = __shfl_up(sum, o), x = __shfl_up(add, o), y = __shfl_up(top, o);
+        if (tid >= o) add = fmax(x + sum, add), top = fmax(y + sum, top), sum += s;
       }
-    if (tid == 0) last_sh[0] = m, last_sh[1] = defined;
-    __syncthreads();
-    m = last_sh[0], defined = last_sh[1];
-    for (int i = tid; i < count; i += 256) {
-      const double old = from_sh[i] + sum_sh[i], now = i + 1 < count ? from_sh[i + 1] : m;
-      keep_sh[i] = gone(old) ? 0.f : pow2(old - now);
-      put_sh[i] = gone(add_sh[i]) ? 0.f : pow2(add_sh[i] - now);
-      if (blockIdx.x % blocks == 0 && base + i > 0) scalars(part(base + i), D)->from = from_sh[i];
+      const double after = fmax(m + sum, add), end = fmax(defined + sum, top);
+      const double before = __shfl_up(after, 1);
+      if (in) from_sh[i] = tid ? before : m;
+      m = last_lane(after), defined = last_lane(end);
     }
-    __syncthreads();
-    for (int i0 = base; i0 < base + count; i0 += kAhead) {
-      f32x4 now[kAhead];
+  if (tid == 0) last_sh[0] = m, last_sh[1] = defined;
+  __syncthreads();
+  m = last_sh[0], defined = last_sh[1];
+  for (int i = tid; i < count; i += 256) {
+    const double old = from_sh[i] + sum_sh[i], now = i + 1 < count ? from_sh[i + 1] : m;
+    keep_sh[i] = gone(old) ? 0.f : pow2(old - now);
+    put_sh[i] = gone(add_sh[i]) ? 0.f : pow2(add_sh[i] - now);
+    if (blockIdx.x % blocks == 0 && i > 0) scalars(part(i), D)->from = from_sh[i];
+  }
+  __syncthreads();
+  for (int i0 = 0; i0 < count; i0 += kAhead) {
+    f32x4 now[kAhead];
 #pragma unroll
-      for (int j = 0; j < kAhead; ++j) now[j] = next[j];
-      if (i0 + kAhead < a.segs) fetch(i0 + kAhead);
+    for (int j = 0; j < kAhead; ++j) now[j] = next[j];
+    if (i0 + kAhead < count) fetch(i0 + kAhead);
 #pragma unroll
-      for (int j = 0; j < kAhead; ++j)
-        if (i0 + j < base + count) {
-          if (mine) *reinterpret_cast<f32x4*>(part(i0 + j) + e) = x;
-          x = scaled(x, keep_sh[i0 + j - base]) + now[j] * put_sh[i0 + j - base];
-        }
-    }
+    for (int j = 0; j < kAhead; ++j)
+      if (i0 + j < count) {
+        if (mine) *reinterpret_cast<f32x4*>(part(i0 + j) + e) = x;
+        x = scaled(x, keep_sh[i0 + j]) + now[j] * put_sh[i0 + j];
+      }
   }
   if (held) {
     *reinterpret_cast<f32x4*>(held) = gone(m) ? x : x * pow2(m - defined);
@@ -1337,6 +1334,7 @@ int chunk_count(const MlstmLaunch& L) { return (L.T + kChunk - 1) / kChunk; }
 // of more run at once. Few chunks are one segment, since two launches more cost as much as they do (5 chunks of 8 heads:
 // 27 us in segments, 35 as one).
 constexpr int kWantGroups = 512, kFewChunks = 4;
+static_assert(kWantGroups <= kScanSegments, "a head's segments");
 void plan(MlstmLaunch& L) {
   const int chunks = chunk_count(L);
   const int64_t lists = (int64_t)L.B * L.H;
