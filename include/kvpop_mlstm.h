@@ -21,7 +21,9 @@
  * Gates: ig = -inf masks a token (its k and v do not matter then, NaN included), fg = -inf forgets
  * everything exactly (where a packed sequence begins), and so does any fg below -2^24, where an fp32 m or lse
  * has no bits left for another token's gate; fg = +inf forgets nothing. NaN, ig = +inf and
- * elements of the other inputs that are not finite reach the results of their sequence and head only.
+ * elements of the other inputs that are not finite reach the results of their sequence and head only (of all
+ * that is packed into one of B). normalize = 0: a read-out's and a gradient's weights exp(b_u - b_t + ig_t) are fp32
+ * numbers; above 2^127 they are infinite, and NaN where they meet a zero.
  */
 #ifndef KVPOP_MLSTM_H
 #define KVPOP_MLSTM_H
@@ -57,7 +59,8 @@ typedef struct kvpop_mlstm_state {
 } kvpop_mlstm_state;
 
 /* The read-outs of whole sequences. state NULL: from nothing held. Else what is held before the first
- * token goes in, what is held after the last comes out (a sequence of length 0 keeps it).
+ * token goes in, what is held after the last comes out (a sequence of length 0 keeps it). Queries of tokens before
+ * the call that are read in it: delay = 0, and q moved by the delay, theirs first.
  * o: bf16 [B, H, T, D] contiguous; rows that are not read (t + delay >= lens[b]) are 0.
  * lse: fp32 [B, H, T] or NULL: log of x . z (normalize = 1; -inf where that is not > 0) or 0
  * (normalize = 0); -inf for rows that are not read. kvpop_mlstm_bwd takes it.
@@ -88,7 +91,7 @@ size_t kvpop_mlstm_fwd_workspace_size(const kvpop_mlstm* a);
  * o: bf16 [B, H, T, D] contiguous, lse: fp32 [B, H, T].
  * Roundings are those of kvpop_mlstm_fwd; for dq the read state's elements keep 16 bits. With normalize = 1, the
  * rounding of o is taken out of d_u (x . dx = 0 tells it) where neither q nor a key of the sequence up to there
- * has a negative element. dfg is a running sum of differences: its error is relative to the largest of a
+ * (the end of its 64 tokens) has a negative element. dfg is a running sum of differences: its error is relative to the largest of a
  * sequence's partial sums, not to each element, and about 2^-16 of the terms with u = s, which cancel in it.
  * Nothing depends on the order of workgroups. workspace as above (kvpop_mlstm_bwd_workspace_size).
  * Errors as kvpop_mlstm_fwd. */

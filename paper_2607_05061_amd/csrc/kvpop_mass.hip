@@ -91,8 +91,9 @@ __device__ __forceinline__ float lse2(float x) { return x == neg_inf() ? -neg_in
 // each 16 KT keys, with half of the rows each (a lane's chain of sums is the time; twice the waves hide it).
 // Else (16 rows at most) each wave takes them from memory.
 // Few rows: codes are read once, and the waits for length, page and codes, one after the other, bound it: 64 x 8 lists
-// of up to 2276 tokens of 128 in e4m3 23 us. Many rows: exponentials and their sums (about 6 vector instructions a
-// pair): 500 queries of 7 heads on 6 lists of up to 9001 (D = 64, int8) 67 us.
+// of up to 2276 tokens of 128 in e4m3 23 us. Many rows: the chain of a workgroup's rows, 128 after 128, with two waves a SIMD
+// on as many CUs as there are blocks of 128 keys: 500 queries of 7 heads on 6 lists of up to 9001 (D = 64, int8; 163 such blocks see them) 67 us,
+// where the exponentials and their sums (about 6 vector instructions a pair) would take 13-17 spread over all CUs.
 template <int D, int FMT, int KT, bool MANY>
 __global__ __launch_bounds__(64 * kWaves * (MANY ? 2 : 1)) void cache_mass_kernel(CacheMassLaunch a, int blocks) {
   constexpr int KS = D / 32, QS = D + 8;

@@ -946,7 +946,7 @@ __global__ __launch_bounds__(MODE == kDkv ? 512 : 256, 2) void mlstm_kernel(Mlst
 #pragma unroll
       for (int t = 0; t < NT; ++t) acc[q][t] = f32x4{0.f, 0.f, 0.f, 0.f};
     // What is held, rounded to bf16 for the product (its terms' errors are independent; out is rounded too). For dq it
-    // is two bf16: there o's rounding, by way of d, is a third error of that size.
+    // is two bf16: x . dx, which corrects do . o and makes dfg, is taken from its products.
 #pragma unroll
     for (int s = 0; s < D / 32; ++s) {
       bf16x8 sf[NT], low[NT];
@@ -1329,10 +1329,12 @@ __global__ __launch_bounds__(kStepThreads) void mlstm_step_kernel(MlstmLaunch a)
 
 int chunk_count(const MlstmLaunch& L) { return (L.T + kChunk - 1) / kChunk; }
 
-// Segments: enough for two workgroups a CU. A training step of 2 x 8 x 16384 tokens takes 510 us with
-// 512 workgroups, 626 with 768, 617 with 1024: each segment adds a matrix that is written and read twice, and not all
-// of more run at once. Few chunks are one segment, since two launches more cost as much as they do (5 chunks of 8 heads:
-// 27 us in segments, 35 as one).
+// Segments: enough for two workgroups a CU: each adds a matrix that is written and read twice, and not all of more run
+// at once. Few chunks are one segment, since two launches more cost as much as they do. Read-outs + gradients, us, D = 128, wanting 256, 512,
+// 1024 workgroups: 8 heads of 16384 tokens 83 + 245, 76 + 241, 103 + 329; 32 of them 264 + 779, 220 + 692, 232 + 771; 64 heads of 1024
+// 52 + 150, 53 + 164, 78 + 238. One segment up to 2, 4, 8 chunks: 8 heads of 3 chunks 22 + 68, 20 + 60, 20 + 60, of 4 23 + 69, 25 + 75,
+// 25 + 75, of 5 23 + 71, 23 + 71, 30 + 91; 64 heads of 4 32 + 86, 25 + 78, 25 + 78. Off the line: one head of 32768 would take 74 + 181
+// with 256 (117 + 281 so), 304 heads of 8 chunks 61 + 232 as one segment (101 + 333 so).
 constexpr int kWantGroups = 512, kFewChunks = 4;
 static_assert(kWantGroups <= kScanSegments, "a head's segments");
 void plan(MlstmLaunch& L) {

@@ -39,7 +39,7 @@ def test_slow_decays_beside_a_large_m_are_kept():
 
 
 @pytest.mark.parametrize("least", [-3e38, -1e30])
-def test_a_state_below_the_range_of_m_is_empty(least):
+def test_a_state_near_the_end_of_the_range_of_m(least):
     """m = -3e38 and a gate of -1.6e7: m stays where fp32 has it, and what is held with it; nothing becomes NaN."""
     st = kv.KvpopMlstmState(torch.ones(1, 1, 64, 64, device="cuda"), torch.ones(1, 1, 64, device="cuda"), torch.full((1, 1), least, device="cuda"))
     x = [b16(y)[0] for y in (np.ones((1, 1, 64)), np.ones((1, 1, 64)), np.ones((1, 1, 64)), np.full((1, 1), -np.inf), np.full((1, 1), -1.6e7))]
