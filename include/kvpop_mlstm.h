@@ -90,9 +90,9 @@ size_t kvpop_mlstm_fwd_workspace_size(const kvpop_mlstm* a);
  * dig, dfg [B, H, T]; 0 for tokens and queries that take no part. do_: bf16 [B, H, T, D] (strided),
  * o: bf16 [B, H, T, D] contiguous, lse: fp32 [B, H, T].
  * Roundings are those of kvpop_mlstm_fwd; for dq the read state's elements keep 16 bits. With normalize = 1, the
- * rounding of o is taken out of d_u (x . dx = 0 tells it) where neither q nor a key of the sequence up to there
- * (the end of its 64 tokens) has a negative element. dfg is a running sum of differences: its error is relative to the largest of a
- * sequence's partial sums, not to each element, and about 2^-16 of the terms with u = s, which cancel in it.
+ * rounding of o is taken out of d_u (x . dx = 0 tells it). dfg is a running sum of differences: its error is
+ * relative to the largest of a sequence's partial sums, not to each element, and about 2^-16 of the terms with
+ * u = s, which cancel in it.
  * Nothing depends on the order of workgroups. workspace as above (kvpop_mlstm_bwd_workspace_size).
  * Errors as kvpop_mlstm_fwd. */
 typedef struct kvpop_mlstm_grads {

@@ -26,7 +26,6 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
@@ -117,17 +116,6 @@ union Frag {
   bf16x4 h[2];
   u32x2 d[2];
   u32x4 u;
-};
-
-// Whether some bf16 of many is negative (-0 is not): the largest of their bits, two at a time.
-struct Signs {
-  u16x2 most = {0, 0};
-  __device__ __forceinline__ void add(uint32_t w) {
-    union { uint32_t u; u16x2 h; } x;
-    x.u = w;
-    most = __builtin_elementwise_max(most, x.h);
-  }
-  __device__ __forceinline__ bool negative() const { return most.x > 0x8000u || most.y > 0x8000u; }
 };
 
 // 8 elements of a row, 16 bytes.
@@ -242,10 +230,8 @@ struct SegmentScalars {
   double sum;   // log f over the segment, -inf with a reset
   double from;  // the exponent of what it starts from
   double top;   // forwards: what m is after the segment alone
-  int32_t negative;  // forwards: some key has a negative element
-  int32_t pad[3];
 };
-__host__ __device__ constexpr int segment_floats(int D) { return D * D + D + 12; }
+__host__ __device__ constexpr int segment_floats(int D) { return D * D + D + 8; }
 __device__ __forceinline__ SegmentScalars* scalars(float* part, int D) {
   return reinterpret_cast<SegmentScalars*>(part + D * D + D);
 }
@@ -285,20 +271,6 @@ struct Tile {
     }
   }
 };
-
-// The signs of a chunk's rows that have a weight: from the registers, or, where some were cleared, from LDS.
-template <int D, int THREADS>
-__device__ __forceinline__ void add_signs(Signs& signs, const Tile<D, THREADS>& tile, const uint16_t* sh, bool cleared, int tid) {
-  constexpr int kPer = Tile<D, THREADS>::kPer;
-  const uint16_t* at = sh + tid / (D / 8) * Tile<D, THREADS>::kStride + 8 * (tid % (D / 8));
-#pragma unroll
-  for (int i = 0; i < kPer; ++i) {
-    u32x4 x = tile.x[i];
-    if (cleared) x = *reinterpret_cast<const u32x4*>(at + i * (THREADS * 8 / D) * Tile<D, THREADS>::kStride);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) signs.add(x[j]);
-  }
-}
 
 // Rows of a chunk that have no weight become zeros, so that nothing in them (NaN) matters.
 template <int D>
@@ -454,7 +426,6 @@ __global__ __launch_bounds__(256, 2) void mlstm_segment_kernel(MlstmLaunch a) {
 #pragma unroll
   for (int j = 0; j < NZ; ++j) z[j] = f32x4{0.f, 0.f, 0.f, 0.f};
   double m = -__builtin_inf(), sum = 0.0, top = -__builtin_inf();
-  Signs signs;
   auto chunk_at = [&](int i) { return rev ? first + count - 1 - i : first + i; };
 
   RawGates<kDkv> raw;
@@ -485,13 +456,11 @@ __global__ __launch_bounds__(256, 2) void mlstm_segment_kernel(MlstmLaunch a) {
     tb.store(b_sh, chunk_at(i) * kChunk, shift, n, tid);
     tc.store(c_sh, chunk_at(i) * kChunk, shift, n, tid);
     __syncthreads();
-    const bool odd = rev ? G.odd_q[slot] : G.odd_k[slot];
-    if (odd) {
+    if (rev ? G.odd_q[slot] : G.odd_k[slot]) {
       clear_rows<D>(b_sh, (rev ? G.r : G.u) + slot * kChunk, tid, 256);
       clear_rows<D>(c_sh, (rev ? G.r : G.u) + slot * kChunk, tid, 256);
       __syncthreads();
     }
-    add_signs(signs, tb, b_sh, odd, tid);
     if (i + 1 < count) {
       tb.load(rb, b, h, chunk_at(i + 1) * kChunk, shift, n, tid);
       tc.load(rc, b, h, chunk_at(i + 1) * kChunk, shift, n, tid);
@@ -545,9 +514,7 @@ __global__ __launch_bounds__(256, 2) void mlstm_segment_kernel(MlstmLaunch a) {
 #pragma unroll
     for (int r = 0; r < 4; ++r)
       if (c == 0) part[D * D + (wave * NZ + j) * 16 + 4 * g + r] = z[j][r];
-  const int negative = __syncthreads_or(signs.negative());
   if (tid == 0) {
-    scalars(part, D)->negative = negative;
     scalars(part, D)->add = m;
     scalars(part, D)->sum = sum;
     scalars(part, D)->top = top;
@@ -652,8 +619,8 @@ struct Shared {
   __align__(16) uint16_t zrow[MODE == kFwd ? 2 * (D + 8) : 8];  // z's high and low bf16 parts
   __align__(16) float far[kRoles][kChunk], far_z[kRoles][kChunk], out[kChunk];
   __align__(16) float z[kRoles][D];
-  float dig[4][kChunk];  // backward: the waves' parts of x . dx, of k . dk
-  int negative[4];       // kDq: the waves' keys up to here have negative elements
+  float dig[4][kChunk];  // backward: the waves' parts of x . dx (of what is held), of k . dk
+  float dig_z[MODE == kDq ? 4 : 1][kChunk];  // kDq: of x . z
 };
 
 // One workgroup per segment of a head. 4 waves (for dk and dv 4 each, over the same tiles): wave w takes
@@ -665,7 +632,7 @@ struct Shared {
 // Chunks follow each other, and the phases of one wait for each other: two waves a SIMD (256 registers a lane; two
 // workgroups a CU, of dk and dv one) fill part of the waits, and neither the products nor HBM are busy
 // all the time. D = 128: read-outs of 4 x 8 x 32768 tokens 266 us (1.07 GB: 4.0 TB/s), of 2 x 8 x 16384 76 us; dq there
-// 120 us, dk and dv 161 us. Twice the waves with 16 columns each needed more registers than they have: read-outs
+// 118 us, dk and dv 161 us. Twice the waves with 16 columns each needed more registers than they have: read-outs
 // 493 us where 4 waves took 277.
 template <int D, int MODE>
 __global__ __launch_bounds__(MODE == kDkv ? 512 : 256, 2) void mlstm_kernel(MlstmLaunch a) {
@@ -729,10 +696,6 @@ __global__ __launch_bounds__(MODE == kDkv ? 512 : 256, 2) void mlstm_kernel(Mlst
     if (MODE == kFwd) set_zrow(tid, z);
   }
   double defined = m;
-  Signs signs;
-  if (MODE == kDq)
-    for (int i = tid; i < seg; i += THREADS)
-      if (scalars(a.parts + ((int64_t)list * a.segs + i) * segment_floats(D), D)->negative) signs.add(0xFFFFFFFFu);
 
   if (REV) {
     // At the end of the segment: what is held there times its gradient.
@@ -772,7 +735,7 @@ __global__ __launch_bounds__(MODE == kDkv ? 512 : 256, 2) void mlstm_kernel(Mlst
 
   for (int it = 0; it < count; ++it) {
     // Addresses are made anew in every chunk (kDq, and D = 64): held over them all, they took so many registers that
-    // others went to memory, whose waits are those of the tiles on their way (dq of 2 x 8 x 16384 of 128 187 us, 120 so; a training
+    // others went to memory, whose waits are those of the tiles on their way (dq of 2 x 8 x 16384 of 128 187 us, 118 so; a training
     // step of 4 x 8 x 4096 of 64 170 us, 159 so).
     int tid_now = tid;
     if (MODE == kDq || D == 64) asm volatile("" : "+v"(tid_now));
@@ -787,8 +750,7 @@ __global__ __launch_bounds__(MODE == kDkv ? 512 : 256, 2) void mlstm_kernel(Mlst
     t2.store(sh.tile[2], chunk * kChunk, late2, n, tid);
     if (REV) t3.store(sh.tile[REV ? 3 : 0], chunk * kChunk, a.delay, n, tid);
     __syncthreads();
-    const bool odd = G.odd_k[slot] | (MODE != kFwd ? G.odd_q[slot] : 0);
-    if (odd) {
+    if (G.odd_k[slot] | (MODE != kFwd ? G.odd_q[slot] : 0)) {
       if (MODE == kFwd) {
         clear_rows<D>(sh.tile[1], G.u + at, tid, THREADS);
         clear_rows<D>(sh.tile[2], G.u + at, tid, THREADS);
@@ -803,11 +765,6 @@ __global__ __launch_bounds__(MODE == kDkv ? 512 : 256, 2) void mlstm_kernel(Mlst
         clear_rows<D>(sh.tile[REV ? 3 : 0], G.r + at, tid, THREADS);
       }
       __syncthreads();
-    }
-    if (MODE == kDq) {
-      add_signs(signs, t2, sh.tile[2], odd, tid);
-      const bool negative = __builtin_amdgcn_ballot_w64(signs.negative()) != 0;
-      if (lane == 0) sh.negative[wave] = negative;
     }
     if (it + 1 < count) load(chunk_at(it + 1), tid);
 
@@ -877,7 +834,7 @@ __global__ __launch_bounds__(MODE == kDkv ? 512 : 256, 2) void mlstm_kernel(Mlst
             p[r] = (__bf16)acc[x][r];
             if (MODE == kFwd) den += acc[x][r], rounded += (float)p[r], bits |= __float_as_uint(acc[x][r]);
           }
-          *reinterpret_cast<bf16x4*>(sh.p[role] + j * PS + 32 * half + 16 * x + 4 * g) = p;
+          if (MODE != kDq) *reinterpret_cast<bf16x4*>(sh.p[role] + j * PS + 32 * half + 16 * x + 4 * g) = p;
           if (MODE == kDq) {
             weighted[2 * half + x] = acc[x];
 #pragma unroll
@@ -916,7 +873,7 @@ __global__ __launch_bounds__(MODE == kDkv ? 512 : 256, 2) void mlstm_kernel(Mlst
       }
       if (g == 0) {
         sh.far[role][j] = far;
-        if (MODE != kFwd) sh.far_z[role][j] = MODE == kDq ? far * alpha : far;
+        if (REV) sh.far_z[role][j] = far;
       }
     }
     if (role == 0 && wave == (REV ? 3 : 0)) {  // the wave that has the least of it
@@ -930,12 +887,14 @@ __global__ __launch_bounds__(MODE == kDkv ? 512 : 256, 2) void mlstm_kernel(Mlst
     const double added = up.added(G, slot), gates_sum = G.resets[slot] ? -__builtin_inf() : G.sum[slot];
 
     const int t_0 = chunk * kChunk;
-    bf16x4 rows_q[MODE == kDq ? 4 : 1][NT];  // dq's rows of q (dk's rows of k are in LDS), on their way
+    // dq's rows of q (dk's rows of k are in LDS): this wave's columns of all of them on their way.
+    auto q_row = [&](int j) __attribute__((always_inline)) { return min(max(t_0 + j - a.delay, 0), n - 1); };
+    bf16x4 rows_q[MODE == kDq ? 4 : 1][NT];
     if (MODE == kDq) {
-      const uint16_t* from = a.q.ptr + b * a.q.sb + h * a.q.sh + wave * NT * 16 + 4 * g;
+      const uint16_t* from = a.q.ptr + b * a.q.sb + h * a.q.sh;
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        const uint16_t* p = from + min(max(t_0 + 16 * q + c - a.delay, 0), n - 1) * a.q.st;
+        const uint16_t* p = from + q_row(16 * q + c) * a.q.st + wave * NT * 16 + 4 * g;
 #pragma unroll
         for (int t = 0; t < NT; ++t) rows_q[MODE == kDq ? q : 0][t] = *reinterpret_cast<const bf16x4*>(p + 16 * t);
       }
@@ -975,7 +934,7 @@ __global__ __launch_bounds__(MODE == kDkv ? 512 : 256, 2) void mlstm_kernel(Mlst
       for (int t = 0; t < NT; ++t) cf[s][t] = column8(c_sh + 32 * s * LS + (wave * NT + t) * 16, LS, g, c);
     // Columns 16 t + 4 g + 0 .. 3 of the wave's of row 16 q + c.
     auto result = [&](int q, int t, float far, float far_z, float fac) __attribute__((always_inline)) {
-      f32x4 y = scaled(acc[q][t], far);
+      f32x4 y = MODE == kDq ? acc[q][t] : scaled(acc[q][t], far);
       if (MODE != kFwd && with_z) y += scaled(*reinterpret_cast<const f32x4*>(sh.z[role] + (wave * NT + t) * 16 + 4 * g), far_z);
 #pragma unroll
       for (int s = 0; s < 2; ++s)
@@ -985,50 +944,76 @@ __global__ __launch_bounds__(MODE == kDkv ? 512 : 256, 2) void mlstm_kernel(Mlst
     };
     // A normalised read-out does not change with the size of x, so x . dx = 0, and what comes out for it is the error of
     // do . o: of the rounding of o, which is not small beside do . (v - o) where a query sees few tokens, by whatever gates and
-    // features. So the rows' x . dx is taken first, and the masked product's do . v - do . o corrected with it. Not where
-    // q (NaN tells) or a key up to here has a negative element: then a row's terms can cancel in x . dx, and what their
-    // roundings leave may be far larger than the error of do . o.
-    if (MODE == kDq && a.normalize && !(sh.negative[0] | sh.negative[1] | sh.negative[2] | sh.negative[3])) {
+    // features. So x . dx is taken first, from the masked product in 32 bits and <x, k> (its rounded elements would leave more than
+    // the error where features of either sign cancel), and do . v - do . o corrected with it. What is rounded then gives
+    // the x . dx that the forget gates' gradients are made of.
+    if (MODE == kDq) {
 #pragma unroll
-      for (int q0 = 0; q0 < 4; q0 += 2) {
-        float dot[2] = {0.f, 0.f};
+      for (int q = 0; q < 4; ++q) {
+        const int j = 16 * q + c;
+        const float far = sh.far[role][j];
+        float dot = 0.f, dot_z = 0.f;
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          const int q = q0 + x, j = 16 * q + c;
-          const float far = sh.far[role][j], far_z = sh.far_z[role][j];
-          Signs row;
+        for (int t = 0; t < NT; ++t) {
+          acc[q][t] = scaled(acc[q][t], far);
+          const f32x4 z = *reinterpret_cast<const f32x4*>(sh.z[role] + (wave * NT + t) * 16 + 4 * g);
 #pragma unroll
-          for (int t = 0; t < NT; ++t) {
-            const f32x4 y = result(q, t, far, far_z, a.scale);
-            union { bf16x4 h; u32x2 u; } w;
-            w.h = rows_q[MODE == kDq ? q : 0][t];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) dot[x] += y[r] * (float)w.h[r];
-            row.add(w.u[0]), row.add(w.u[1]);
+          for (int r = 0; r < 4; ++r) {
+            const float x = (float)rows_q[MODE == kDq ? q : 0][t][r];
+            dot += acc[q][t][r] * x, dot_z += z[r] * x;
           }
-          dot[x] = sum_groups(row.negative() ? __builtin_nanf("") : dot[x]);
-          asm volatile("" : "+v"(dot[x]));
         }
-#pragma unroll
-        for (int x = 0; x < 2; ++x)
-          if (g == 0) sh.dig[wave][16 * (q0 + x) + c] = dot[x];
+        dot = sum_groups(dot), dot_z = sum_groups(dot_z);
+        asm volatile("" : "+v"(dot), "+v"(dot_z));
+        if (g == 0) sh.dig[wave][j] = dot, sh.dig_z[MODE == kDq ? wave : 0][j] = far == 0.f ? 0.f : far * dot_z;
       }
+      bf16x8 row_q[D / 32];  // all of the wave's own rows, which the caches have by now
+      const uint16_t* p = a.q.ptr + b * a.q.sb + h * a.q.sh + q_row(16 * wave + c) * a.q.st + 8 * g;
+#pragma unroll
+      for (int s = 0; s < D / 32; ++s) row_q[s] = row8(p + 32 * s);
+      f32x4 score[4];
+      float in = 0.f;
+#pragma unroll
+      for (int kt = 0; kt < 4; ++kt) {
+        if (kt / 2 > wave / 2) continue;
+        score[kt] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int s = 0; s < D / 32; ++s) score[kt] = mfma(row8(c_sh + (16 * kt + c) * LS + 32 * s + 8 * g), row_q[s], score[kt]);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) in += weighted[kt][r] * score[kt][r];
+      }
+      in = sum_groups(in);
       __syncthreads();
       const int j = 16 * wave + c, t = t_0 + j;
-      float x = sh.dig[0][j] + sh.dig[1][j] + sh.dig[2][j] + sh.dig[3][j];
-      if (x != x || gone(G.r[at + j])) x = 0.f;
+      const bool read = !gone(G.r[at + j]);
+      float held = 0.f, held_z = 0.f;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) held += sh.dig[w][j], held_z += sh.dig_z[MODE == kDq ? w : 0][j];
+      float d = G.d[at + j], x = 0.f;
+      if (a.normalize && read) x = a.scale * (held + d * held_z + in);
+      if (x != x) x = 0.f;
+      d -= x;
+      in = 0.f;
 #pragma unroll
       for (int kt = 0; kt < 4; ++kt) {
         if (kt / 2 > wave / 2) continue;
         bf16x4 p;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) p[r] = (__bf16)(weighted[kt][r] - x * (float)weight[kt][r]);
+        for (int r = 0; r < 4; ++r) {
+          p[r] = (__bf16)(weighted[kt][r] - x * (float)weight[kt][r]);
+          in += (float)p[r] * score[kt][r];
+        }
         *reinterpret_cast<bf16x4*>(sh.p[role] + j * PS + 16 * kt + 4 * g) = p;
       }
+      in = sum_groups(in);
       if (g == 0) {
-        const float d = G.d[at + j] - x;
         sh.far_z[role][j] = sh.far[role][j] * d;
-        if (t >= a.delay && t < n) a.dots[(int64_t)list * a.T + t - a.delay] = -d;
+        if (t < n) {
+          const bool mine = t >= a.delay;
+          // A row that is not read has dx = 0, whatever q holds.
+          a.xdx[(int64_t)list * a.T + t] = mine && read ? a.scale * (held + d * held_z + in) : 0.f;
+          if (a.normalize && mine) a.dots[(int64_t)list * a.T + t - a.delay] = -d;
+        }
       }
       __syncthreads();
     }
@@ -1048,15 +1033,14 @@ __global__ __launch_bounds__(MODE == kDkv ? 512 : 256, 2) void mlstm_kernel(Mlst
           for (int t = 0; t < NT; ++t) {
             acc[q][t] = result(q, t, far, far_z, fac);
             bf16x4 with;
-            if (MODE == kDq) with = rows_q[MODE == kDq ? q : 0][t];
             if (REV) with = *reinterpret_cast<const bf16x4*>(sh.tile[0] + j * LS + (wave * NT + t) * 16 + 4 * g);
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
               y[x][t][r] = (__bf16)acc[q][t][r];
-              if (MODE != kFwd) dot[x] += acc[q][t][r] * (float)with[r];
+              if (REV) dot[x] += acc[q][t][r] * (float)with[r];
             }
           }
-          if (MODE != kFwd) dot[x] = sum_groups(dot[x]);
+          if (REV) dot[x] = sum_groups(dot[x]);
         }
         // The values are made before the branch: where the products' results were first read behind one, the
         // compiler had left out the wait that they need.
@@ -1070,8 +1054,7 @@ __global__ __launch_bounds__(MODE == kDkv ? 512 : 256, 2) void mlstm_kernel(Mlst
           if (t_0 + j >= late && t_0 + j < n)
 #pragma unroll
             for (int t = 0; t < NT; ++t) *reinterpret_cast<bf16x4*>(to + 16 * (q0 + x) * D + 16 * t) = y[x][t];
-          // A row that is not read has dx = 0, whatever q holds.
-          if (MODE != kFwd && g == 0 && (MODE == kDq || role)) sh.dig[wave][j] = MODE == kDq && gone(G.r[at + j]) ? 0.f : dot[x];
+          if (REV && g == 0 && role) sh.dig[wave][j] = dot[x];
         }
       }
     }
@@ -1112,16 +1095,12 @@ __global__ __launch_bounds__(MODE == kDkv ? 512 : 256, 2) void mlstm_kernel(Mlst
     }
     m = up.next;
     __syncthreads();
-    if (MODE != kFwd && tid < kChunk) {
+    if (REV && tid < kChunk) {
       const int t = chunk * kChunk + tid;
       if (t < n) {
         const float x = sh.dig[0][tid] + sh.dig[1][tid] + sh.dig[2][tid] + sh.dig[3][tid];
-        if (REV) {
-          a.dig32[(int64_t)list * a.T + t] = x;
-          a.dig[(int64_t)list * a.T + t] = bf16_bits(x);
-        } else {
-          a.xdx[(int64_t)list * a.T + t] = t >= a.delay ? x : 0.f;
-        }
+        a.dig32[(int64_t)list * a.T + t] = x;
+        a.dig[(int64_t)list * a.T + t] = bf16_bits(x);
       }
     }
   }
