@@ -736,7 +736,7 @@ __global__ __launch_bounds__(MODE == kDkv ? 512 : 256, 2) void mlstm_kernel(Mlst
   for (int it = 0; it < count; ++it) {
     // Addresses are made anew in every chunk (kDq, and D = 64): held over them all, they took so many registers that
     // others went to memory, whose waits are those of the tiles on their way (dq of 2 x 8 x 16384 of 128 187 us, 118 so; a training
-    // step of 4 x 8 x 4096 of 64 170 us, 159 so).
+    // step of 4 x 8 x 4096 of 64 170 us, 155 so).
     int tid_now = tid;
     if (MODE == kDq || D == 64) asm volatile("" : "+v"(tid_now));
     const int tid = tid_now, lane = tid & 63, g = lane >> 4, c = lane & 15;
